@@ -467,6 +467,166 @@ int cocktail_selftest_arithmetic(uint64_t* mismatches, void* stream);
  */
 int cocktail_plan_field(const void* plan_host, const char* name, int32_t index, int64_t* value);
 
+/* ======================================= A paged cache in 4 bits ======================================= */
+
+/*
+ * Sequences of a serving batch whose K and V live in pages: which pages a sequence has, how long it is, and how many sequences
+ * hold a page.  All of it lives on the device, so that a generation loop needs no host round trip and can be captured into a
+ * graph.  Any number of pools (K and V of every layer) can be addressed by one table.
+ *
+ *   table     page of every page_size tokens of a sequence, in token order; -1 behind the ceil(len / page_size) pages it has
+ *   seq_lens  tokens of the sequence
+ *   refs      table entries that name the page; 0 = free
+ *   status    [0]: 0, or why the last cocktail_pages_resize did nothing: the number of pages that were missing, -1 if a row of
+ *             the table was too short, -2 if a shared page had to be copied and no pools were given; [1..3] zero
+ * To start with every entry of the table is -1 and the rest is zero.
+ */
+#define COCKTAIL_MAX_SEQS 4096
+#define COCKTAIL_MAX_POOLS 256
+typedef struct cocktail_page_table {
+  int32_t* table;       /* DEVICE [num_seqs][table_stride]                                            */
+  int32_t* seq_lens;    /* DEVICE [num_seqs]                                                          */
+  int32_t* refs;        /* DEVICE [num_pages]                                                         */
+  int32_t* status;      /* DEVICE [4]                                                                 */
+  int32_t num_seqs;     /* 1 .. COCKTAIL_MAX_SEQS                                                     */
+  int32_t table_stride; /* pages a sequence can have; table_stride * page_size < 2^31                 */
+  int32_t page_size;    /* tokens per page                                                            */
+  int32_t num_pages;    /* pages of every pool                                                        */
+} cocktail_page_table;
+
+/* Bytes of the workspace that cocktail_pages_resize and cocktail_pages_compact take (host only). */
+int cocktail_pages_workspace(const cocktail_page_table* pages, size_t* bytes);
+
+/*
+ * Every sequence b becomes delta[b] tokens longer (shorter if negative; never shorter than 0, so that a large negative value
+ * frees the sequence).  Pages behind the new end are given back (refs - 1).  Pages that are lacking are taken: the lowest-numbered
+ * ones that were free when the call began, sequence after sequence.  A sequence that grows out of a partly filled page which
+ * other sequences hold takes a copy of it first (before its further pages), so that what it stores there is its own; where a page
+ * is held by growing sequences only, the last of them keeps it.  The copies are made in all `num_pools` pools.
+ * All or nothing: if pages are lacking, or the table has too few columns, nothing changes and status[0] says so; the
+ * cocktail_fp4_store calls that follow then store nothing, until a resize succeeds.
+ *
+ *   delta       DEVICE int32 [num_seqs]
+ *   pools       HOST array of DEVICE pointers to pools of num_pages pages of page_bytes bytes each; 16-byte aligned
+ *   num_pools   0 .. COCKTAIL_MAX_POOLS; with 0 nothing can be copied: for callers whose sequences share no partly filled pages
+ *               (where one has to be, nothing is done and status[0] is -2)
+ *   page_bytes  a multiple of 16
+ *   workspace   DEVICE, cocktail_pages_workspace bytes, 16-byte aligned, not initialised
+ *
+ * One launch, and one for the copies if there are pools.  Errors: EINVAL, EALIGN, ENOSPACE, EHIP.
+ */
+int cocktail_pages_resize(const cocktail_page_table* pages, const int32_t* delta, void* const* pools, int32_t num_pools,
+                          int64_t page_bytes, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Forks: sequence b becomes what sequence source[b] was before the call, sharing its pages (also a partly filled last one, see
+ * cocktail_pages_resize).  source[b] == b leaves it as it is, a negative source frees it; a source that is no sequence
+ * (>= num_seqs) leaves it as it is too.  A step of a beam search is one call; no page is copied.
+ *
+ *   source  DEVICE int32 [num_seqs]
+ *
+ * One launch.  Errors: EINVAL, EALIGN, EHIP.
+ */
+int cocktail_pages_fork(const cocktail_page_table* pages, const int32_t* source, void* stream);
+
+/*
+ * Compaction: with n pages in use, the i-th page in use behind the first n moves to the i-th free page among them, in all pools,
+ * and the table and the references follow; afterwards pages 0 .. n-1 are in use.  Arguments as cocktail_pages_resize.
+ * Two launches.  Errors: EINVAL, EALIGN, ENOSPACE, EHIP.
+ */
+int cocktail_pages_compact(const cocktail_page_table* pages, void* const* pools, int32_t num_pools, int64_t page_bytes,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Diagnostic: waits for `stream` and reads status[0] (synchronises and copies).  COCKTAIL_OK, or COCKTAIL_ESTATE if the last
+ * cocktail_pages_resize could not be done.  Other errors: EINVAL, EHIP. */
+int cocktail_pages_check(const cocktail_page_table* pages, void* stream);
+
+/*
+ * A paged cache that holds K and V in microscaled 4-bit floating point (1 bit sign, 2 bits exponent, 1 bit mantissa, and an
+ * 8-bit power of two per 32 channels), from the first token on and for every token: 4.25 bits a value.  One pool per layer.
+ *
+ * Page: num_kv_heads runs, one per head, each of page_size * (D + D/16) bytes:
+ *   K codes   token i, channel c: byte i * D/2 + c/2, low half for even channels
+ *   V codes   in quads of tokens: token i, byte y = c/2: (i/4) * 2D + (y/4) * 16 + (i%4) * 4 + y%4, low half for even channels
+ *   K scales  token i, group g of 32 channels: byte i * D/32 + g
+ *   V scales  token i, group g: byte (i/4) * D/8 + g * 4 + i%4
+ * (Sixteen tokens of K are what the lanes of a wave hold as one operand of a matrix instruction, 16 bytes of contiguous memory
+ * each; a quad of V is a piece of sixteen bytes per eight channels, so that a lane has tokens side by side.  No byte
+ * is shared by two tokens.)
+ *
+ * Quantizer, per token, kv head and group of 32 channels, K and V alike (every step exact in binary32):
+ *   e     = clamp(floor(log2(max |x|)) - 2, -23, 13); -23 if all are zero; scale byte = e + 127
+ *   code  = sign of x, and the number of the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| * 2^-e (ties to the even number,
+ *           6 beyond 6)
+ * Value of a code: exact in fp16 and bf16.  Beyond 49152 = 6 * 2^13 values saturate (infinities too); NaN is stored as 0.
+ */
+typedef struct cocktail_fp4_cache {
+  cocktail_page_table pages; /* page_size a multiple of 16 up to 65536                                */
+  void* pool;                /* DEVICE num_pages pages of cocktail_fp4_page_bytes, 16-byte aligned    */
+  int32_t num_kv_heads;
+  int32_t head_dim;          /* 64 or 128                                                             */
+} cocktail_fp4_cache;
+
+#define COCKTAIL_FP16 0
+#define COCKTAIL_BF16 1
+
+int cocktail_fp4_page_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int64_t* bytes);
+
+/*
+ * Stores new tokens: row t of k and v, starts[b] <= t < starts[b+1], is quantized into the cache as one of the last
+ * n = starts[b+1] - starts[b] tokens of sequence b (token seq_lens[b] - n + t - starts[b]).  Call cocktail_pages_resize first: it
+ * makes the room and counts the tokens.  Rows for tokens before the first, or behind what the table row can hold, or on a page that
+ * is no page of the pool, are left out.  Nothing else in the pool is written.
+ *
+ *   k, v      DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d; strides in elements, multiples of 8
+ *   dtype     COCKTAIL_FP16 or COCKTAIL_BF16
+ *   total     rows; 0 is fine
+ *   starts    DEVICE int32 [num_seqs + 1], ascending from 0 to total, or NULL: total / num_seqs rows for every sequence
+ *             (total a multiple of num_seqs).  A sequence whose range is not within [0, total] is left out.
+ *
+ * One launch.  Errors: EINVAL, EUNSUPPORTED (head_dim), EALIGN, EHIP.
+ */
+int cocktail_fp4_store(const cocktail_fp4_cache* cache, const void* k, const void* v, int32_t dtype, int64_t stride_t,
+                       int64_t stride_h, int64_t total, const int32_t* starts, void* stream);
+
+/*
+ * Reads tokens back as the values they stand for: the counterpart of cocktail_fp4_store, with the same rows and arguments.  Rows
+ * that cocktail_fp4_store leaves out are zeros, but those of a sequence with a bad range are not written.  (With
+ * starts = prefix sums of seq_lens: whole contexts, for instance for cocktail_reorder_quantize.)  One launch.
+ */
+int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32_t dtype, int64_t stride_t, int64_t stride_h,
+                        int64_t total, const int32_t* starts, void* stream);
+
+/*
+ * Attention of the newest tokens of every sequence over its cached keys, themselves included (causal): with n = starts[b+1] -
+ * starts[b] queries and len = seq_lens[b], query i of sequence b attends to tokens 0 .. len - n + i.  One query per sequence is a
+ * decode step, some are the verification of drafts, many a prompt or a part of one; a batch may mix them.
+ *     out[t,h] = softmax(sm_scale * q[t,h] . K^T) V,   kv head h / (num_q_heads / num_kv_heads)
+ * Products and sums in binary32, K and V as stored, softmax weights rounded to fp16 (relative 2^-12) relative to a maximum that is
+ * at most 2^8 too small.  bf16 queries are used as fp16 times a power of two of their own (exact, but for channels below 2^-14
+ * of the largest).
+ *
+ *   q         DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d, strides multiples of 8
+ *   dtype     of q and out
+ *   total, starts   as cocktail_fp4_store
+ *   max_new   no sequence has more queries (a sequence that has is left out); with starts == NULL it has to be total / num_seqs
+ *   max_len   about the length of the longest sequence, for the split of the work only (results do not depend on it but for the order
+ *             of sums); <= 0: as many as the table can hold
+ *   sm_scale  <= 0 selects 1/sqrt(D)
+ *   out       DEVICE [total][num_q_heads][D], 16-byte aligned; zeros for a query without keys
+ *   lse       DEVICE fp32 [total][num_q_heads] natural log-sum-exp (-inf without keys), or NULL
+ *   workspace DEVICE, at least cocktail_fp4_attention_workspace bytes for the same sizes, 16-byte aligned, not initialised; calls
+ *             that share one must not overlap in time
+ *
+ * Keys on a page that is no page of the pool are left out.  Calls on the same inputs agree bit for bit.
+ * num_q_heads / num_kv_heads from 1 to COCKTAIL_MAX_Q_PER_KV.  Up to four launches.  Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
+ */
+int cocktail_fp4_attention_workspace(const cocktail_fp4_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,
+                                     int32_t max_len, int32_t uniform, size_t* bytes);
+int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t num_q_heads, const void* q, int32_t dtype, int64_t stride_t,
+                           int64_t stride_h, int64_t total, const int32_t* starts, int32_t max_new, int32_t max_len,
+                           float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Message of the last failure on the calling thread ("" if none).  Static storage. */
 const char* cocktail_last_error(void);
 

@@ -21,6 +21,8 @@ STATIC_WORKSPACE_BYTES = 16 << 20
 
 OK, EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP, ESTATE = 0, -1, -2, -3, -4, -5, -6
 SRC_STRIDED, SRC_RAGGED = 0, 1
+FP16, BF16 = 0, 1
+MAX_SEQS, MAX_POOLS = 4096, 256
 
 
 class Shape(C.Structure):
@@ -53,6 +55,15 @@ class PagedSource(C.Structure):
                 ("stride_page", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64)]
 
 
+class PageTableDesc(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("seq_lens", C.c_void_p), ("refs", C.c_void_p), ("status", C.c_void_p),
+                ("num_seqs", C.c_int32), ("table_stride", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int32)]
+
+
+class Fp4CacheDesc(C.Structure):
+    _fields_ = [("pages", PageTableDesc), ("pool", C.c_void_p), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
 EXPORTS = {
     "cocktail_plan": (C.c_int, [C.POINTER(Shape), C.POINTER(C.c_int32), C.POINTER(C.c_uint8), C.c_int32,
                                 C.POINTER(Sizes), C.c_void_p, C.c_size_t, C.POINTER(C.c_int32),
@@ -81,6 +92,22 @@ EXPORTS = {
     "cocktail_default_workers": (C.c_int, [C.POINTER(Shape), C.POINTER(C.c_int32)]),
     "cocktail_stream_read_probe": (C.c_int, [C.c_void_p, C.c_size_t, C.c_void_p, C.POINTER(C.c_size_t), C.c_void_p]),
     "cocktail_selftest_arithmetic": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "cocktail_pages_workspace": (C.c_int, [C.POINTER(PageTableDesc), C.POINTER(C.c_size_t)]),
+    "cocktail_pages_resize": (C.c_int, [C.POINTER(PageTableDesc), C.c_void_p, C.POINTER(C.c_void_p), C.c_int32, C.c_int64, C.c_void_p,
+                                        C.c_size_t, C.c_void_p]),
+    "cocktail_pages_fork": (C.c_int, [C.POINTER(PageTableDesc), C.c_void_p, C.c_void_p]),
+    "cocktail_pages_compact": (C.c_int, [C.POINTER(PageTableDesc), C.POINTER(C.c_void_p), C.c_int32, C.c_int64, C.c_void_p, C.c_size_t,
+                                         C.c_void_p]),
+    "cocktail_pages_check": (C.c_int, [C.POINTER(PageTableDesc), C.c_void_p]),
+    "cocktail_fp4_page_bytes": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]),
+    "cocktail_fp4_store": (C.c_int, [C.POINTER(Fp4CacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                     C.c_void_p]),
+    "cocktail_fp4_gather": (C.c_int, [C.POINTER(Fp4CacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                      C.c_void_p]),
+    "cocktail_fp4_attention_workspace": (C.c_int, [C.POINTER(Fp4CacheDesc), C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                                   C.POINTER(C.c_size_t)]),
+    "cocktail_fp4_attention": (C.c_int, [C.POINTER(Fp4CacheDesc), C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                         C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "cocktail_last_error": (C.c_char_p, []),
     "cocktail_version": (C.c_int, []),
 }

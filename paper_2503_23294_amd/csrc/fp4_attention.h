@@ -1,0 +1,70 @@
+// What the kernels of cocktail_fp4_attention share.
+#pragma once
+#include <type_traits>
+
+#include "fp4_common.h"
+
+namespace cocktail {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kNoMax = -3.0e38f;      // reference maximum of a row that has seen no key
+constexpr float kMaxSlack = 8.0f;       // a reference maximum may be this much too small (base 2) before it is raised: weights up to 2^8
+constexpr int kUnit = 32;               // tokens that a wave of the decode kernel takes at a time
+constexpr int kDecodeRows = 32;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
+constexpr int kDecodeWaves = 4;         // waves per workgroup there
+constexpr int kTileKeys = 64;           // keys per step of the tile kernel
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Fp4Attention {
+  Fp4Batch batch;
+  const char* q;
+  char* out;
+  float* lse;
+  int64_t stride_t, stride_h;   // of q, bytes
+  int32_t rep, bf16;            // query heads per kv head
+  float scale;                  // sm_scale * log2(e)
+  int32_t rows;                 // most rows that a partial state of the decode kernel has: min(max_new * rep, kDecodeRows)
+  int32_t workers;              // waves of the decode kernel
+  int32_t decode_rows;          // sequences with at most so many rows are the decode kernel's, the others the tile kernel's
+  int32_t splits;               // parts that the tile kernel cuts the keys of a row into
+  int32_t* prefix;              // workspace: units of the sequences before b [num_seqs + 1], then units per worker
+  float* part_ml;               // (m, l, l unrounded) of the partial states
+  float* part_o;                // their weighted sums
+  float* tile_ml;
+  float* tile_o;
+};
+
+// A sequence as one kernel sees it: its rows (none if they are the other kernel's), tokens.
+struct Fp4Seq {
+  int first, n, len;
+};
+
+__device__ __forceinline__ Fp4Seq decode_seq(const Fp4Attention& a, int b) {
+  const Fp4Span s = fp4_span(a.batch, b);
+  return {s.first, s.count * a.rep <= a.decode_rows ? s.count : 0, fp4_len(a.batch, b)};
+}
+
+__device__ __forceinline__ int decode_units(const Fp4Seq& s) { return s.n > 0 ? (s.len + kUnit - 1) / kUnit : 0; }
+
+__device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
+  const _Float16 a = _Float16(lo), b = _Float16(hi);
+  return as_u32(h2{a, b});
+}
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi, int bf16) {
+  if (!bf16) return pack_halves(lo, hi);
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, b2{__bf16(lo), __bf16(hi)});
+}
+// Two bf16 in a word as floats.
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+
+// Power of two that brings a row of bf16 values, the largest of which is `top`, below 2; 1 for rows of zeros.  Not far from the ends of
+// the range, where its reciprocal would be lost.
+__device__ __forceinline__ float row_factor(float top) {
+  const uint32_t e = __builtin_bit_cast(uint32_t, top) >> 23;
+  return top == 0.f ? 1.f : __builtin_bit_cast(float, (e < 20u ? 20u : e > 230u ? 230u : e) << 23);
+}
+
+}  // namespace cocktail

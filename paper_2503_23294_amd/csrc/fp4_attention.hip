@@ -1,0 +1,218 @@
+// cocktail_fp4_attention: which kernel serves which sequences, the merge of partial states, the C entry.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <type_traits>
+
+#include "fp4_decode_impl.h"
+#include "fp4_tiles_impl.h"
+
+namespace cocktail {
+
+// One wave per (new token, query head): joins the partial states of its row, if it has more than one, and writes rows without keys.
+template <int HD>
+__global__ __launch_bounds__(256) void fp4_merge_kernel(Fp4Attention a) {
+  constexpr int kPer = HD / 64;
+  const Fp4Batch& bt = a.batch;
+  const int lane = threadIdx.x & 63;
+  const int heads = bt.num_kv_heads * a.rep;
+  const int64_t row = __builtin_amdgcn_readfirstlane(int(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (row >= int64_t(bt.total) * heads) return;
+  const int t = int(row / heads), hq = int(row - int64_t(t) * heads);
+  int b = 0;
+  if (bt.starts) {
+    int e = bt.num_seqs;   // the last sequence that does not start behind t (those before it with the same start are empty)
+    while (e - b > 1) {
+      const int mid = (b + e) >> 1;
+      if (bt.starts[mid] <= t) b = mid;
+      else e = mid;
+    }
+  } else {
+    b = t / bt.uniform;
+  }
+  const Fp4Span s = fp4_span(bt, b);
+  if (t < s.first || t >= s.first + s.count) return;   // rows of a sequence with a bad range
+  const int h = hq / a.rep;
+  const float* ml;
+  const float* po;
+  int64_t first_slot, step;   // partial states of this row: the first one and, from the second one on, their distance; in rows
+  int64_t second_slot;
+  int parts;
+  if (s.count * a.rep <= a.decode_rows) {
+    const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
+    const int64_t units = int64_t(a.prefix[bt.num_seqs]) * bt.num_kv_heads;
+    const int64_t share = (units + a.workers - 1) / a.workers;
+    const int r = (t - s.first) * a.rep + hq - h * a.rep;
+    parts = 0;
+    first_slot = second_slot = step = 0;
+    if (per_head > 0) {
+      const int64_t u0 = int64_t(before) * bt.num_kv_heads + int64_t(h) * per_head, u1 = u0 + per_head - 1;
+      const int64_t w0 = u0 / share, w1 = u1 / share;
+      if (w0 == w1) return;   // its wave has finished it
+      parts = int(w1 - w0) + 1;
+      first_slot = (2 * w0 + (u0 == w0 * share ? 0 : 1)) * a.rows + r;
+      second_slot = 2 * (w0 + 1) * a.rows + r;
+      step = 2 * int64_t(a.rows);
+    }
+    ml = a.part_ml;
+    po = a.part_o;
+  } else {
+    if (a.splits == 1) return;
+    parts = a.splits;
+    step = int64_t(bt.total) * heads;
+    first_slot = row;
+    second_slot = row + step;
+    ml = a.tile_ml;
+    po = a.tile_o;
+  }
+  auto slot = [&](int k) -> int64_t { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
+  float top = kNoMax;
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, ml[slot(k) * 3]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float l = 0.f, lsum = 0.f, o[kPer] = {};
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) {
+    const int64_t at = slot(k);
+    const float w = __builtin_amdgcn_exp2f(ml[at * 3] - top);
+    l += w * ml[at * 3 + 1];
+    lsum += w * ml[at * 3 + 2];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) o[x] += w * po[at * HD + lane * kPer + x];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (kPer == 2) {
+    reinterpret_cast<uint32_t*>(a.out)[row * 64 + lane] = pack_out(o[0] * inv, o[1] * inv, a.bf16);
+  } else {
+    reinterpret_cast<uint16_t*>(a.out)[row * 64 + lane] = uint16_t(pack_out(o[0] * inv, 0.f, a.bf16));
+  }
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(lsum)) * kLn2;
+}
+
+}  // namespace cocktail
+
+using namespace cocktail;
+
+namespace {
+
+// What a call launches, from what the host knows: bounds, no lengths.
+struct Split {
+  bool decode, tiles;
+  int rows, row_tiles, workers, tile_blocks, splits;
+  size_t prefix_bytes, part_rows, tile_rows, bytes;
+};
+
+Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_new, int64_t max_len, bool uniform) {
+  Split s = {};
+  const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
+  if (max_len <= 0 || max_len > capacity) max_len = capacity;
+  const int64_t most_rows = max_new * rep;
+  // a batch may hold sequences for either kernel unless every sequence has the same number of queries
+  s.tiles = most_rows > kDecodeRows;
+  s.decode = !s.tiles || (!uniform && rep <= kDecodeRows);
+  s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
+  s.row_tiles = s.rows <= 16 ? 1 : 2;
+  if (s.decode) {
+    // Two waves per SIMD of 256 compute units; not less than two units for a wave, where the reads that a wave waits for one after the other
+    // weigh more than the units do.
+    const int64_t seqs = c->pages.num_seqs < total ? c->pages.num_seqs : total;
+    const int64_t units = seqs * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
+    int64_t workers = (units + 1) / 2;
+    workers = workers > 2048 ? 2048 : workers < 4 ? 4 : (workers + 3) / 4 * 4;
+    s.workers = int(workers);
+    s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
+    s.part_rows = 2 * size_t(workers) * s.rows;
+  }
+  s.splits = 1;
+  if (s.tiles) {
+    const int64_t seqs = c->pages.num_seqs;
+    s.tile_blocks = int(uniform ? seqs * ((most_rows + kTileRows - 1) / kTileRows) : total * rep / kTileRows + (seqs < total ? seqs : total));
+    const int64_t have = int64_t(s.tile_blocks) * c->num_kv_heads;
+    int64_t splits = (512 + have - 1) / have;
+    const int64_t longest = (max_len + 511) / 512;
+    splits = splits > longest ? longest : splits;
+    s.splits = int(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+    if (s.splits > 1) s.tile_rows = size_t(s.splits) * size_t(total) * c->num_kv_heads * rep;
+  }
+  s.bytes = s.prefix_bytes + (s.part_rows + s.tile_rows) * (c->head_dim + 4) * sizeof(float) + 64;
+  return s;
+}
+
+int check_attention(const cocktail_fp4_cache* c, int32_t num_q_heads, int64_t total, int32_t max_new) {
+  if (int rc = check_fp4_cache(c)) return rc;
+  if (num_q_heads < 1 || num_q_heads % c->num_kv_heads)
+    return fail(COCKTAIL_EINVAL, "num_q_heads %d is not a positive multiple of num_kv_heads %d", num_q_heads, c->num_kv_heads);
+  if (num_q_heads / c->num_kv_heads > COCKTAIL_MAX_Q_PER_KV)
+    return fail(COCKTAIL_EUNSUPPORTED, "num_q_heads / num_kv_heads = %d, at most %d", num_q_heads / c->num_kv_heads, COCKTAIL_MAX_Q_PER_KV);
+  if (total < 0 || total * num_q_heads > (int64_t(1) << 31) - 8) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
+  if (total && (max_new < 1 || max_new > total)) return fail(COCKTAIL_EINVAL, "max_new %d is not in 1 .. total (%lld)", max_new, (long long)total);
+  const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
+  if (c->pages.num_seqs * ((capacity + kUnit - 1) / kUnit) >= (int64_t(1) << 31))
+    return fail(COCKTAIL_EINVAL, "%d sequences of up to %lld tokens are too many for one call", c->pages.num_seqs, (long long)capacity);
+  return COCKTAIL_OK;
+}
+
+}  // namespace
+
+extern "C" int cocktail_fp4_attention_workspace(const cocktail_fp4_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,
+                                                int32_t max_len, int32_t uniform, size_t* bytes) {
+  if (!bytes) return fail(COCKTAIL_EINVAL, "bytes is NULL");
+  if (int rc = check_attention(cache, num_q_heads, total, max_new)) return rc;
+  *bytes = total ? split_of(cache, num_q_heads / cache->num_kv_heads, total, max_new, max_len, uniform != 0).bytes : 0;
+  return COCKTAIL_OK;
+}
+
+extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t num_q_heads, const void* q, int32_t dtype, int64_t stride_t,
+                                      int64_t stride_h, int64_t total, const int32_t* starts, int32_t max_new, int32_t max_len,
+                                      float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  Fp4Attention a = {};
+  if (int rc = check_attention(cache, num_q_heads, total, max_new)) return rc;
+  if (int rc = check_fp4_rows(cache, q, out, dtype, stride_t, stride_h, total, starts, num_q_heads, &a.batch)) return rc;
+  if (!total) return COCKTAIL_OK;
+  if (!starts && max_new != total / cache->pages.num_seqs)
+    return fail(COCKTAIL_EINVAL, "without starts max_new (%d) must be total / num_seqs (%lld)", max_new, (long long)(total / cache->pages.num_seqs));
+  if (std::isnan(sm_scale) || std::isinf(sm_scale)) return fail(COCKTAIL_EINVAL, "sm_scale must be finite");
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(COCKTAIL_EALIGN, "lse must be 4-byte aligned");
+  if (!workspace) return fail(COCKTAIL_EINVAL, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(COCKTAIL_EALIGN, "workspace must be 16-byte aligned");
+  const int hd = cache->head_dim;
+  a.rep = num_q_heads / cache->num_kv_heads;
+  const Split s = split_of(cache, a.rep, total, max_new, max_len, !starts);
+  if (workspace_bytes < s.bytes) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, s.bytes);
+  a.batch.max_new = max_new;
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.stride_t = 2 * stride_t;
+  a.stride_h = 2 * stride_h;
+  a.bf16 = dtype == COCKTAIL_BF16;
+  a.scale = (sm_scale > 0.f ? sm_scale : 1.f / std::sqrt(float(hd))) * kLog2e;
+  a.rows = s.rows;
+  a.workers = s.workers;
+  a.decode_rows = s.decode ? kDecodeRows : 0;
+  a.splits = s.splits;
+  char* w = static_cast<char*>(workspace);
+  a.prefix = reinterpret_cast<int32_t*>(w);
+  w += s.prefix_bytes;
+  a.part_o = reinterpret_cast<float*>(w);
+  w += s.part_rows * hd * sizeof(float);
+  a.tile_o = reinterpret_cast<float*>(w);
+  w += s.tile_rows * hd * sizeof(float);
+  a.part_ml = reinterpret_cast<float*>(w);
+  w += s.part_rows * 3 * sizeof(float);
+  a.tile_ml = reinterpret_cast<float*>(w);
+
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = hipSuccess;
+  if (s.decode) {
+    auto kernel = hd == 128 ? (s.row_tiles == 1 ? fp4_decode_kernel<128, 1> : fp4_decode_kernel<128, 2>)
+                            : (s.row_tiles == 1 ? fp4_decode_kernel<64, 1> : fp4_decode_kernel<64, 2>);
+    e = launch_lds(kernel, dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
+  }
+  if (e == hipSuccess && s.tiles)
+    e = launch(hd == 128 ? fp4_tile_kernel<128> : fp4_tile_kernel<64>, dim3(s.tile_blocks, cache->num_kv_heads, s.splits), dim3(64 * kTileWaves), st, a);
+  if (e == hipSuccess && (s.decode || s.splits > 1))
+    e = launch(hd == 128 ? fp4_merge_kernel<128> : fp4_merge_kernel<64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);
+  if (e != hipSuccess) return fail(COCKTAIL_EHIP, "attention launch failed: %s", hipGetErrorString(e));
+  return COCKTAIL_OK;
+}

@@ -1,0 +1,347 @@
+// Decode kernel of cocktail_fp4_attention: up to 32 query rows (new tokens x query heads of a kv head) per (sequence, kv head).
+//
+// Bound by memory: a key costs 2 * 17/32 D bytes and 4 D * rows operations.  What it takes to read at the rate of the memory:
+//  * Work is cut by tokens, not by sequences: the units of 32 tokens of all (sequence, kv head) segments are numbered, and every wave takes an
+//    equal share of consecutive ones, whatever the lengths are.  The numbering is made on the device from seq_lens, so that lengths can change
+//    under a captured graph.  A segment inside one share is finished by its wave, the others leave a partial state per wave.
+//  * A lane's operands are whole pieces of memory: of K, 16 tokens x D/4 channels (lane = token t, quarter j) are one operand of a 16x16x32
+//    product S^T = K Q^T, the channels being taken in an order of the product's own (the same for Q); of V, lane (c, j) has channels
+//    [8 c, 8 c + 8) of tokens 4 j .. 4 j + 3, which after a transposition of pairs are the operands of O^T = V^T P^T.
+//    The result layout of S^T (lane: a query row, tokens 4 j + x) is the operand layout of P^T with tokens numbered accordingly: weights
+//    never leave their lane.
+//  * Codes become fp16 with one instruction per pair that applies the scale as well.
+//  * The reference maximum is only raised when a logit exceeds it by 2^8 (exact, the result does not depend on it), so that the common step has
+//    no exchange between lanes at all.  Sums of the rounded weights come from a product with ones (the matrix cores are idle otherwise).
+#pragma once
+#include "fp4_attention.h"
+
+namespace cocktail {
+
+// 16 tokens of one (sequence, kv head) as a lane holds them.
+template <int HD>
+struct Fp4Tile {
+  u32x4 k;          // HD 64: the first half
+  uint32_t k_scale;
+  u32x4 v;
+  uint32_t v_scale;
+  int ok;           // wave-uniform: the page is one
+};
+
+// The pages of a segment in order, 64 of them in the lanes of a register and the next 64 on their way.
+struct Fp4Pages {
+  const int32_t* row;
+  int stride, first, ids, next;
+  __device__ __forceinline__ int fetch(int col, int lane) const { return col + lane < stride ? row[col + lane] : -1; }
+  __device__ __forceinline__ void start(const int32_t* r, int s, int col, int lane) {
+    row = r;
+    stride = s;
+    first = col;
+    ids = fetch(col, lane);
+    next = fetch(col + 64, lane);
+  }
+  __device__ __forceinline__ int get(int col, int lane) {
+    if (col >= first + 64) {
+      first += 64;
+      ids = next;
+      next = fetch(first + 64, lane);
+    }
+    return __builtin_amdgcn_readlane(ids, col - first);
+  }
+};
+
+// Units before every sequence into LDS (pre[0 .. num_seqs]); `scratch`: kDecodeWaves + 1 ints.  Workgroup of 64 * kDecodeWaves threads.
+__device__ __forceinline__ void decode_prefix(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int run = 0;
+  for (int base = 0; base < a.batch.num_seqs; base += 64 * kDecodeWaves) {
+    const int b = base + threadIdx.x;
+    const int v = b < a.batch.num_seqs ? decode_units(decode_seq(a, b)) : 0;
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[wave] = x;
+    __syncthreads();
+    int before = run;
+    for (int w = 0; w < kDecodeWaves; ++w) {
+      if (w < wave) before += scratch[w];
+      run += scratch[w];
+    }
+    if (b < a.batch.num_seqs) pre[b] = before + x - v;
+  }
+  if (threadIdx.x == 0) pre[a.batch.num_seqs] = run;
+  __syncthreads();
+}
+
+template <int HD, int RT>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Attention a) {
+  constexpr int kSteps = HD / 32;        // products per 16 tokens of S
+  constexpr int kChannelTiles = HD / 16;
+  extern __shared__ int32_t pre[];
+  __shared__ int32_t scratch[kDecodeWaves + 1];
+  const int lane = threadIdx.x & 63;
+  const int c16 = lane & 15, j = lane >> 4;
+  decode_prefix(a, pre, scratch);
+  const Fp4Batch& bt = a.batch;
+  const int64_t units = int64_t(pre[bt.num_seqs]) * bt.num_kv_heads;
+  const int64_t share = (units + a.workers - 1) / a.workers;
+  if (blockIdx.x == 0) {
+    for (int b = threadIdx.x; b <= bt.num_seqs; b += 64 * kDecodeWaves) a.prefix[b] = pre[b];
+  }
+  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+  int64_t u = w * share;
+  const int64_t end = u + share < units ? u + share : units;
+  if (u >= end) return;
+  const int P = bt.page_size;
+  const int64_t run = fp4_run_bytes(HD, P);
+  // byte offsets of a lane's pieces in 16 tokens
+  const uint32_t off_k = c16 * (HD / 2) + j * (HD / 8);
+  const uint32_t off_ks = uint32_t(P) * HD + c16 * (HD / 32) + (HD == 128 ? j : j >> 1);
+  const uint32_t off_v = uint32_t(P) * (HD / 2) + j * (2 * HD) + (HD == 128 ? c16 : c16 >> 1) * 16;
+  const uint32_t off_vs = uint32_t(P) * HD + uint32_t(P) * (HD / 32) + j * (HD / 8) + (HD == 128 ? c16 >> 2 : c16 >> 3) * 4;
+
+  bool first_segment = true;
+  int b = 0, e = bt.num_seqs;   // the sequence of unit u: the last one with no more units before it
+  while (e - b > 1) {
+    const int m = (b + e) >> 1;
+    if (int64_t(pre[m]) * bt.num_kv_heads <= u) b = m;
+    else e = m;
+  }
+  while (u < end) {
+    while (int64_t(__builtin_amdgcn_readfirstlane(pre[b + 1])) * bt.num_kv_heads <= u) ++b;
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int before = __builtin_amdgcn_readfirstlane(pre[b]);
+    const int per_head = __builtin_amdgcn_readfirstlane(pre[b + 1]) - before;
+    const int64_t local = u - int64_t(before) * bt.num_kv_heads;
+    const int h = int(local / per_head), u0 = int(local - int64_t(h) * per_head);
+    const int u1 = int(end - u < per_head - u0 ? u0 + (end - u) : per_head);
+    const Fp4Seq seq = decode_seq(a, b);
+    const int n = seq.n, len = seq.len, rows = n * a.rep;
+
+    // the queries: lane (row c16, quarter j) has the channels that its K pieces have
+    h8 q[RT][kSteps];
+    float c[RT], m[RT], lsum[RT];
+    f32x4 l[RT], o[RT][kChannelTiles];
+    int lim[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = rt * 16 + c16, i = r / a.rep;
+      const bool live = r < rows;
+      u32x4 raw[kSteps] = {};
+      if (live) {
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.q + (seq.first + i) * a.stride_t + (h * a.rep + r - i * a.rep) * a.stride_h + j * (HD / 2));
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) raw[s] = src[s];
+      }
+      c[rt] = a.scale;
+      if (a.bf16) {
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(fabsf(bf_lo(raw[s][x])), fabsf(bf_hi(raw[s][x]))));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float f = row_factor(top), inv = 1.f / f;
+        c[rt] *= f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) raw[s][x] = pack_halves(bf_lo(raw[s][x]) * inv, bf_hi(raw[s][x]) * inv);
+      }
+      c[rt] = fmaxf(c[rt], 1.2e-38f);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) q[rt][s] = __builtin_bit_cast(h8, raw[s]);
+      lim[rt] = live ? len - n + i + 1 : 0;
+      m[rt] = kNoMax;
+      lsum[rt] = 0.f;
+      l[rt] = f32x4{};
+#pragma unroll
+      for (int ct = 0; ct < kChannelTiles; ++ct) o[rt][ct] = f32x4{};
+    }
+
+    Fp4Pages pages;
+    int col = u0 * kUnit / P, at = u0 * kUnit - col * P;   // of the next tile to load
+    pages.start(bt.table + int64_t(b) * bt.table_stride, bt.table_stride, col, lane);
+    int left = len - u0 * kUnit;                            // tokens from the next tile to load on
+    auto load_tile = [&](Fp4Tile<HD>& t) {
+      const int id = left > 0 ? pages.get(col, lane) : -1;
+      t.ok = uint32_t(id) < uint32_t(bt.num_pages);
+      const char* base = bt.pool + (int64_t(t.ok ? id : 0) * bt.num_kv_heads + h) * run;
+      if constexpr (HD == 128) {
+        t.k = *reinterpret_cast<const u32x4*>(base + at * (HD / 2) + off_k);
+      } else {
+        const u32x2 half = *reinterpret_cast<const u32x2*>(base + at * (HD / 2) + off_k);
+        t.k = u32x4{half[0], half[1], 0, 0};
+      }
+      t.k_scale = *reinterpret_cast<const uint8_t*>(base + at * (HD / 32) + off_ks);
+      t.v = *reinterpret_cast<const u32x4*>(base + at * (HD / 2) + off_v);
+      t.v_scale = *reinterpret_cast<const uint32_t*>(base + at * (HD / 32) + off_vs);
+      at += 16;
+      left -= 16;
+      if (at == P) at = 0, ++col;
+    };
+    const int free_below = len - n + 1;   // tokens that every query sees
+
+    auto compute = [&](Fp4Tile<HD>& ta, Fp4Tile<HD>& tb, int tok0) {
+      // logits
+      f32x4 s[RT][2];
+      {
+        const float sa = __builtin_bit_cast(float, ta.k_scale << 23), sb = __builtin_bit_cast(float, tb.k_scale << 23);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{};
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          const u32x4 wa = {fp4_pair<0>(ta.k[st], sa), fp4_pair<1>(ta.k[st], sa), fp4_pair<2>(ta.k[st], sa), fp4_pair<3>(ta.k[st], sa)};
+          const u32x4 wb = {fp4_pair<0>(tb.k[st], sb), fp4_pair<1>(tb.k[st], sb), fp4_pair<2>(tb.k[st], sb), fp4_pair<3>(tb.k[st], sb)};
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            s[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wa), q[rt][st], s[rt][0], 0, 0, 0);
+            s[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wb), q[rt][st], s[rt][1], 0, 0, 0);
+          }
+        }
+      }
+      // keys that a query does not see, and what lies in places that no token has been stored to
+      if (tok0 + kUnit > free_below || !ta.ok || !tb.ok) {
+        const int ka = tok0 + 4 * j, kb = ka + 16;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            s[rt][0][x] = ta.ok && ka + x < lim[rt] ? s[rt][0][x] : -__builtin_inff();
+            s[rt][1][x] = tb.ok && kb + x < lim[rt] ? s[rt][1][x] : -__builtin_inff();
+          }
+          if (!(ta.ok && ka + x < len)) ta.v[x] = 0, ta.v_scale = (ta.v_scale & ~(255u << (8 * x))) | 127u << (8 * x);
+          if (!(tb.ok && kb + x < len)) tb.v[x] = 0, tb.v_scale = (tb.v_scale & ~(255u << (8 * x))) | 127u << (8 * x);
+        }
+      }
+      // weights
+      h8 p[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
+                          fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3]))) * c[rt];
+        if (__any(top > m[rt] + kMaxSlack)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float raised = fmaxf(m[rt], top), alpha = __builtin_amdgcn_exp2f(m[rt] - raised);
+          m[rt] = raised;
+          lsum[rt] *= alpha;
+          l[rt] *= alpha;
+#pragma unroll
+          for (int ct = 0; ct < kChannelTiles; ++ct) o[rt][ct] *= alpha;
+        }
+        float w8[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) w8[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][x >> 2][x & 3], c[rt], -m[rt]));
+        lsum[rt] += ((w8[0] + w8[1]) + (w8[2] + w8[3])) + ((w8[4] + w8[5]) + (w8[6] + w8[7]));
+        p[rt] = __builtin_bit_cast(h8, u32x4{pack_halves(w8[0], w8[1]), pack_halves(w8[2], w8[3]), pack_halves(w8[4], w8[5]), pack_halves(w8[6], w8[7])});
+        const _Float16 one = _Float16(1.f);
+        l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h8{one, one, one, one, one, one, one, one}, p[rt], l[rt], 0, 0, 0);
+      }
+      // weighted sums
+      const float va0 = fp4_scale(ta.v_scale, 0), va1 = fp4_scale(ta.v_scale, 1), va2 = fp4_scale(ta.v_scale, 2), va3 = fp4_scale(ta.v_scale, 3);
+      const float vb0 = fp4_scale(tb.v_scale, 0), vb1 = fp4_scale(tb.v_scale, 1), vb2 = fp4_scale(tb.v_scale, 2), vb3 = fp4_scale(tb.v_scale, 3);
+      auto pair_of_channels = [&](auto byte_tag, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, int ct) {
+        constexpr int B = decltype(byte_tag)::value;
+        const uint32_t x0 = fp4_pair<B>(a0, va0), x1 = fp4_pair<B>(a1, va1), x2 = fp4_pair<B>(a2, va2), x3 = fp4_pair<B>(a3, va3);
+        const uint32_t y0 = fp4_pair<B>(b0, vb0), y1 = fp4_pair<B>(b1, vb1), y2 = fp4_pair<B>(b2, vb2), y3 = fp4_pair<B>(b3, vb3);
+        const u32x4 even = {__builtin_amdgcn_perm(x1, x0, 0x05040100), __builtin_amdgcn_perm(x3, x2, 0x05040100), __builtin_amdgcn_perm(y1, y0, 0x05040100),
+                            __builtin_amdgcn_perm(y3, y2, 0x05040100)};
+        const u32x4 odd = {__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302), __builtin_amdgcn_perm(y1, y0, 0x07060302),
+                           __builtin_amdgcn_perm(y3, y2, 0x07060302)};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, even), p[rt], o[rt][ct], 0, 0, 0);
+          o[rt][ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, odd), p[rt], o[rt][ct + 1], 0, 0, 0);
+        }
+      };
+      uint32_t a0 = ta.v[0], a1 = ta.v[1], a2 = ta.v[2], a3 = ta.v[3], b0 = tb.v[0], b1 = tb.v[1], b2 = tb.v[2], b3 = tb.v[3];
+      if constexpr (HD == 64) {
+        // a lane has half a piece: channels 4 c .. 4 c + 3
+        const int sh = (c16 & 1) * 16;
+        a0 >>= sh, a1 >>= sh, a2 >>= sh, a3 >>= sh, b0 >>= sh, b1 >>= sh, b2 >>= sh, b3 >>= sh;
+      }
+      pair_of_channels(std::integral_constant<int, 0>{}, a0, a1, a2, a3, b0, b1, b2, b3, 0);
+      pair_of_channels(std::integral_constant<int, 1>{}, a0, a1, a2, a3, b0, b1, b2, b3, 2);
+      if constexpr (HD == 128) {
+        pair_of_channels(std::integral_constant<int, 2>{}, a0, a1, a2, a3, b0, b1, b2, b3, 4);
+        pair_of_channels(std::integral_constant<int, 3>{}, a0, a1, a2, a3, b0, b1, b2, b3, 6);
+      }
+    };
+
+    // the next unit is on its way while one is worked on
+    Fp4Tile<HD> x0, x1, y0, y1;
+    load_tile(x0);
+    load_tile(x1);
+    for (int k = u0; k < u1; k += 2) {
+      if (k + 1 < u1) {
+        load_tile(y0);
+        load_tile(y1);
+      }
+      compute(x0, x1, k * kUnit);
+      if (k + 1 >= u1) break;
+      if (k + 2 < u1) {
+        load_tile(x0);
+        load_tile(x1);
+      }
+      compute(y0, y1, (k + 1) * kUnit);
+    }
+
+    // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
+    // each end, so two places per wave are enough
+    const bool whole = u0 == 0 && u1 == per_head;
+    const int64_t slot = 2 * int64_t(w) + (first_segment ? 0 : 1);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float sum = lsum[rt];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      const int r = rt * 16 + c16;
+      if (r >= rows) continue;
+      const float lr = l[rt][0];
+      if (whole) {
+        const int i = r / a.rep;
+        const int64_t row = int64_t(seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
+        const float inv = lr == 0.f ? 0.f : 1.f / lr;
+        char* dst = a.out + row * (2 * HD) + j * (HD / 2);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if constexpr (HD == 128) {
+            u32x4 v;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) v[y] = pack_out(o[rt][2 * y][x] * inv, o[rt][2 * y + 1][x] * inv, a.bf16);
+            *reinterpret_cast<u32x4*>(dst + 16 * x) = v;
+          } else {
+            u32x2 v;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) v[y] = pack_out(o[rt][2 * y][x] * inv, o[rt][2 * y + 1][x] * inv, a.bf16);
+            *reinterpret_cast<u32x2*>(dst + 8 * x) = v;
+          }
+        }
+        if (a.lse && j == 0) a.lse[row] = lr == 0.f ? -__builtin_inff() : (m[rt] + __builtin_amdgcn_logf(sum)) * kLn2;
+      } else {
+        const int64_t at_row = slot * a.rows + r;
+        float* dst = a.part_o + at_row * HD + j * (HD / 4);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < kChannelTiles / 4; ++y)
+            *reinterpret_cast<f32x4*>(dst + x * kChannelTiles + 4 * y) = f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
+        if (j == 0) {
+          float* ml = a.part_ml + at_row * 3;
+          ml[0] = m[rt];
+          ml[1] = lr;
+          ml[2] = sum;
+        }
+      }
+    }
+    first_segment = false;
+    u += u1 - u0;
+  }
+}
+
+}  // namespace cocktail
