@@ -9,16 +9,105 @@
 
 namespace cocktail {
 
-// One wave per (new token, query head): joins the partial states of its row, if it has more than one, and writes rows without keys.
+// Sum of a row's partial states: `parts` of them, the first at row `first_slot` of the arrays and the others at second_slot, second_slot + step ...
+// Wave `wave` of `waves` takes every waves-th; o: the lane's channels, l and lsum: whole sums (in every wave).
 template <int HD>
-__global__ __launch_bounds__(256) void fp4_merge_kernel(Fp4Attention a) {
+struct Merged {
+  float top, l, lsum, o[HD / 64];
+};
+template <int HD>
+__device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* po, int64_t first_slot, int64_t second_slot, int64_t step, int parts,
+                                                  int wave, int waves, int lane) {
   constexpr int kPer = HD / 64;
+  auto slot = [&](int k) -> int64_t { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
+  Merged<HD> r = {};
+  r.top = kNoMax;
+  for (int k = lane; k < parts; k += 64) r.top = fmaxf(r.top, ml[slot(k) * 3]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) r.top = fmaxf(r.top, __shfl_xor(r.top, d));
+  for (int base = 0; base < parts; base += 64) {
+    float w = 0.f;
+    if (base + lane < parts) {
+      const float* x = ml + slot(base + lane) * 3;
+      w = __builtin_amdgcn_exp2f(x[0] - r.top);
+      r.l += w * x[1];
+      r.lsum += w * x[2];
+    }
+    const int n = parts - base < 64 ? parts - base : 64;
+#pragma unroll 8
+    for (int k = wave; k < n; k += waves) {
+      const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k));
+      const float* src = po + slot(base + k) * HD + lane * kPer;
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) r.o[x] += wk * src[x];
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    r.l += __shfl_xor(r.l, d);
+    r.lsum += __shfl_xor(r.lsum, d);
+  }
+  return r;
+}
+
+template <int HD>
+__device__ __forceinline__ void write_merged(const Fp4Attention& a, const Merged<HD>& r, int64_t row, int lane) {
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  if constexpr (HD == 128) {
+    reinterpret_cast<uint32_t*>(a.out)[row * 64 + lane] = pack_out(r.o[0] * inv, r.o[1] * inv, a.bf16);
+  } else {
+    reinterpret_cast<uint16_t*>(a.out)[row * 64 + lane] = uint16_t(pack_out(r.o[0] * inv, 0.f, a.bf16));
+  }
+  if (a.lse && lane == 0) a.lse[row] = r.l == 0.f ? -__builtin_inff() : (r.top + __builtin_amdgcn_logf(r.lsum)) * kLn2;
+}
+
+// Rows of the decode kernel: a workgroup per (sequence, new token, query head) joins what the waves of its segment left, if there were
+// several, and writes rows without keys.
+template <int HD>
+__global__ __launch_bounds__(256) void fp4_merge_decode_kernel(Fp4Attention a, int most_new) {
+  constexpr int kPer = HD / 64;
+  __shared__ float o[3][HD];
+  const Fp4Batch& bt = a.batch;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int heads = bt.num_kv_heads * a.rep;
+  const int hq = blockIdx.x % heads, bi = blockIdx.x / heads;
+  const int b = bi / most_new, i = bi % most_new;
+  const Fp4Seq s = decode_seq(a, b);
+  if (i >= s.n) return;
+  const int h = hq / a.rep;
+  const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
+  const int64_t units = int64_t(a.prefix[bt.num_seqs]) * bt.num_kv_heads;
+  const int64_t row = int64_t(s.first + i) * heads + hq;
+  Merged<HD> r = {};
+  if (per_head > 0) {
+    const int64_t share = (units + a.workers - 1) / a.workers;
+    const int64_t u0 = int64_t(before) * bt.num_kv_heads + int64_t(h) * per_head, u1 = u0 + per_head - 1;
+    const int64_t w0 = u0 / share, w1 = u1 / share;
+    if (w0 == w1) return;   // its wave has finished it
+    const int in_state = i * a.rep + hq - h * a.rep;
+    r = merge_parts<HD>(a.part_ml, a.part_o, (2 * w0 + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state, 2 * (w0 + 1) * a.rows + in_state,
+                        2 * int64_t(a.rows), int(w1 - w0) + 1, wave, 4, lane);
+  }
+  if (wave) {
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) o[wave - 1][lane * kPer + x] = r.o[x];
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) r.o[x] += (o[0][lane * kPer + x] + o[1][lane * kPer + x]) + o[2][lane * kPer + x];
+  write_merged<HD>(a, r, row, lane);
+}
+
+// Rows of the tile kernel whose keys were cut: a wave per (new token, query head).
+template <int HD>
+__global__ __launch_bounds__(256) void fp4_merge_tiles_kernel(Fp4Attention a) {
   const Fp4Batch& bt = a.batch;
   const int lane = threadIdx.x & 63;
   const int heads = bt.num_kv_heads * a.rep;
-  const int64_t row = __builtin_amdgcn_readfirstlane(int(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (row >= int64_t(bt.total) * heads) return;
-  const int t = int(row / heads), hq = int(row - int64_t(t) * heads);
+  const int row = __builtin_amdgcn_readfirstlane(int(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (row >= bt.total * heads) return;
+  const int t = row / heads;
   int b = 0;
   if (bt.starts) {
     int e = bt.num_seqs;   // the last sequence that does not start behind t (those before it with the same start are empty)
@@ -31,62 +120,10 @@ __global__ __launch_bounds__(256) void fp4_merge_kernel(Fp4Attention a) {
     b = t / bt.uniform;
   }
   const Fp4Span s = fp4_span(bt, b);
-  if (t < s.first || t >= s.first + s.count) return;   // rows of a sequence with a bad range
-  const int h = hq / a.rep;
-  const float* ml;
-  const float* po;
-  int64_t first_slot, step;   // partial states of this row: the first one and, from the second one on, their distance; in rows
-  int64_t second_slot;
-  int parts;
-  if (s.count * a.rep <= a.decode_rows) {
-    const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
-    const int64_t units = int64_t(a.prefix[bt.num_seqs]) * bt.num_kv_heads;
-    const int64_t share = (units + a.workers - 1) / a.workers;
-    const int r = (t - s.first) * a.rep + hq - h * a.rep;
-    parts = 0;
-    first_slot = second_slot = step = 0;
-    if (per_head > 0) {
-      const int64_t u0 = int64_t(before) * bt.num_kv_heads + int64_t(h) * per_head, u1 = u0 + per_head - 1;
-      const int64_t w0 = u0 / share, w1 = u1 / share;
-      if (w0 == w1) return;   // its wave has finished it
-      parts = int(w1 - w0) + 1;
-      first_slot = (2 * w0 + (u0 == w0 * share ? 0 : 1)) * a.rows + r;
-      second_slot = 2 * (w0 + 1) * a.rows + r;
-      step = 2 * int64_t(a.rows);
-    }
-    ml = a.part_ml;
-    po = a.part_o;
-  } else {
-    if (a.splits == 1) return;
-    parts = a.splits;
-    step = int64_t(bt.total) * heads;
-    first_slot = row;
-    second_slot = row + step;
-    ml = a.tile_ml;
-    po = a.tile_o;
-  }
-  auto slot = [&](int k) -> int64_t { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
-  float top = kNoMax;
-  for (int k = lane; k < parts; k += 64) top = fmaxf(top, ml[slot(k) * 3]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float l = 0.f, lsum = 0.f, o[kPer] = {};
-#pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const int64_t at = slot(k);
-    const float w = __builtin_amdgcn_exp2f(ml[at * 3] - top);
-    l += w * ml[at * 3 + 1];
-    lsum += w * ml[at * 3 + 2];
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) o[x] += w * po[at * HD + lane * kPer + x];
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if constexpr (kPer == 2) {
-    reinterpret_cast<uint32_t*>(a.out)[row * 64 + lane] = pack_out(o[0] * inv, o[1] * inv, a.bf16);
-  } else {
-    reinterpret_cast<uint16_t*>(a.out)[row * 64 + lane] = uint16_t(pack_out(o[0] * inv, 0.f, a.bf16));
-  }
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(lsum)) * kLn2;
+  // not the rows of a sequence with a bad range, or of the decode kernel
+  if (t < s.first || t >= s.first + s.count || s.count * a.rep <= a.decode_rows) return;
+  const int64_t step = int64_t(bt.total) * heads;
+  write_merged<HD>(a, merge_parts<HD>(a.tile_ml, a.tile_o, row, row + step, step, a.splits, 0, 1, lane), row, lane);
 }
 
 }  // namespace cocktail
@@ -144,7 +181,7 @@ int check_attention(const cocktail_fp4_cache* c, int32_t num_q_heads, int64_t to
     return fail(COCKTAIL_EINVAL, "num_q_heads %d is not a positive multiple of num_kv_heads %d", num_q_heads, c->num_kv_heads);
   if (num_q_heads / c->num_kv_heads > COCKTAIL_MAX_Q_PER_KV)
     return fail(COCKTAIL_EUNSUPPORTED, "num_q_heads / num_kv_heads = %d, at most %d", num_q_heads / c->num_kv_heads, COCKTAIL_MAX_Q_PER_KV);
-  if (total < 0 || total * num_q_heads > (int64_t(1) << 31) - 8) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
+  if (total < 0 || total * num_q_heads > (int64_t(1) << 30)) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
   if (total && (max_new < 1 || max_new > total)) return fail(COCKTAIL_EINVAL, "max_new %d is not in 1 .. total (%lld)", max_new, (long long)total);
   const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
   if (c->pages.num_seqs * ((capacity + kUnit - 1) / kUnit) >= (int64_t(1) << 31))
@@ -210,9 +247,13 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     e = launch_lds(kernel, dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }
   if (e == hipSuccess && s.tiles)
-    e = launch(hd == 128 ? fp4_tile_kernel<128> : fp4_tile_kernel<64>, dim3(s.tile_blocks, cache->num_kv_heads, s.splits), dim3(64 * kTileWaves), st, a);
-  if (e == hipSuccess && (s.decode || s.splits > 1))
-    e = launch(hd == 128 ? fp4_merge_kernel<128> : fp4_merge_kernel<64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);
+    e = launch(hd == 128 ? fp4_tile_kernel<128> : fp4_tile_kernel<64>, dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * kTileWaves), st, a);
+  if (e == hipSuccess && s.decode) {
+    const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
+    e = launch(hd == 128 ? fp4_merge_decode_kernel<128> : fp4_merge_decode_kernel<64>, dim3(uint32_t(cache->pages.num_seqs) * most_new * num_q_heads), dim3(256), st, a, most_new);
+  }
+  if (e == hipSuccess && s.splits > 1)
+    e = launch(hd == 128 ? fp4_merge_tiles_kernel<128> : fp4_merge_tiles_kernel<64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return COCKTAIL_OK;
 }

@@ -6,13 +6,15 @@
 
 namespace cocktail {
 
-// A thread's share is one group of 32 channels of a quad of tokens (four consecutive ones from a multiple of four: a V piece holds
-// them side by side, and no two threads write the same byte).  `items` of them per quad: (K or V, head, group), group fastest, so
-// that neighbouring threads read neighbouring memory.  Quads are numbered over the batch with room for one that starts and one
-// that ends inside a sequence's range: those of sequence b are first[b] / 4 + 2 b and following.
+// A thread's share is eight channels of a quad of tokens (four consecutive ones from a multiple of four: a V piece holds them side by
+// side, and no two threads write the same byte): sixteen bytes of each of four rows, so that neighbouring threads read and write
+// neighbouring memory on both sides.  The four threads of a group of 32 channels find its scale together.  (A whole group per
+// thread, 64 bytes of a row, was 4 times slower on the way back, whose stores then leave lines half written, and a third slower on
+// the way in.)  `units` per quad: (K or V, head, eight channels), channels fastest.  Quads are numbered over the batch with room for
+// one that starts and one that ends inside a sequence's range: those of sequence b are first[b] / 4 + 2 b and following.
 struct Fp4Item {
   int seq, pos, row, lo, hi;   // sequence, position of the quad's first token, row of that token; tokens lo .. hi-1 of the quad are in the range
-  int head, group, is_v;
+  int head, part, is_v;        // part: channels 8 part .. 8 part + 7
   bool active;
 };
 
@@ -21,14 +23,17 @@ __device__ __forceinline__ int quad_number(int first, int b) { return (first >> 
 // starts[0 .. num_seqs] in LDS; the thread's item from its number in the grid.
 template <int HD>
 __device__ __forceinline__ Fp4Item find_item(const Fp4Batch& a, const int32_t* lds_starts) {
-  constexpr int kGroups = HD / kFp4Group;
+  constexpr int kParts = HD / 8;
   Fp4Item it;
-  const uint32_t per_quad = 2u * kGroups * a.num_kv_heads;
-  const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
-  const int quad = int(i / per_quad);
-  uint32_t unit = uint32_t(i - uint64_t(quad) * per_quad);
-  it.group = unit % kGroups;
-  unit /= kGroups;
+  const uint32_t per_quad = 2u * kParts * a.num_kv_heads;
+  const uint64_t begin = uint64_t(blockIdx.x) * 256;
+  const uint64_t quad0 = begin / per_quad;                      // (of the workgroup: scalar)
+  uint32_t unit = uint32_t(begin - quad0 * per_quad) + threadIdx.x;
+  const uint32_t ahead = unit / per_quad;
+  const int quad = int(quad0 + ahead);
+  unit -= ahead * per_quad;
+  it.part = unit % kParts;
+  unit /= kParts;
   it.is_v = unit >= uint32_t(a.num_kv_heads);
   it.head = it.is_v ? unit - a.num_kv_heads : unit;
   // the last sequence whose first quad is not behind this one
@@ -86,29 +91,52 @@ __device__ __forceinline__ uint32_t encode_pair(uint32_t old, uint32_t x, float 
   }
 }
 
-// 32 channels in 16 bits -> 16 bytes of codes and the scale byte.  The conversion instruction divides by the power of two and
-// rounds to nearest even, which is the definition; it would make a NaN the largest code, so those are cleared before (their bits, taken as
-// an integer without the sign, are the only ones above infinity's).
+// The value of the lane of the same four that differs in the bits of X (1, 2).
+template <int X>
+__device__ __forceinline__ uint32_t of_quad_lane(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), X == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
+}
+
+// Four words of each of four lanes: word i of lane j becomes word j of lane i.
+__device__ __forceinline__ u32x4 transpose_quad(u32x4 v, int j) {
+  // swap the off-diagonal blocks of two, then of one
+  const bool hi = j & 2, odd = j & 1;
+  const uint32_t a = of_quad_lane<2>(hi ? v[0] : v[2]), b = of_quad_lane<2>(hi ? v[1] : v[3]);
+  if (hi) v[0] = a, v[1] = b;
+  else v[2] = a, v[3] = b;
+  const uint32_t c = of_quad_lane<1>(odd ? v[0] : v[1]), d = of_quad_lane<1>(odd ? v[2] : v[3]);
+  if (odd) v[0] = c, v[2] = d;
+  else v[1] = c, v[3] = d;
+  return v;
+}
+
+// Eight channels in 16 bits, a quarter of a group whose other quarters the lanes of the same four have -> their codes, and the scale byte.
+// The conversion instruction divides by the power of two and rounds to nearest even, which is the definition; it would make a NaN
+// the largest code, so those are cleared before (their bits, taken as an integer without the sign, are the only ones above infinity's).
 template <bool BF16>
-__device__ __forceinline__ u32x4 encode_group(u32x4 (&x)[4], uint32_t* scale_byte) {
+__device__ __forceinline__ uint32_t encode_part(u32x4 x, uint32_t* scale_byte) {
   constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) m = pk_max_u16(m, x[i / 4][i % 4] & 0x7fff7fffu);
+  for (int i = 0; i < 4; ++i) m = pk_max_u16(m, x[i] & 0x7fff7fffu);
   uint32_t top = (m & 0xffffu) > (m >> 16) ? m & 0xffffu : m >> 16;
   if (top > kInf) {
     top = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      uint32_t w = x[i / 4][i % 4];
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w = x[i];
       if ((w & 0x7fffu) > kInf) w &= 0xffff0000u;
       if (((w >> 16) & 0x7fffu) > kInf) w &= 0xffffu;
-      x[i / 4][i % 4] = w;
+      x[i] = w;
       const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
       top = lo > top ? lo : top;
       top = hi > top ? hi : top;
     }
   }
+  uint32_t other = of_quad_lane<1>(top);
+  top = other > top ? other : top;
+  other = of_quad_lane<2>(top);
+  top = other > top ? other : top;
   float f;
   if constexpr (BF16) f = __builtin_bit_cast(float, top << 16);
   else f = float(__builtin_bit_cast(_Float16, uint16_t(top)));
@@ -116,17 +144,11 @@ __device__ __forceinline__ u32x4 encode_group(u32x4 (&x)[4], uint32_t* scale_byt
   e = e < kFp4LeastExp + 127 ? kFp4LeastExp + 127 : e > kFp4MostExp + 127 ? kFp4MostExp + 127 : e;
   *scale_byte = uint32_t(e);
   const float scale = __builtin_bit_cast(float, uint32_t(e) << 23);
-  u32x4 codes;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w = 0;
-    w = encode_pair<BF16, 0>(w, x[i][0], scale);
-    w = encode_pair<BF16, 1>(w, x[i][1], scale);
-    w = encode_pair<BF16, 2>(w, x[i][2], scale);
-    w = encode_pair<BF16, 3>(w, x[i][3], scale);
-    codes[i] = w;
-  }
-  return codes;
+  uint32_t w = 0;
+  w = encode_pair<BF16, 0>(w, x[0], scale);
+  w = encode_pair<BF16, 1>(w, x[1], scale);
+  w = encode_pair<BF16, 2>(w, x[2], scale);
+  return encode_pair<BF16, 3>(w, x[3], scale);
 }
 
 struct Fp4Rows {
@@ -146,53 +168,43 @@ __global__ __launch_bounds__(256) void fp4_store_kernel(Fp4Batch a, Fp4Rows r) {
   const int64_t run = fp4_run_bytes(HD, a.page_size);
   char* base = page_run(a, it, run);
   if (!base) return;
-  const char* src = (it.is_v ? r.v : r.k) + it.head * r.stride_h + it.group * 64;
-  u32x4 x[4][4];
+  const char* src = (it.is_v ? r.v : r.k) + it.head * r.stride_h + it.part * 16;
+  u32x4 x[4] = {};
 #pragma unroll
   for (int t = 0; t < 4; ++t)
-    if (t >= it.lo && t < it.hi) {
-      const u32x4* p = reinterpret_cast<const u32x4*>(src + (it.row + t) * r.stride_t);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[t][i] = __builtin_nontemporal_load(p + i);
-    }
+    if (t >= it.lo && t < it.hi) x[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (it.row + t) * r.stride_t));
   const int at = it.pos % a.page_size, p = a.page_size;
-  u32x4 codes[4];
+  u32x4 codes;
   uint32_t scale[4];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (t >= it.lo && t < it.hi) codes[t] = encode_group<BF16>(x[t], &scale[t]);
+  for (int t = 0; t < 4; ++t) codes[t] = encode_part<BF16>(x[t], &scale[t]);
+  const int j = it.part & 3, group = it.part >> 2;
   if (!it.is_v) {
-    char* dst = base + at * (HD / 2) + it.group * 16;
-    char* sc = base + p * HD + at * (HD / 32) + it.group;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (t >= it.lo && t < it.hi) {
-        *reinterpret_cast<u32x4*>(dst + t * (HD / 2)) = codes[t];
-        sc[t * (HD / 32)] = char(scale[t]);
-      }
+    // lane j of the four writes token j: sixteen bytes of its row
+    const u32x4 row = transpose_quad(codes, j);
+    if (j >= it.lo && j < it.hi) {
+      *reinterpret_cast<u32x4*>(base + (at + j) * (HD / 2) + group * 16) = row;
+      base[p * HD + (at + j) * (HD / 32) + group] = char(j == 0 ? scale[0] : j == 1 ? scale[1] : j == 2 ? scale[2] : scale[3]);
+    }
     return;
   }
-  char* dst = base + p * (HD / 2) + (at / 4) * (2 * HD) + it.group * 64;   // the group's four pieces
-  char* sc = base + p * HD + p * (HD / 32) + (at / 4) * (HD / 8) + it.group * 4;
+  char* dst = base + p * (HD / 2) + (at / 4) * (2 * HD) + it.part * 16;
+  char* sc = base + p * HD + p * (HD / 32) + (at / 4) * (HD / 8) + group * 4;
   if (it.lo == 0 && it.hi == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<u32x4*>(dst + i * 16) = u32x4{codes[0][i], codes[1][i], codes[2][i], codes[3][i]};
-    *reinterpret_cast<uint32_t*>(sc) = scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24;
+    *reinterpret_cast<u32x4*>(dst) = codes;
+    if (j == 0) *reinterpret_cast<uint32_t*>(sc) = scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24;
     return;
   }
 #pragma unroll
   for (int t = 0; t < 4; ++t)
     if (t >= it.lo && t < it.hi) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(dst + i * 16 + t * 4) = codes[t][i];
-      sc[t] = char(scale[t]);
+      *reinterpret_cast<uint32_t*>(dst + t * 4) = codes[t];
+      if (j == 0) sc[t] = char(scale[t]);
     }
 }
 
 template <bool BF16>
 __device__ __forceinline__ uint32_t decode_word(uint32_t codes, float scale, int byte) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   switch (byte) {
     case 0: return BF16 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)) : fp4_pair<0>(codes, scale);
     case 1: return BF16 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)) : fp4_pair<1>(codes, scale);
@@ -209,44 +221,28 @@ __global__ __launch_bounds__(256) void fp4_gather_kernel(Fp4Batch a, Fp4Rows r) 
   if (!it.active) return;
   const int64_t run = fp4_run_bytes(HD, a.page_size);
   const char* base = page_run(a, it, run);
-  u32x4 codes[4] = {};                 // by token
-  uint32_t scale[4] = {127, 127, 127, 127};
+  const int j = it.part & 3, group = it.part >> 2;
+  u32x4 codes = {};                 // of the thread's channels, by token
+  uint32_t scales = 0x7f7f7f7fu;
   if (base) {
     const int at = it.pos % a.page_size, p = a.page_size;
     if (!it.is_v) {
-      const char* src = base + at * (HD / 2) + it.group * 16;
-      const char* sc = base + p * HD + at * (HD / 32) + it.group;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        codes[t] = *reinterpret_cast<const u32x4*>(src + t * (HD / 2));
-        scale[t] = uint8_t(sc[t * (HD / 32)]);
-      }
+      const u32x4 row = *reinterpret_cast<const u32x4*>(base + (at + j) * (HD / 2) + group * 16);   // of token j
+      codes = transpose_quad(row, j);
+      const uint8_t* sc = reinterpret_cast<const uint8_t*>(base + p * HD + at * (HD / 32) + group);
+      scales = sc[0] | sc[HD / 32] << 8 | sc[2 * (HD / 32)] << 16 | uint32_t(sc[3 * (HD / 32)]) << 24;
     } else {
-      const char* src = base + p * (HD / 2) + (at / 4) * (2 * HD) + it.group * 64;
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(base + p * HD + p * (HD / 32) + (at / 4) * (HD / 8) + it.group * 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x4 piece = *reinterpret_cast<const u32x4*>(src + i * 16);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) codes[t][i] = piece[t];
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t) scale[t] = (w >> (8 * t)) & 255u;
+      codes = *reinterpret_cast<const u32x4*>(base + p * (HD / 2) + (at / 4) * (2 * HD) + it.part * 16);
+      scales = *reinterpret_cast<const uint32_t*>(base + p * HD + p * (HD / 32) + (at / 4) * (HD / 8) + group * 4);
     }
   }
-  char* dst = (it.is_v ? r.v : r.k) + it.head * r.stride_h + it.group * 64;
+  char* dst = (it.is_v ? r.v : r.k) + it.head * r.stride_h + it.part * 16;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
     if (t >= it.lo && t < it.hi) {
-      const float s = __builtin_bit_cast(float, scale[t] << 23);
-      u32x4* out = reinterpret_cast<u32x4*>(dst + (it.row + t) * r.stride_t);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4 x;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) x[y] = decode_word<BF16>(codes[t][i], s, y);
-        __builtin_nontemporal_store(x, out + i);
-      }
+      const float s = fp4_scale(scales, t);
+      const u32x4 x = {decode_word<BF16>(codes[t], s, 0), decode_word<BF16>(codes[t], s, 1), decode_word<BF16>(codes[t], s, 2), decode_word<BF16>(codes[t], s, 3)};
+      __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(dst + (it.row + t) * r.stride_t));
     }
 }
 
@@ -293,7 +289,7 @@ template <class Kernel>
 int launch_rows(Kernel kernel, const Fp4Batch& a, const Fp4Rows& r, int head_dim, void* stream, const char* what) {
   if (!a.total) return COCKTAIL_OK;
   const uint64_t quads = uint64_t(a.total) / 4 + 2 * uint64_t(a.num_seqs) + 1;
-  const uint64_t blocks = (quads * (2 * a.num_kv_heads * (head_dim / kFp4Group)) + 255) / 256;
+  const uint64_t blocks = (quads * (2 * a.num_kv_heads * (head_dim / 8)) + 255) / 256;
   if (blocks >= uint64_t(1) << 31) return fail(COCKTAIL_EINVAL, "%s of %d rows of %d heads is more than one launch takes", what, a.total, a.num_kv_heads);
   const hipError_t e = launch_lds(kernel, dim3(uint32_t(blocks)), dim3(256), (a.num_seqs + 1) * sizeof(int32_t), static_cast<hipStream_t>(stream), a, r);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "%s launch failed: %s", what, hipGetErrorString(e));

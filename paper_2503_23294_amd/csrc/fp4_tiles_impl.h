@@ -36,7 +36,9 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   const Fp4Batch& bt = a.batch;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-  // which rows: tile number blockIdx.x of the batch
+  // which rows: heads first, so that the heaviest tiles of all heads come first and the tiles of a head, which read the same keys, run on the same XCD
+  const int h = blockIdx.x % bt.num_kv_heads;
+  const int number = blockIdx.x / bt.num_kv_heads / a.splits, split = blockIdx.x / bt.num_kv_heads % a.splits;   // tile of the batch, part of its keys
   int run_tiles = 0;
   if (tid == 0) found[0] = -1;
   for (int base = 0; base < bt.num_seqs; base += kThreads) {
@@ -58,17 +60,16 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
       run_tiles += scratch[w];
     }
     const int mine = before + x - v;
-    if (int(blockIdx.x) >= mine && int(blockIdx.x) < mine + v) {
+    if (number >= mine && number < mine + v) {
       found[0] = b;
-      found[1] = v - 1 - (int(blockIdx.x) - mine);   // the last rows of a sequence see most keys: first
+      found[1] = v - 1 - (number - mine);   // the last rows of a sequence see most keys: first
     }
-    if (run_tiles > int(blockIdx.x)) break;
+    if (run_tiles > number) break;
   }
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(found[0]);
   if (b < 0) return;
   const int tile = __builtin_amdgcn_readfirstlane(found[1]);
-  const int h = blockIdx.y, split = blockIdx.z;
   const Fp4Span span = fp4_span(bt, b);
   const int n = span.count, rows = n * a.rep, len = fp4_len(bt, b);
   const int r0 = tile * kTileRows;
