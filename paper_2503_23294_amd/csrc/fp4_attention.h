@@ -14,6 +14,7 @@ constexpr int kUnit = 32;               // tokens that a wave of the decode kern
 constexpr int kDecodeRows = 32;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
 constexpr int kDecodeWaves = 4;         // waves per workgroup there
 constexpr int kTileKeys = 64;           // keys per step of the tile kernel
+constexpr uint64_t kCachedBytes = 256u << 20;   // the last cache before the memory
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Fp4Attention {
@@ -28,7 +29,7 @@ struct Fp4Attention {
   int32_t workers;              // waves of the decode kernel
   int32_t decode_rows;          // sequences with at most so many rows are the decode kernel's, the others the tile kernel's
   int32_t splits;               // parts that the tile kernel cuts the keys of a row into
-  int32_t* prefix;              // workspace: units of the sequences before b [num_seqs + 1], then units per worker
+  int32_t* prefix;              // workspace: units of the sequences before b [num_seqs + 1]
   float* part_ml;               // (m, l, l unrounded) of the partial states
   float* part_o;                // their weighted sums
   float* tile_ml;
@@ -46,6 +47,9 @@ __device__ __forceinline__ Fp4Seq decode_seq(const Fp4Attention& a, int b) {
 }
 
 __device__ __forceinline__ int decode_units(const Fp4Seq& s) { return s.n > 0 ? (s.len + kUnit - 1) / kUnit : 0; }
+
+// Units of a wave of the decode kernel.
+__device__ __forceinline__ uint32_t unit_share(uint32_t units, int workers) { return (units + uint32_t(workers) - 1) / uint32_t(workers); }
 
 __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
   const _Float16 a = _Float16(lo), b = _Float16(hi);

@@ -61,41 +61,47 @@ __device__ __forceinline__ void write_merged(const Fp4Attention& a, const Merged
   if (a.lse && lane == 0) a.lse[row] = r.l == 0.f ? -__builtin_inff() : (r.top + __builtin_amdgcn_logf(r.lsum)) * kLn2;
 }
 
-// Rows of the decode kernel: a workgroup per (sequence, new token, query head) joins what the waves of its segment left, if there were
-// several, and writes rows without keys.
-template <int HD>
-__global__ __launch_bounds__(256) void fp4_merge_decode_kernel(Fp4Attention a, int most_new) {
-  constexpr int kPer = HD / 64;
-  __shared__ float o[3][HD];
+// Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves of its segment left, if there were several, and
+// writes rows without keys.  WAVES waves for a row, at least four to a workgroup.
+template <int HD, int WAVES>
+__global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode_kernel(Fp4Attention a, int most_new) {
+  constexpr int kPer = HD / 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
+  __shared__ float o[WAVES][HD];
   const Fp4Batch& bt = a.batch;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int heads = bt.num_kv_heads * a.rep;
-  const int hq = blockIdx.x % heads, bi = blockIdx.x / heads;
-  const int b = bi / most_new, i = bi % most_new;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
+  const uint32_t heads = bt.num_kv_heads * a.rep;
+  const uint32_t number = blockIdx.x * kRows + (WAVES < 4 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0);
+  const uint32_t hq = number % heads, bi = number / heads;
+  const int b = bi / uint32_t(most_new), i = bi % uint32_t(most_new);
+  if (b >= bt.num_seqs) return;   // (kRows > 1 only, where nobody waits for anybody)
+  const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
+  const uint32_t units = uint32_t(a.prefix[bt.num_seqs]) * uint32_t(bt.num_kv_heads);
   const Fp4Seq s = decode_seq(a, b);
   if (i >= s.n) return;
-  const int h = hq / a.rep;
-  const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
-  const int64_t units = int64_t(a.prefix[bt.num_seqs]) * bt.num_kv_heads;
+  const uint32_t h = hq / uint32_t(a.rep);
   const int64_t row = int64_t(s.first + i) * heads + hq;
   Merged<HD> r = {};
   if (per_head > 0) {
-    const int64_t share = (units + a.workers - 1) / a.workers;
-    const int64_t u0 = int64_t(before) * bt.num_kv_heads + int64_t(h) * per_head, u1 = u0 + per_head - 1;
-    const int64_t w0 = u0 / share, w1 = u1 / share;
+    const uint32_t share = unit_share(units, a.workers);
+    const uint32_t u0 = uint32_t(before) * uint32_t(bt.num_kv_heads) + h * uint32_t(per_head), u1 = u0 + uint32_t(per_head) - 1;
+    const uint32_t w0 = u0 / share, w1 = u1 / share;
     if (w0 == w1) return;   // its wave has finished it
-    const int in_state = i * a.rep + hq - h * a.rep;
-    r = merge_parts<HD>(a.part_ml, a.part_o, (2 * w0 + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state, 2 * (w0 + 1) * a.rows + in_state,
-                        2 * int64_t(a.rows), int(w1 - w0) + 1, wave, 4, lane);
+    const int in_state = i * a.rep + int(hq - h * a.rep);
+    r = merge_parts<HD>(a.part_ml, a.part_o, (2 * int64_t(w0) + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state, 2 * (int64_t(w0) + 1) * a.rows + in_state,
+                        2 * int64_t(a.rows), int(w1 - w0) + 1, wave, WAVES, lane);
   }
-  if (wave) {
+  if constexpr (WAVES > 1) {
+    if (wave) {
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) o[wave - 1][lane * kPer + x] = r.o[x];
+      for (int x = 0; x < kPer; ++x) o[wave][lane * kPer + x] = r.o[x];
+    }
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v)
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) r.o[x] += o[v][lane * kPer + x];
   }
-  __syncthreads();
-  if (wave) return;
-#pragma unroll
-  for (int x = 0; x < kPer; ++x) r.o[x] += (o[0][lane * kPer + x] + o[1][lane * kPer + x]) + o[2][lane * kPer + x];
   write_merged<HD>(a, r, row, lane);
 }
 
@@ -184,7 +190,7 @@ int check_attention(const cocktail_fp4_cache* c, int32_t num_q_heads, int64_t to
   if (total < 0 || total * num_q_heads > (int64_t(1) << 30)) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
   if (total && (max_new < 1 || max_new > total)) return fail(COCKTAIL_EINVAL, "max_new %d is not in 1 .. total (%lld)", max_new, (long long)total);
   const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
-  if (c->pages.num_seqs * ((capacity + kUnit - 1) / kUnit) >= (int64_t(1) << 31))
+  if (double(c->pages.num_seqs) * ((capacity + kUnit - 1) / kUnit) * c->num_kv_heads > 4.29e9)   // (numbers of units are 32 bits wide)
     return fail(COCKTAIL_EINVAL, "%d sequences of up to %lld tokens are too many for one call", c->pages.num_seqs, (long long)capacity);
   return COCKTAIL_OK;
 }
@@ -250,7 +256,13 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     e = launch(hd == 128 ? fp4_tile_kernel<128> : fp4_tile_kernel<64>, dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * kTileWaves), st, a);
   if (e == hipSuccess && s.decode) {
     const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
-    e = launch(hd == 128 ? fp4_merge_decode_kernel<128> : fp4_merge_decode_kernel<64>, dim3(uint32_t(cache->pages.num_seqs) * most_new * num_q_heads), dim3(256), st, a, most_new);
+    const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;
+    // states that a row has, about: many of them are read by many waves at a time (40 heads, 51 states each: 8.8 us by four waves), a few by one
+    const int parts = s.workers / (cache->pages.num_seqs * cache->num_kv_heads);
+    if (parts >= 16)
+      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
+    else
+      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 1> : fp4_merge_decode_kernel<64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
   }
   if (e == hipSuccess && s.splits > 1)
     e = launch(hd == 128 ? fp4_merge_tiles_kernel<128> : fp4_merge_tiles_kernel<64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);

@@ -27,53 +27,100 @@ struct Fp4Tile {
   int ok;           // wave-uniform: the page is one
 };
 
-// The pages of a segment in order, 64 of them in the lanes of a register and the next 64 on their way.
-struct Fp4Pages {
-  const int32_t* row;
-  int stride, first, ids, next;
-  __device__ __forceinline__ int fetch(int col, int lane) const { return col + lane < stride ? row[col + lane] : -1; }
-  __device__ __forceinline__ void start(const int32_t* r, int s, int col, int lane) {
-    row = r;
-    stride = s;
-    first = col;
-    ids = fetch(col, lane);
-    next = fetch(col + 64, lane);
-  }
-  __device__ __forceinline__ int get(int col, int lane) {
-    if (col >= first + 64) {
-      first += 64;
-      ids = next;
-      next = fetch(first + 64, lane);
-    }
-    return __builtin_amdgcn_readlane(ids, col - first);
-  }
+// A word of the page table through the scalar data path: the table is written by other launches only, and the address is wave-uniform.
+__device__ __forceinline__ int table_entry(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uint64_t>(p));
+}
+
+// Inclusive prefix sum over the lanes of a wave, without a trip through shared memory: shifts inside rows of 16, then the last lane of a row
+// to the rows behind it.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// Which units are whose: with up to 64 sequences every wave has them in its lanes, otherwise the workgroup has the units before every sequence
+// in LDS (pre[0 .. num_seqs]).
+struct Fp4Units {
+  Fp4Seq seq;        // of sequence `lane`
+  int units, before; // its units, and those before it
+  uint32_t total;    // of all sequences and kv heads
 };
 
-// Units before every sequence into LDS (pre[0 .. num_seqs]); `scratch`: kDecodeWaves + 1 ints.  Workgroup of 64 * kDecodeWaves threads.
-__device__ __forceinline__ void decode_prefix(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
+__device__ __forceinline__ Fp4Units number_units(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Fp4Units r = {};
   int run = 0;
-  for (int base = 0; base < a.batch.num_seqs; base += 64 * kDecodeWaves) {
-    const int b = base + threadIdx.x;
-    const int v = b < a.batch.num_seqs ? decode_units(decode_seq(a, b)) : 0;
-    int x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(x, d);
-      if (lane >= d) x += y;
+  if (a.batch.num_seqs <= 64) {
+    if (lane < a.batch.num_seqs) {
+      r.seq = decode_seq(a, lane);
+      r.units = decode_units(r.seq);
     }
-    __syncthreads();
-    if (lane == 63) scratch[wave] = x;
-    __syncthreads();
-    int before = run;
-    for (int w = 0; w < kDecodeWaves; ++w) {
-      if (w < wave) before += scratch[w];
-      run += scratch[w];
+    const int upto = wave_prefix(r.units);
+    r.before = upto - r.units;
+    run = __builtin_amdgcn_readlane(upto, 63);
+    if (blockIdx.x == 0 && wave == 0) {
+      if (lane < a.batch.num_seqs) a.prefix[lane] = r.before;
+      if (lane == 0) a.prefix[a.batch.num_seqs] = run;
     }
-    if (b < a.batch.num_seqs) pre[b] = before + x - v;
+  } else {
+    for (int base = 0; base < a.batch.num_seqs; base += 64 * kDecodeWaves) {
+      const int b = base + threadIdx.x;
+      const int v = b < a.batch.num_seqs ? decode_units(decode_seq(a, b)) : 0;
+      const int x = wave_prefix(v);
+      __syncthreads();
+      if (lane == 63) scratch[wave] = x;
+      __syncthreads();
+      int before = run;
+      for (int w = 0; w < kDecodeWaves; ++w) {
+        if (w < wave) before += scratch[w];
+        run += scratch[w];
+      }
+      if (b < a.batch.num_seqs) pre[b] = before + x - v;
+    }
+    if (threadIdx.x == 0) pre[a.batch.num_seqs] = run;
+    __syncthreads();
+    if (blockIdx.x == 0)
+      for (int b = threadIdx.x; b <= a.batch.num_seqs; b += 64 * kDecodeWaves) a.prefix[b] = pre[b];
   }
-  if (threadIdx.x == 0) pre[a.batch.num_seqs] = run;
-  __syncthreads();
+  r.total = uint32_t(run) * uint32_t(a.batch.num_kv_heads);
+  return r;
+}
+
+// The sequence of unit u: the last one with units that has no more than u before it.
+struct Fp4Place {
+  int b, before, per_head;
+  Fp4Seq seq;
+};
+__device__ __forceinline__ Fp4Place find_unit(const Fp4Attention& a, const Fp4Units& units, const int32_t* pre, uint32_t u) {
+  Fp4Place p;
+  const uint32_t heads = a.batch.num_kv_heads;
+  if (a.batch.num_seqs <= 64) {
+    const uint64_t candidates = __ballot(units.units > 0 && uint32_t(units.before) * heads <= u);
+    p.b = 63 - __builtin_clzll(candidates);
+    p.before = __builtin_amdgcn_readlane(units.before, p.b);
+    p.per_head = __builtin_amdgcn_readlane(units.units, p.b);
+    p.seq = {__builtin_amdgcn_readlane(units.seq.first, p.b), __builtin_amdgcn_readlane(units.seq.n, p.b), __builtin_amdgcn_readlane(units.seq.len, p.b)};
+  } else {
+    int b = 0, e = a.batch.num_seqs;
+    while (e - b > 1) {
+      const int m = (b + e) >> 1;
+      if (uint32_t(pre[m]) * heads <= u) b = m;
+      else e = m;
+    }
+    // (of sequences with the same number before them the search ends at the last, which is the one with units)
+    p.b = __builtin_amdgcn_readfirstlane(b);
+    p.before = __builtin_amdgcn_readfirstlane(pre[p.b]);
+    p.per_head = __builtin_amdgcn_readfirstlane(pre[p.b + 1]) - p.before;
+    const Fp4Seq s = decode_seq(a, p.b);
+    p.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+  }
+  return p;
 }
 
 template <int HD, int RT>
@@ -84,17 +131,16 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Att
   __shared__ int32_t scratch[kDecodeWaves + 1];
   const int lane = threadIdx.x & 63;
   const int c16 = lane & 15, j = lane >> 4;
-  decode_prefix(a, pre, scratch);
   const Fp4Batch& bt = a.batch;
-  const int64_t units = int64_t(pre[bt.num_seqs]) * bt.num_kv_heads;
-  const int64_t share = (units + a.workers - 1) / a.workers;
-  if (blockIdx.x == 0) {
-    for (int b = threadIdx.x; b <= bt.num_seqs; b += 64 * kDecodeWaves) a.prefix[b] = pre[b];
-  }
+  const Fp4Units units = number_units(a, pre, scratch);
+  const uint32_t share = unit_share(units.total, a.workers);
   const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
-  int64_t u = w * share;
-  const int64_t end = u + share < units ? u + share : units;
+  uint32_t u = w * share;
+  const uint32_t end = u + share < units.total ? u + share : units.total;
   if (u >= end) return;
+  // read once and not again before hundreds of MB have passed: past the caches, which then read faster (128K, 40 heads: 130 -> 111 us); what
+  // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches)
+  const bool stream = uint64_t(units.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
   // byte offsets of a lane's pieces in 16 tokens
@@ -104,45 +150,88 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Att
   const uint32_t off_vs = uint32_t(P) * HD + uint32_t(P) * (HD / 32) + j * (HD / 8) + (HD == 128 ? c16 >> 2 : c16 >> 3) * 4;
 
   bool first_segment = true;
-  int b = 0, e = bt.num_seqs;   // the sequence of unit u: the last one with no more units before it
-  while (e - b > 1) {
-    const int m = (b + e) >> 1;
-    if (int64_t(pre[m]) * bt.num_kv_heads <= u) b = m;
-    else e = m;
-  }
   while (u < end) {
-    while (int64_t(__builtin_amdgcn_readfirstlane(pre[b + 1])) * bt.num_kv_heads <= u) ++b;
-    b = __builtin_amdgcn_readfirstlane(b);
-    const int before = __builtin_amdgcn_readfirstlane(pre[b]);
-    const int per_head = __builtin_amdgcn_readfirstlane(pre[b + 1]) - before;
-    const int64_t local = u - int64_t(before) * bt.num_kv_heads;
-    const int h = int(local / per_head), u0 = int(local - int64_t(h) * per_head);
-    const int u1 = int(end - u < per_head - u0 ? u0 + (end - u) : per_head);
-    const Fp4Seq seq = decode_seq(a, b);
-    const int n = seq.n, len = seq.len, rows = n * a.rep;
+    const Fp4Place place = find_unit(a, units, pre, u);
+    const int b = place.b, per_head = place.per_head;
+    const uint32_t local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
+    const int h = local / uint32_t(per_head), u0 = local - uint32_t(h) * per_head;
+    const int u1 = end - u < uint32_t(per_head - u0) ? u0 + int(end - u) : per_head;
+    const int n = place.seq.n, len = place.seq.len, rows = n * a.rep;
 
     // the queries: lane (row c16, quarter j) has the channels that its K pieces have
+    u32x4 raw[RT][kSteps] = {};
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = rt * 16 + c16, i = r / a.rep;
+      if (r < rows) {
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.q + (place.seq.first + i) * a.stride_t + (h * a.rep + r - i * a.rep) * a.stride_h + j * (HD / 2));
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) raw[rt][s] = src[s];
+      }
+    }
+
+    // The tiles of the segment in order.  Every step loads two tiles and reads the table for two further on, whether they exist or not
+    // (the last ones are then loaded again): with loads under a condition, the number of those in flight is not known when the code is made,
+    // and every wait becomes one for all of them.
+    const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
+    const int last_tile = 2 * u1 - 1 < (len + 15) / 16 - 1 ? 2 * u1 - 1 : (len + 15) / 16 - 1;
+    const int tiles_per_page = P / 16;
+    int tile = 2 * u0, col = tile / tiles_per_page, in_page = tile - col * tiles_per_page;   // of the table read
+    auto next_tile = [&](int& id, int& at) {
+      id = table_entry(table + col);
+      at = in_page;
+      const int more = tile < last_tile ? 1 : 0;
+      tile += more;
+      in_page += more;
+      const bool turn = in_page == tiles_per_page;
+      col += turn ? 1 : 0;
+      in_page = turn ? 0 : in_page;
+    };
+    int id0, id1, at0, at1;   // of the next two tiles to load
+    next_tile(id0, at0);
+    next_tile(id1, at1);
+    const char* head = bt.pool + h * run;
+    const int64_t page_bytes = run * bt.num_kv_heads;
+    auto load_tile = [&](auto policy, Fp4Tile<HD>& t, int id, int at) {
+      constexpr int kPolicy = decltype(policy)::value;
+      // a resource per page: the address is a base in scalar registers, an offset of the lane that never changes and one of the tile; a page
+      // that is none has no bytes, and reads of it give zeros
+      t.ok = uint32_t(id) < uint32_t(bt.num_pages);
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(head + (t.ok ? id : 0) * page_bytes), 0, t.ok ? int(run) : 0, 0x00020000);
+      const int rows = at * (8 * HD), scales = at * (HD / 2);   // 16 tokens
+      if constexpr (HD == 128) {
+        t.k = __builtin_amdgcn_raw_buffer_load_b128(rs, off_k, rows, kPolicy);
+      } else {
+        const u32x2 half = __builtin_amdgcn_raw_buffer_load_b64(rs, off_k, rows, kPolicy);
+        t.k = u32x4{half[0], half[1], 0, 0};
+      }
+      t.v = __builtin_amdgcn_raw_buffer_load_b128(rs, off_v, rows, kPolicy);
+      t.k_scale = __builtin_amdgcn_raw_buffer_load_b8(rs, off_ks, scales, 0);
+      t.v_scale = __builtin_amdgcn_raw_buffer_load_b32(rs, off_vs, scales, 0);
+    };
+    auto load_unit = [&](auto policy, Fp4Tile<HD>& ta, Fp4Tile<HD>& tb) {
+      load_tile(policy, ta, id0, at0);
+      load_tile(policy, tb, id1, at1);
+      next_tile(id0, at0);
+      next_tile(id1, at1);
+    };
+    Fp4Tile<HD> x0, x1, y0, y1;
+    if (stream) load_unit(std::integral_constant<int, 2>{}, x0, x1);
+    else load_unit(std::integral_constant<int, 0>{}, x0, x1);
+
     h8 q[RT][kSteps];
     float c[RT], m[RT], lsum[RT];
     f32x4 l[RT], o[RT][kChannelTiles];
     int lim[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int r = rt * 16 + c16, i = r / a.rep;
-      const bool live = r < rows;
-      u32x4 raw[kSteps] = {};
-      if (live) {
-        const u32x4* src = reinterpret_cast<const u32x4*>(a.q + (seq.first + i) * a.stride_t + (h * a.rep + r - i * a.rep) * a.stride_h + j * (HD / 2));
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) raw[s] = src[s];
-      }
       c[rt] = a.scale;
       if (a.bf16) {
         float top = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(fabsf(bf_lo(raw[s][x])), fabsf(bf_hi(raw[s][x]))));
+          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(fabsf(bf_lo(raw[rt][s][x])), fabsf(bf_hi(raw[rt][s][x]))));
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float f = row_factor(top), inv = 1.f / f;
@@ -150,40 +239,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Att
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) raw[s][x] = pack_halves(bf_lo(raw[s][x]) * inv, bf_hi(raw[s][x]) * inv);
+          for (int x = 0; x < 4; ++x) raw[rt][s][x] = pack_halves(bf_lo(raw[rt][s][x]) * inv, bf_hi(raw[rt][s][x]) * inv);
       }
       c[rt] = fmaxf(c[rt], 1.2e-38f);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) q[rt][s] = __builtin_bit_cast(h8, raw[s]);
-      lim[rt] = live ? len - n + i + 1 : 0;
+      for (int s = 0; s < kSteps; ++s) q[rt][s] = __builtin_bit_cast(h8, raw[rt][s]);
+      const int r = rt * 16 + c16;
+      lim[rt] = r < rows ? len - n + r / a.rep + 1 : 0;
       m[rt] = kNoMax;
       lsum[rt] = 0.f;
       l[rt] = f32x4{};
 #pragma unroll
       for (int ct = 0; ct < kChannelTiles; ++ct) o[rt][ct] = f32x4{};
     }
-
-    Fp4Pages pages;
-    int col = u0 * kUnit / P, at = u0 * kUnit - col * P;   // of the next tile to load
-    pages.start(bt.table + int64_t(b) * bt.table_stride, bt.table_stride, col, lane);
-    int left = len - u0 * kUnit;                            // tokens from the next tile to load on
-    auto load_tile = [&](Fp4Tile<HD>& t) {
-      const int id = left > 0 ? pages.get(col, lane) : -1;
-      t.ok = uint32_t(id) < uint32_t(bt.num_pages);
-      const char* base = bt.pool + (int64_t(t.ok ? id : 0) * bt.num_kv_heads + h) * run;
-      if constexpr (HD == 128) {
-        t.k = *reinterpret_cast<const u32x4*>(base + at * (HD / 2) + off_k);
-      } else {
-        const u32x2 half = *reinterpret_cast<const u32x2*>(base + at * (HD / 2) + off_k);
-        t.k = u32x4{half[0], half[1], 0, 0};
-      }
-      t.k_scale = *reinterpret_cast<const uint8_t*>(base + at * (HD / 32) + off_ks);
-      t.v = *reinterpret_cast<const u32x4*>(base + at * (HD / 2) + off_v);
-      t.v_scale = *reinterpret_cast<const uint32_t*>(base + at * (HD / 32) + off_vs);
-      at += 16;
-      left -= 16;
-      if (at == P) at = 0, ++col;
-    };
     const int free_below = len - n + 1;   // tokens that every query sees
 
     auto compute = [&](Fp4Tile<HD>& ta, Fp4Tile<HD>& tb, int tok0) {
@@ -274,22 +342,18 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Att
     };
 
     // the next unit is on its way while one is worked on
-    Fp4Tile<HD> x0, x1, y0, y1;
-    load_tile(x0);
-    load_tile(x1);
-    for (int k = u0; k < u1; k += 2) {
-      if (k + 1 < u1) {
-        load_tile(y0);
-        load_tile(y1);
+    auto walk = [&](auto policy) {
+      for (int k = u0;;) {
+        load_unit(policy, y0, y1);
+        compute(x0, x1, k * kUnit);
+        if (++k >= u1) break;
+        load_unit(policy, x0, x1);
+        compute(y0, y1, k * kUnit);
+        if (++k >= u1) break;
       }
-      compute(x0, x1, k * kUnit);
-      if (k + 1 >= u1) break;
-      if (k + 2 < u1) {
-        load_tile(x0);
-        load_tile(x1);
-      }
-      compute(y0, y1, (k + 1) * kUnit);
-    }
+    };
+    if (stream) walk(std::integral_constant<int, 2>{});
+    else walk(std::integral_constant<int, 0>{});
 
     // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
     // each end, so two places per wave are enough
@@ -305,7 +369,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Att
       const float lr = l[rt][0];
       if (whole) {
         const int i = r / a.rep;
-        const int64_t row = int64_t(seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
+        const int64_t row = int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
         const float inv = lr == 0.f ? 0.f : 1.f / lr;
         char* dst = a.out + row * (2 * HD) + j * (HD / 2);
 #pragma unroll
