@@ -11,7 +11,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kNoMax = -3.0e38f;      // reference maximum of a row that has seen no key
 constexpr float kMaxSlack = 8.0f;       // a reference maximum may be this much too small (base 2) before it is raised: weights up to 2^8
 constexpr int kUnit = 32;               // tokens that a wave of the decode kernel takes at a time
-constexpr int kDecodeRows = 32;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
+constexpr int kDecodeRows = 64;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
 constexpr int kDecodeWaves = 4;         // waves per workgroup there
 constexpr int kTileKeys = 64;           // keys per step of the tile kernel
 constexpr uint64_t kCachedBytes = 256u << 20;   // the last cache before the memory

@@ -154,14 +154,17 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   s.tiles = most_rows > kDecodeRows;
   s.decode = !s.tiles || (!uniform && rep <= kDecodeRows);
   s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
-  s.row_tiles = s.rows <= 16 ? 1 : 2;
+  s.row_tiles = (s.rows + 15) / 16;
   if (s.decode) {
-    // Two waves per SIMD of 256 compute units; not less than two units for a wave, where the reads that a wave waits for one after the other
-    // weigh more than the units do.
+    // Two waves per SIMD of 256 compute units (128K, 40 heads: 1024, 2048, 3072 waves 116, 111, 113 us), one where a wave has more than one operand of
+    // queries (8 x 16K, 32 rows: 2048 waves 53 us, 1024 48 us; their states are larger and the matrix cores have more to do); and four units at
+    // least for a wave, at half a microsecond each: with fewer the states cost more than that (8 heads, 16K: 2, 4, 8 units 20.8, 15.4, 15.0 us;
+    // 2K: 10.2, 10.9, 14.7).
     const int64_t seqs = c->pages.num_seqs < total ? c->pages.num_seqs : total;
     const int64_t units = seqs * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
-    int64_t workers = (units + 1) / 2;
-    workers = workers > 2048 ? 2048 : workers < 4 ? 4 : (workers + 3) / 4 * 4;
+    int64_t workers = (units + 3) / 4;
+    const int64_t fill = s.row_tiles == 1 ? 2048 : 1024;
+    workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
@@ -248,8 +251,10 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (s.decode) {
-    auto kernel = hd == 128 ? (s.row_tiles == 1 ? fp4_decode_kernel<128, 1> : fp4_decode_kernel<128, 2>)
-                            : (s.row_tiles == 1 ? fp4_decode_kernel<64, 1> : fp4_decode_kernel<64, 2>);
+    typedef void (*Kernel)(Fp4Attention);
+    static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1>, fp4_decode_kernel<64, 2>, fp4_decode_kernel<64, 3>, fp4_decode_kernel<64, 4>},
+                                         {fp4_decode_kernel<128, 1>, fp4_decode_kernel<128, 2>, fp4_decode_kernel<128, 3>, fp4_decode_kernel<128, 4>}};
+    const Kernel kernel = kernels[hd == 128][s.row_tiles - 1];
     e = launch_lds(kernel, dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }
   if (e == hipSuccess && s.tiles)
@@ -259,7 +264,7 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;
     // states that a row has, about: many of them are read by many waves at a time (40 heads, 51 states each: 8.8 us by four waves), a few by one
     const int parts = s.workers / (cache->pages.num_seqs * cache->num_kv_heads);
-    if (parts >= 16)
+    if (parts >= 16 && most <= 512)
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
     else
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 1> : fp4_merge_decode_kernel<64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);

@@ -124,7 +124,7 @@ __device__ __forceinline__ Fp4Place find_unit(const Fp4Attention& a, const Fp4Un
 }
 
 template <int HD, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void fp4_decode_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];

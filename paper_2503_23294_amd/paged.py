@@ -1,11 +1,11 @@
 """Binding of the paged 4-bit cache: the page table (cocktail_pages_*) and the cache on top of it (cocktail_fp4_*).
 
-Same names as the C entry points.  torch supplies device memory and streams; workspaces are taken from its allocator per call, in the
-order of the call's stream, so that calls on several streams or in several captured graphs never share one.
+Same names as the C entry points.  torch supplies device memory and streams.  Workspaces: a cache keeps one per stream for the calls that are
+made on it, one after the other; what is captured into a graph has one of its own, from the graph's memory, so that graphs and eager calls never
+share one.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from typing import Optional, Sequence, Tuple
 
@@ -19,14 +19,31 @@ _DTYPES = {torch.float16: _lib.FP16, torch.bfloat16: _lib.BF16}
 
 
 def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
-    """Makes the tensors' device current for the call, and the stream for what is allocated in it."""
+    """Makes the tensors' device current for the call, and the stream for what is allocated in it; None where both are already."""
     if stream is not None:
         if stream.device != device:
             raise ValueError("the stream belongs to another device than the tensors")
         return torch.cuda.stream(stream)
     if device.index != torch.cuda.current_device():
         return torch.cuda.device(device)
-    return contextlib.nullcontext()
+    return None
+
+
+class _Workspaces:
+    """Workspaces by stream."""
+
+    def __init__(self, device: torch.device):
+        self.device = device
+        self.kept = {}
+
+    def get(self, need: int, stream: int) -> torch.Tensor:
+        """A workspace for a call that is about to be made on the current stream, whose handle is `stream`."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws = self.kept.get(stream)
+        if ws is None or ws.numel() < need:
+            ws = self.kept[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return ws
 
 
 def _int32(name: str, t: torch.Tensor, shape: Tuple[int, ...], device: torch.device) -> None:
@@ -69,6 +86,7 @@ class PageTable:
         need = C.c_size_t(0)
         check(lib().cocktail_pages_workspace(C.byref(self.desc), C.byref(need)))   # also checks the sizes
         self.workspace_bytes = int(need.value)
+        self.workspaces = _Workspaces(dev)
 
     @property
     def num_seqs(self) -> int:
@@ -94,6 +112,9 @@ class Fp4Cache:
         self.pages, self.pool = pages, pool
         self.num_kv_heads, self.head_dim = int(num_kv_heads), int(head_dim)
         self.desc = _lib.Fp4CacheDesc(pages.desc, pool.data_ptr(), self.num_kv_heads, self.head_dim)
+        self.desc_ref = C.byref(self.desc)
+        self.workspaces = _Workspaces(pages.device)
+        self.workspace_bytes = {}   # by the sizes of the call
 
 
 def _pool_list(pages: PageTable, pools: Sequence[torch.Tensor]):
@@ -115,51 +136,67 @@ def cocktail_pages_resize(pages: PageTable, delta: torch.Tensor, pools: Sequence
                           stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sequence b becomes delta[b] tokens longer or shorter (device int32 [num_seqs]).  A partly filled page that others hold is
     copied, in all `pools` (tensors [num_pages, ...]), before its sequence grows out of it."""
+    on = _on(pages.device, stream)
+    if on is not None:
+        with on:
+            return cocktail_pages_resize(pages, delta, pools)
     _int32("delta", delta, (pages.num_seqs,), pages.device)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    with _on(pages.device, stream):
-        ws = pages.refs.new_empty((pages.workspace_bytes + 3) // 4)
-        check(lib().cocktail_pages_resize(C.byref(pages.desc), delta.data_ptr(), array, n, bytes_per_page, ws.data_ptr(),
-                                          pages.workspace_bytes, _stream_ptr(stream)))
+    st = _stream_ptr(None)
+    check(lib().cocktail_pages_resize(C.byref(pages.desc), delta.data_ptr(), array, n, bytes_per_page,
+                                      pages.workspaces.get(pages.workspace_bytes, st).data_ptr(), pages.workspace_bytes, st))
 
 
 def cocktail_pages_fork(pages: PageTable, source: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sequence b becomes what sequence source[b] was (device int32 [num_seqs]); source[b] == b leaves it, a negative one frees it."""
+    on = _on(pages.device, stream)
+    if on is not None:
+        with on:
+            return cocktail_pages_fork(pages, source)
     _int32("source", source, (pages.num_seqs,), pages.device)
-    with _on(pages.device, stream):
-        check(lib().cocktail_pages_fork(C.byref(pages.desc), source.data_ptr(), _stream_ptr(stream)))
+    check(lib().cocktail_pages_fork(C.byref(pages.desc), source.data_ptr(), _stream_ptr(None)))
 
 
 def cocktail_pages_compact(pages: PageTable, pools: Sequence[torch.Tensor] = (), stream: Optional[torch.cuda.Stream] = None) -> None:
     """Moves the pages in use to the front of the pools."""
+    on = _on(pages.device, stream)
+    if on is not None:
+        with on:
+            return cocktail_pages_compact(pages, pools)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    with _on(pages.device, stream):
-        ws = pages.refs.new_empty((pages.workspace_bytes + 3) // 4)
-        check(lib().cocktail_pages_compact(C.byref(pages.desc), array, n, bytes_per_page, ws.data_ptr(), pages.workspace_bytes,
-                                           _stream_ptr(stream)))
+    st = _stream_ptr(None)
+    check(lib().cocktail_pages_compact(C.byref(pages.desc), array, n, bytes_per_page,
+                                       pages.workspaces.get(pages.workspace_bytes, st).data_ptr(), pages.workspace_bytes, st))
 
 
 def cocktail_pages_check(pages: PageTable, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Waits for the stream and raises CocktailError (code -6) if the last cocktail_pages_resize could not be done."""
-    with _on(pages.device, stream):
-        check(lib().cocktail_pages_check(C.byref(pages.desc), _stream_ptr(stream)))
+    on = _on(pages.device, stream)
+    if on is not None:
+        with on:
+            return cocktail_pages_check(pages)
+    check(lib().cocktail_pages_check(C.byref(pages.desc), _stream_ptr(None)))
 
 
-def _rows(name: str, t: torch.Tensor, heads: int, head_dim: int, device: torch.device) -> None:
-    if t.dtype not in _DTYPES or t.device != device or t.dim() != 3 or tuple(t.shape[1:]) != (heads, head_dim) or t.stride(2) != 1:
-        raise TypeError(f"{name} must be a float16 or bfloat16 tensor [tokens, {heads}, {head_dim}] on {device}, channels contiguous")
+def _rows(name: str, t: torch.Tensor, heads: int, head_dim: int, device: torch.device) -> Tuple[int, int, int]:
+    """Checks rows [tokens, heads, head_dim] and gives their number and their strides of tokens and heads (those of a dimension of one entry
+    say nothing)."""
+    shape = t.shape
+    if t.dtype not in _DTYPES or t.device != device or len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
+        raise TypeError(f"{name} must be a float16 or bfloat16 tensor [tokens, {heads}, {head_dim}] on {device}")
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise TypeError(f"the channels of {name} must be contiguous")
+    return shape[0], st if shape[0] > 1 else heads * head_dim, sh if heads > 1 else head_dim
 
 
 def _starts(cache: Fp4Cache, starts: Optional[torch.Tensor]) -> Optional[int]:
     if starts is None:
         return None
-    _int32("starts", starts, (cache.pages.num_seqs + 1,), cache.pages.device)
+    if starts.dtype != torch.int32 or starts.device != cache.pages.device or starts.dim() != 1 or \
+            starts.shape[0] != cache.pages.num_seqs + 1 or not starts.is_contiguous():
+        raise TypeError(f"starts must be a contiguous int32 tensor [{cache.pages.num_seqs + 1}] on {cache.pages.device}")
     return starts.data_ptr()
-
-
-def _strides(t: torch.Tensor) -> Tuple[int, int]:
-    """Strides of tokens and heads; those of a dimension of one entry say nothing."""
-    return (int(t.stride(0)) if t.shape[0] > 1 else t.shape[1] * t.shape[2], int(t.stride(1)) if t.shape[1] > 1 else t.shape[2])
 
 
 def cocktail_fp4_store(cache: Fp4Cache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
@@ -167,32 +204,34 @@ def cocktail_fp4_store(cache: Fp4Cache, k: torch.Tensor, v: torch.Tensor, starts
     """Quantizes new tokens into the cache: rows starts[b] .. starts[b+1] of k and v ([tokens, Hkv, D]) become the last tokens of sequence
     b.  Without `starts` every sequence has the same number of rows.  Call cocktail_pages_resize first: it makes the room."""
     dev = cache.pages.device
-    _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
-    _rows("v", v, cache.num_kv_heads, cache.head_dim, dev)
-    if k.dtype != v.dtype or k.shape != v.shape or _strides(k) != _strides(v):
+    on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return cocktail_fp4_store(cache, k, v, starts)
+    rows = _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
+    if rows != _rows("v", v, cache.num_kv_heads, cache.head_dim, dev) or k.dtype != v.dtype:
         raise ValueError("k and v must have the same type, shape and strides")
-    st, sh = _strides(k)
-    with _on(dev, stream):
-        check(lib().cocktail_fp4_store(C.byref(cache.desc), k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], st, sh, k.shape[0],
-                                       _starts(cache, starts), _stream_ptr(stream)))
+    check(lib().cocktail_fp4_store(cache.desc_ref, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], rows[1], rows[2], rows[0],
+                                   _starts(cache, starts), _stream_ptr(None)))
 
 
 def cocktail_fp4_gather(cache: Fp4Cache, total: int, starts: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float16,
                         out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream: Optional[torch.cuda.Stream] = None):
     """Reads tokens back as the values they stand for: k, v [total, Hkv, D], rows as in cocktail_fp4_store."""
     dev = cache.pages.device
-    with _on(dev, stream):
-        if out is None:
-            shape = (int(total), cache.num_kv_heads, cache.head_dim)
-            out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
-        k, v = out
-        _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
-        _rows("v", v, cache.num_kv_heads, cache.head_dim, dev)
-        if k.dtype != v.dtype or k.shape != v.shape or _strides(k) != _strides(v) or k.shape[0] != total:
-            raise ValueError("k and v must have the same type, shape and strides, and `total` rows")
-        st, sh = _strides(k)
-        check(lib().cocktail_fp4_gather(C.byref(cache.desc), k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], st, sh, int(total),
-                                        _starts(cache, starts), _stream_ptr(stream)))
+    on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return cocktail_fp4_gather(cache, total, starts, dtype, out)
+    if out is None:
+        shape = (int(total), cache.num_kv_heads, cache.head_dim)
+        out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+    k, v = out
+    rows = _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
+    if rows != _rows("v", v, cache.num_kv_heads, cache.head_dim, dev) or k.dtype != v.dtype or rows[0] != total:
+        raise ValueError("k and v must have the same type, shape and strides, and `total` rows")
+    check(lib().cocktail_fp4_gather(cache.desc_ref, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], rows[1], rows[2], rows[0],
+                                    _starts(cache, starts), _stream_ptr(None)))
     return k, v
 
 
@@ -203,27 +242,36 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
     (out, lse).  max_new: no sequence has more queries (default: as many as there are rows); max_len: about the longest
     sequence, for the split of the work (default: what the table can hold)."""
     dev = cache.pages.device
+    on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return cocktail_fp4_attention(cache, q, starts, max_new, max_len, sm_scale, out, lse)
     if q.dim() != 3:
         raise TypeError("q must be [tokens, Hq, D]")
-    total, heads = int(q.shape[0]), int(q.shape[1])
-    _rows("q", q, heads, cache.head_dim, dev)
+    heads = q.shape[1]
+    total, st, sh = _rows("q", q, heads, cache.head_dim, dev)
     if max_new is None:
         max_new = total // cache.pages.num_seqs if starts is None else total
-    need = C.c_size_t(0)
-    st, sh = _strides(q)
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty((total, heads, cache.head_dim), dtype=q.dtype, device=dev)
-        elif out.dtype != q.dtype or out.shape != q.shape or out.device != dev or not out.is_contiguous():
-            raise ValueError("out must be a contiguous tensor of q's type, shape and device")
-        if lse is None:
-            lse = torch.empty((total, heads), dtype=torch.float32, device=dev)
-        elif lse.dtype != torch.float32 or tuple(lse.shape) != (total, heads) or lse.device != dev or not lse.is_contiguous():
-            raise ValueError("lse must be a contiguous float32 tensor [tokens, Hq]")
-        check(lib().cocktail_fp4_attention_workspace(C.byref(cache.desc), heads, total, int(max_new), int(max_len),
-                                                     1 if starts is None else 0, C.byref(need)))
-        ws = torch.empty(int(need.value), dtype=torch.uint8, device=dev)
-        check(lib().cocktail_fp4_attention(C.byref(cache.desc), heads, q.data_ptr(), _DTYPES[q.dtype], st, sh, total,
-                                           _starts(cache, starts), int(max_new), int(max_len), float(sm_scale), out.data_ptr(),
-                                           lse.data_ptr(), ws.data_ptr(), int(need.value), _stream_ptr(stream)))
+    if out is None:
+        out = torch.empty((total, heads, cache.head_dim), dtype=q.dtype, device=dev)
+    elif out.dtype != q.dtype or out.shape != q.shape or out.device != dev or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's type, shape and device")
+    if lse is None:
+        lse = torch.empty((total, heads), dtype=torch.float32, device=dev)
+    elif lse.dtype != torch.float32 or tuple(lse.shape) != (total, heads) or lse.device != dev or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [tokens, Hq]")
+    first = _starts(cache, starts)
+    key = (heads, total, max_new, max_len, starts is None)
+    need = cache.workspace_bytes.get(key)
+    if need is None:
+        size = C.c_size_t(0)
+        check(lib().cocktail_fp4_attention_workspace(cache.desc_ref, heads, total, int(max_new), int(max_len),
+                                                     1 if starts is None else 0, C.byref(size)))
+        if len(cache.workspace_bytes) > 4096:
+            cache.workspace_bytes.clear()
+        need = cache.workspace_bytes[key] = int(size.value)
+    handle = _stream_ptr(None)
+    check(lib().cocktail_fp4_attention(cache.desc_ref, heads, q.data_ptr(), _DTYPES[q.dtype], st, sh, total, first, int(max_new), int(max_len),
+                                       float(sm_scale), out.data_ptr(), lse.data_ptr(), cache.workspaces.get(need, handle).data_ptr(), need,
+                                       handle))
     return out, lse
