@@ -71,4 +71,21 @@ __device__ __forceinline__ float row_factor(float top) {
   return top == 0.f ? 1.f : __builtin_bit_cast(float, (e < 20u ? 20u : e > 230u ? 230u : e) << 23);
 }
 
+// A word of the page table through the scalar data path: the table is written by other launches only, and the address is wave-uniform.
+__device__ __forceinline__ int table_entry(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uint64_t>(p));
+}
+
+// Inclusive prefix sum over the lanes of a wave, without a trip through shared memory: shifts inside rows of 16, then the last lane of a row
+// to the rows behind it.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
 }  // namespace cocktail

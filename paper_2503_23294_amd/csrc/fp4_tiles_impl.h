@@ -19,11 +19,18 @@ struct Fp4TileLds {
   static constexpr int kChannelStride = kTileKeys + 8;
   _Float16 k[kTileKeys * kKeyStride];
   _Float16 v[HD * kChannelStride];
-  int32_t ok[4];
 };
 
 __device__ __forceinline__ int tile_count(const Fp4Attention& a, const Fp4Span& s) {
   return s.count * a.rep > a.decode_rows ? (s.count * a.rep + kTileRows - 1) / kTileRows : 0;
+}
+
+// One of four values that are the same in all lanes, by the lane's own number.
+__device__ __forceinline__ const char* pick(int k, const char* a, const char* b, const char* c, const char* d) {
+  const uint64_t x = uint64_t(a), y = uint64_t(b), z = uint64_t(c), w = uint64_t(d);
+  const uint32_t lo01 = (k & 1) ? uint32_t(y) : uint32_t(x), hi01 = (k & 1) ? uint32_t(y >> 32) : uint32_t(x >> 32);
+  const uint32_t lo23 = (k & 1) ? uint32_t(w) : uint32_t(z), hi23 = (k & 1) ? uint32_t(w >> 32) : uint32_t(z >> 32);
+  return reinterpret_cast<const char*>(uint64_t((k & 2) ? hi23 : hi01) << 32 | ((k & 2) ? lo23 : lo01));
 }
 
 template <int HD>
@@ -31,26 +38,22 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   constexpr int kThreads = 64 * kTileWaves;
   constexpr int kSteps = HD / 16, kChannelTiles = HD / 32;
   constexpr int kItems = 2 * HD;                     // 16-byte pieces of 64 keys, of K and of V each
-  __shared__ Fp4TileLds<HD> lds;
+  __shared__ Fp4TileLds<HD> buffers[2];
   __shared__ int32_t found[4], scratch[kTileWaves + 1];
   const Fp4Batch& bt = a.batch;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // which rows: heads first, so that the heaviest tiles of all heads come first and the tiles of a head, which read the same keys, run on the same XCD
-  const int h = blockIdx.x % bt.num_kv_heads;
-  const int number = blockIdx.x / bt.num_kv_heads / a.splits, split = blockIdx.x / bt.num_kv_heads % a.splits;   // tile of the batch, part of its keys
+  const uint32_t heads = bt.num_kv_heads, splits = a.splits;
+  const int h = blockIdx.x % heads;
+  const int number = blockIdx.x / heads / splits, split = blockIdx.x / heads % splits;   // tile of the batch, part of its keys
   int run_tiles = 0;
   if (tid == 0) found[0] = -1;
   for (int base = 0; base < bt.num_seqs; base += kThreads) {
     const int b = base + tid;
     const Fp4Span s = b < bt.num_seqs ? fp4_span(bt, b) : Fp4Span{0, 0};
     const int v = tile_count(a, s);
-    int x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
+    const int x = wave_prefix(v);
     __syncthreads();
     if (lane == 63) scratch[wave] = x;
     __syncthreads();
@@ -71,13 +74,14 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   if (b < 0) return;
   const int tile = __builtin_amdgcn_readfirstlane(found[1]);
   const Fp4Span span = fp4_span(bt, b);
-  const int n = span.count, rows = n * a.rep, len = fp4_len(bt, b);
+  const int first = __builtin_amdgcn_readfirstlane(span.first), n = __builtin_amdgcn_readfirstlane(span.count);
+  const int rows = n * a.rep, len = __builtin_amdgcn_readfirstlane(fp4_len(bt, b));
   const int r0 = tile * kTileRows;
   const int last_row = (r0 + kTileRows < rows ? r0 + kTileRows : rows) - 1;
   int most = len - n + last_row / a.rep + 1;          // keys that the last row sees
   most = most < 0 ? 0 : most;
-  const int steps = (most + kTileKeys - 1) / kTileKeys;
-  const int k0 = int(int64_t(steps) * split / a.splits), k1 = int(int64_t(steps) * (split + 1) / a.splits);
+  const uint32_t steps = (most + kTileKeys - 1) / kTileKeys;
+  const int k0 = steps * uint32_t(split) / splits, k1 = steps * uint32_t(split + 1) / splits;   // (steps < 2^25, splits up to 64)
 
   // the wave's rows
   const int row_lane = lane & 31, half = lane >> 5;
@@ -87,12 +91,111 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   const int wave_first = r0 + wave * 32, wave_last = wave_first + 31 < rows ? wave_first + 31 : rows - 1;
   const int wave_most = wave_first < rows ? len - n + wave_last / a.rep + 1 : 0;   // beyond: nothing to do for this wave
   const int wave_free = wave_first + 31 < rows ? len - n + wave_first / a.rep + 1 : 0;   // below: no masking
+
+  // a thread's pieces of every 64 keys: of K token key_k, channels 32 g .. 32 g + 31; of V a quad of tokens, eight channels
+  constexpr bool kBoth = kItems > kThreads / 2;      // else half of the threads takes K, the other half V
+  const int item = kBoth ? tid : tid % kItems;
+  const bool does_k = kBoth || tid < kItems, does_v = kBoth || tid >= kItems;   // the same for a wave
+  const int key_k = item / (HD / 32), g = item % (HD / 32);
+  const int quad = item & 15, piece = item >> 4;
+  const int P = bt.page_size;
+  const int64_t run = fp4_run_bytes(HD, P);
+  const int64_t page_bytes = run * bt.num_kv_heads;
+  const char* head = bt.pool + h * run;
+  // offsets inside 16 tokens' codes, and from there to the scales less those of the tokens (in a page's run: 16 tokens are 8 HD bytes of codes
+  // and HD / 2 of scales)
+  const uint32_t off_k = (key_k & 15) * (HD / 2) + g * 16, off_ks = uint32_t(P) * HD + (key_k & 15) * (HD / 32) + g;
+  const uint32_t off_v = uint32_t(P) * (HD / 2) + (quad & 3) * (2 * HD) + piece * 16;
+  const uint32_t off_vs = uint32_t(P) * HD + uint32_t(P) * (HD / 32) + (quad & 3) * (HD / 8) + (piece >> 2) * 4;
+  const int sub_k = key_k >> 4, sub_v = quad >> 2;
+
+  // the 16-token tiles of the keys in order, as in the decode kernel: the table is read a step ahead of the loads, these a step ahead of their use,
+  // without conditions (behind the last tile it is the last tile again, which is masked by its number)
+  const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
+  const int last_tile = len > 0 ? (len - 1) >> 4 : 0;
+  const int tiles_per_page = P / 16;
+  int next16 = 4 * k0, col = next16 / tiles_per_page, in_page = next16 - col * tiles_per_page;
+  int id[4], at[4];
+  auto next_tiles = [&]() {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      id[x] = table_entry(table + col);
+      at[x] = in_page;
+      const int more = next16 < last_tile ? 1 : 0;
+      next16 += more;
+      in_page += more;
+      const bool turn = in_page == tiles_per_page;
+      col += turn ? 1 : 0;
+      in_page = turn ? 0 : in_page;
+    }
+  };
+  struct Raw {
+    u32x4 k, v;
+    uint32_t ks, vs;
+    int bad;   // of the four tiles, a bit each
+  };
+  auto load = [&]() {
+    Raw x = {};
+    const char *rows_of[4], *scales_of[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const bool ok = uint32_t(id[y]) < uint32_t(bt.num_pages);
+      x.bad |= ok ? 0 : 1 << y;
+      const char* base = head + (ok ? id[y] : 0) * page_bytes;
+      rows_of[y] = base + at[y] * (8 * HD);
+      scales_of[y] = base + at[y] * (HD / 2);
+    }
+    if (does_k) {
+      x.k = *reinterpret_cast<const u32x4*>(pick(sub_k, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_k);
+      x.ks = *reinterpret_cast<const uint8_t*>(pick(sub_k, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_ks);
+    }
+    if (does_v) {
+      x.v = *reinterpret_cast<const u32x4*>(pick(sub_v, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_v);
+      x.vs = *reinterpret_cast<const uint32_t*>(pick(sub_v, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_vs);
+    }
+    return x;
+  };
+  auto stage = [&](Raw& x, int step, Fp4TileLds<HD>& lds) {
+    if (x.bad || (step + 1) * kTileKeys > len) {
+      // what lies in places that no token has been stored to must not be taken for numbers: weights of zero do not hide a NaN.  (Of K it does
+      // not matter, logits are masked.)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if ((x.bad >> sub_v & 1) || step * kTileKeys + quad * 4 + t >= len) x.v[t] = 0, x.vs = (x.vs & ~(255u << (8 * t))) | 127u << (8 * t);
+    }
+    if (does_k) {
+      const float s = __builtin_bit_cast(float, x.ks << 23);
+      u32x4* dst = reinterpret_cast<u32x4*>(lds.k + key_k * Fp4TileLds<HD>::kKeyStride + g * 32);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) dst[y] = u32x4{fp4_pair<0>(x.k[y], s), fp4_pair<1>(x.k[y], s), fp4_pair<2>(x.k[y], s), fp4_pair<3>(x.k[y], s)};
+    }
+    if (does_v) {
+      // tokens of 16 in the order of quads 0, 2, 1, 3
+      const int place = (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1);
+      _Float16* dst = lds.v + piece * 8 * Fp4TileLds<HD>::kChannelStride + place * 4;
+      const float s0 = fp4_scale(x.vs, 0), s1 = fp4_scale(x.vs, 1), s2 = fp4_scale(x.vs, 2), s3 = fp4_scale(x.vs, 3);
+      auto put = [&](auto byte_tag) {
+        constexpr int B = decltype(byte_tag)::value;
+        const uint32_t x0 = fp4_pair<B>(x.v[0], s0), x1 = fp4_pair<B>(x.v[1], s1), x2 = fp4_pair<B>(x.v[2], s2), x3 = fp4_pair<B>(x.v[3], s3);
+        *reinterpret_cast<u32x2*>(dst + (2 * B) * Fp4TileLds<HD>::kChannelStride) =
+            u32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100), __builtin_amdgcn_perm(x3, x2, 0x05040100)};
+        *reinterpret_cast<u32x2*>(dst + (2 * B + 1) * Fp4TileLds<HD>::kChannelStride) =
+            u32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302)};
+      };
+      put(std::integral_constant<int, 0>{});
+      put(std::integral_constant<int, 1>{});
+      put(std::integral_constant<int, 2>{});
+      put(std::integral_constant<int, 3>{});
+    }
+  };
+
+  // the queries
   h8 q[kSteps];
   float c = a.scale;
   {
     u32x4 raw[kSteps] = {};
     if (live) {
-      const char* src = a.q + (span.first + i) * a.stride_t + (h * a.rep + r - i * a.rep) * a.stride_h + half * 16;
+      const char* src = a.q + (first + i) * a.stride_t + (h * a.rep + r - i * a.rep) * a.stride_h + half * 16;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + s * 32);
     }
@@ -115,96 +218,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
     for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(h8, raw[s]);
   }
 
-  // a thread's pieces of every 64 keys: of K token key_k, channels 32 g .. 32 g + 31; of V a quad of tokens, eight channels
-  constexpr bool kBoth = kItems <= kThreads / 2 ? false : true;   // else the first half of the threads takes K, the second V
-  const int item = kBoth ? tid : tid % kItems;
-  const bool does_k = kBoth || tid < kItems, does_v = kBoth || tid >= kItems;
-  const int key_k = item / (HD / 32), g = item % (HD / 32);
-  const int quad = item & 15, piece = item >> 4;
-  const int P = bt.page_size;
-  const int64_t run = fp4_run_bytes(HD, P);
-  const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
-  auto page_of = [&](int tok) -> int { return tok < len ? table[tok / P] : -1; };
-  struct Raw {
-    u32x4 k, v;
-    uint32_t ks, vs;
-    int ok;
-  };
-  auto load = [&](int step, int id_k, int id_v) {
-    Raw x = {};
-    x.ks = 127;
-    x.vs = 0x7f7f7f7fu;
-    const int tk = step * kTileKeys + key_k, tv = step * kTileKeys + quad * 4;
-    if (does_k && uint32_t(id_k) < uint32_t(bt.num_pages) && tk < len) {
-      const char* base = bt.pool + (int64_t(id_k) * bt.num_kv_heads + h) * run;
-      const int at = tk % P;
-      x.k = *reinterpret_cast<const u32x4*>(base + at * (HD / 2) + g * 16);
-      x.ks = *reinterpret_cast<const uint8_t*>(base + P * HD + at * (HD / 32) + g);
-      x.ok = 1;
-    }
-    if (does_v && uint32_t(id_v) < uint32_t(bt.num_pages) && tv < len) {
-      const char* base = bt.pool + (int64_t(id_v) * bt.num_kv_heads + h) * run;
-      const int at = tv % P;
-      x.v = *reinterpret_cast<const u32x4*>(base + P * (HD / 2) + at * (HD / 2) + piece * 16);
-      x.vs = *reinterpret_cast<const uint32_t*>(base + P * HD + P * (HD / 32) + at * (HD / 32) + (piece >> 2) * 4);
-#pragma unroll
-      for (int t = 1; t < 4; ++t)
-        if (tv + t >= len) x.v[t] = 0, x.vs = (x.vs & ~(255u << (8 * t))) | 127u << (8 * t);
-    }
-    return x;
-  };
-  auto stage = [&](const Raw& x, int step) {
-    if (does_k) {
-      const float s = __builtin_bit_cast(float, x.ks << 23);
-      u32x4* dst = reinterpret_cast<u32x4*>(lds.k + key_k * Fp4TileLds<HD>::kKeyStride + g * 32);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) dst[y] = u32x4{fp4_pair<0>(x.k[y], s), fp4_pair<1>(x.k[y], s), fp4_pair<2>(x.k[y], s), fp4_pair<3>(x.k[y], s)};
-      // pages hold multiples of 16 tokens; keys behind the last one are masked by their number
-      if (g == 0 && key_k % 16 == 0) lds.ok[key_k / 16] = x.ok || step * kTileKeys + key_k >= len;
-    }
-    if (does_v) {
-      // tokens of 16 in the order of quads 0, 2, 1, 3
-      const int place = (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1);
-      _Float16* dst = lds.v + piece * 8 * Fp4TileLds<HD>::kChannelStride + place * 4;
-      const float s0 = fp4_scale(x.vs, 0), s1 = fp4_scale(x.vs, 1), s2 = fp4_scale(x.vs, 2), s3 = fp4_scale(x.vs, 3);
-      auto put = [&](auto byte_tag) {
-        constexpr int B = decltype(byte_tag)::value;
-        const uint32_t x0 = fp4_pair<B>(x.v[0], s0), x1 = fp4_pair<B>(x.v[1], s1), x2 = fp4_pair<B>(x.v[2], s2), x3 = fp4_pair<B>(x.v[3], s3);
-        *reinterpret_cast<u32x2*>(dst + (2 * B) * Fp4TileLds<HD>::kChannelStride) =
-            u32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100), __builtin_amdgcn_perm(x3, x2, 0x05040100)};
-        *reinterpret_cast<u32x2*>(dst + (2 * B + 1) * Fp4TileLds<HD>::kChannelStride) =
-            u32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302)};
-      };
-      put(std::integral_constant<int, 0>{});
-      put(std::integral_constant<int, 1>{});
-      put(std::integral_constant<int, 2>{});
-      put(std::integral_constant<int, 3>{});
-    }
-  };
-
   float m = kNoMax, lsum = 0.f;
   f32x16 o[kChannelTiles];
 #pragma unroll
   for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] = f32x16{};
 
-  int id_k = -1, id_v = -1;
-  Raw next = {};
-  if (k0 < k1) {
-    next = load(k0, page_of(k0 * kTileKeys + key_k), page_of(k0 * kTileKeys + quad * 4));
-    id_k = page_of((k0 + 1) * kTileKeys + key_k);
-    id_v = page_of((k0 + 1) * kTileKeys + quad * 4);
-  }
-  for (int step = k0; step < k1; ++step) {
-    __syncthreads();   // the step before has been read
-    stage(next, step);
-    if (step + 1 < k1) {
-      next = load(step + 1, id_k, id_v);
-      id_k = page_of((step + 2) * kTileKeys + key_k);
-      id_v = page_of((step + 2) * kTileKeys + quad * 4);
-    }
-    __syncthreads();
+  auto compute = [&](int step, int bad, const Fp4TileLds<HD>& lds) {
     const int tok0 = step * kTileKeys;
-    if (tok0 >= wave_most) continue;   // (the whole wave)
     f32x16 s[2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -214,15 +234,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
       for (int st = 0; st < kSteps; ++st)
         s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + st * 16), q[st], s[tt], 0, 0, 0);
     }
-    const int ok0 = lds.ok[0], ok1 = lds.ok[1], ok2 = lds.ok[2], ok3 = lds.ok[3];
-    if (tok0 + kTileKeys > wave_free || !(ok0 && ok1 && ok2 && ok3)) {
+    if (tok0 + kTileKeys > wave_free || bad) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const int tok = tok0 + tt * 32 + 8 * (x >> 2) + 4 * half + (x & 3);
-          const int ok = tt == 0 ? (x < 8 ? ok0 : ok1) : (x < 8 ? ok2 : ok3);
-          s[tt][x] = ok && tok < lim ? s[tt][x] : -__builtin_inff();
+          s[tt][x] = !(bad >> (2 * tt + (x >> 3)) & 1) && tok < lim ? s[tt][x] : -__builtin_inff();
         }
     }
     float top = s[0][0];
@@ -253,11 +271,33 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
       for (int u = 0; u < 4; ++u)
         o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + u * 16), p[u], o[ct], 0, 0, 0);
     }
+  };
+
+  // Two buffers: while the waves work on the keys in one, they put the next ones into the other; one barrier a step.
+  if (k0 < k1) {
+    next_tiles();
+    Raw now = load();
+    next_tiles();
+    int bad = now.bad;
+    stage(now, k0, buffers[0]);
+    now = load();
+    next_tiles();
+    __syncthreads();
+    for (int step = k0; step < k1; ++step) {
+      const int at_buffer = (step - k0) & 1;
+      const int bad_next = now.bad;
+      if (step + 1 < k1) stage(now, step + 1, buffers[at_buffer ^ 1]);
+      now = load();
+      next_tiles();
+      if (step * kTileKeys < wave_most) compute(step, bad, buffers[at_buffer]);
+      bad = bad_next;
+      __syncthreads();
+    }
   }
 
   lsum += __shfl_xor(lsum, 32);
   if (!live) return;
-  const int64_t row = int64_t(span.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
+  const int64_t row = int64_t(first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
   if (a.splits == 1) {
     const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
     char* dst = a.out + row * (2 * HD);
