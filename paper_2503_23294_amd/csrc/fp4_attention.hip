@@ -141,7 +141,7 @@ namespace {
 // What a call launches, from what the host knows: bounds, no lengths.
 struct Split {
   bool decode, tiles;
-  int rows, row_tiles, workers, tile_blocks, splits;
+  int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
   size_t prefix_bytes, part_rows, tile_rows, bytes;
 };
 
@@ -172,7 +172,10 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   s.splits = 1;
   if (s.tiles) {
     const int64_t seqs = c->pages.num_seqs;
-    s.tile_blocks = int(uniform ? seqs * ((most_rows + kTileRows - 1) / kTileRows) : total * rep / kTileRows + (seqs < total ? seqs : total));
+    // Eight waves share what it takes to bring the keys into LDS where that leaves a workgroup for every compute unit, four otherwise.
+    s.tile_waves = total * rep * c->num_kv_heads >= 256 * 256 && most_rows > 128 ? 8 : 4;
+    const int64_t tile_rows = 32 * s.tile_waves;
+    s.tile_blocks = int(uniform ? seqs * ((most_rows + tile_rows - 1) / tile_rows) : total * rep / tile_rows + (seqs < total ? seqs : total));
     const int64_t have = int64_t(s.tile_blocks) * c->num_kv_heads;
     int64_t splits = (512 + have - 1) / have;
     const int64_t longest = (max_len + 511) / 512;
@@ -258,7 +261,8 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     e = launch_lds(kernel, dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }
   if (e == hipSuccess && s.tiles)
-    e = launch(hd == 128 ? fp4_tile_kernel<128> : fp4_tile_kernel<64>, dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * kTileWaves), st, a);
+    e = launch(s.tile_waves == 8 ? (hd == 128 ? fp4_tile_kernel<128, 8> : fp4_tile_kernel<64, 8>) : (hd == 128 ? fp4_tile_kernel<128, 4> : fp4_tile_kernel<64, 4>),
+               dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * s.tile_waves), st, a);
   if (e == hipSuccess && s.decode) {
     const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;

@@ -10,19 +10,22 @@
 
 namespace cocktail {
 
-constexpr int kTileWaves = 4;
-constexpr int kTileRows = 32 * kTileWaves;
 
+// K in chunks of 32 keys, a ring of five: the two that are read in a step, the one before them that a slower wave may still read, and the
+// two that are written.  V of 64 keys, twice.
+constexpr int kChunk = 32, kRing = 5;
+constexpr float kSumLimit = 16384.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then
 template <int HD>
 struct Fp4TileLds {
   static constexpr int kKeyStride = HD + 8;          // halves; rows shift by four banks
   static constexpr int kChannelStride = kTileKeys + 8;
-  _Float16 k[kTileKeys * kKeyStride];
-  _Float16 v[HD * kChannelStride];
+  _Float16 k[kRing][kChunk * kKeyStride];
+  _Float16 v[2][HD * kChannelStride];
 };
 
+template <int WAVES>
 __device__ __forceinline__ int tile_count(const Fp4Attention& a, const Fp4Span& s) {
-  return s.count * a.rep > a.decode_rows ? (s.count * a.rep + kTileRows - 1) / kTileRows : 0;
+  return s.count * a.rep > a.decode_rows ? (s.count * a.rep + 32 * WAVES - 1) / (32 * WAVES) : 0;
 }
 
 // One of four values that are the same in all lanes, by the lane's own number.
@@ -33,13 +36,12 @@ __device__ __forceinline__ const char* pick(int k, const char* a, const char* b,
   return reinterpret_cast<const char*>(uint64_t((k & 2) ? hi23 : hi01) << 32 | ((k & 2) ? lo23 : lo01));
 }
 
-template <int HD>
-__global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attention a) {
-  constexpr int kThreads = 64 * kTileWaves;
+template <int HD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a) {
+  constexpr int kThreads = 64 * WAVES, kTileRows = 32 * WAVES;
   constexpr int kSteps = HD / 16, kChannelTiles = HD / 32;
-  constexpr int kItems = 2 * HD;                     // 16-byte pieces of 64 keys, of K and of V each
-  __shared__ Fp4TileLds<HD> buffers[2];
-  __shared__ int32_t found[4], scratch[kTileWaves + 1];
+  __shared__ Fp4TileLds<HD> lds;
+  __shared__ int32_t found[4], scratch[WAVES];
   const Fp4Batch& bt = a.batch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -52,13 +54,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   for (int base = 0; base < bt.num_seqs; base += kThreads) {
     const int b = base + tid;
     const Fp4Span s = b < bt.num_seqs ? fp4_span(bt, b) : Fp4Span{0, 0};
-    const int v = tile_count(a, s);
+    const int v = tile_count<WAVES>(a, s);
     const int x = wave_prefix(v);
     __syncthreads();
     if (lane == 63) scratch[wave] = x;
     __syncthreads();
     int before = run_tiles;
-    for (int w = 0; w < kTileWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w < wave) before += scratch[w];
       run_tiles += scratch[w];
     }
@@ -88,29 +90,26 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
   const int r = r0 + wave * 32 + row_lane, i = r / a.rep;
   const bool live = r < rows;
   const int lim = live ? len - n + i + 1 : 0;
-  const int wave_first = r0 + wave * 32, wave_last = wave_first + 31 < rows ? wave_first + 31 : rows - 1;
-  const int wave_most = wave_first < rows ? len - n + wave_last / a.rep + 1 : 0;   // beyond: nothing to do for this wave
+  const int wave_first = r0 + wave * 32;
   const int wave_free = wave_first + 31 < rows ? len - n + wave_first / a.rep + 1 : 0;   // below: no masking
 
-  // a thread's pieces of every 64 keys: of K token key_k, channels 32 g .. 32 g + 31; of V a quad of tokens, eight channels
-  constexpr bool kBoth = kItems > kThreads / 2;      // else half of the threads takes K, the other half V
-  const int item = kBoth ? tid : tid % kItems;
-  const bool does_k = kBoth || tid < kItems, does_v = kBoth || tid >= kItems;   // the same for a wave
-  const int key_k = item / (HD / 32), g = item % (HD / 32);
-  const int quad = item & 15, piece = item >> 4;
+  // A thread's pieces of every 64 keys: kPieces words (of eight channels) of a key of K, and as many pairs of channels of a quad of tokens of V.
+  constexpr int kPieces = HD * 8 / kThreads;
+  constexpr int kParts = HD / 8 / kPieces;           // threads that share a key
+  const int key = tid / kParts, part = tid % kParts, quad = tid & 15, v_part = tid >> 4;
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
   const int64_t page_bytes = run * bt.num_kv_heads;
   const char* head = bt.pool + h * run;
-  // offsets inside 16 tokens' codes, and from there to the scales less those of the tokens (in a page's run: 16 tokens are 8 HD bytes of codes
-  // and HD / 2 of scales)
-  const uint32_t off_k = (key_k & 15) * (HD / 2) + g * 16, off_ks = uint32_t(P) * HD + (key_k & 15) * (HD / 32) + g;
-  const uint32_t off_v = uint32_t(P) * (HD / 2) + (quad & 3) * (2 * HD) + piece * 16;
-  const uint32_t off_vs = uint32_t(P) * HD + uint32_t(P) * (HD / 32) + (quad & 3) * (HD / 8) + (piece >> 2) * 4;
-  const int sub_k = key_k >> 4, sub_v = quad >> 2;
+  // offsets inside 16 tokens (in a page's run: 8 HD bytes of codes and HD / 2 of scales)
+  const uint32_t off_k = (key & 15) * (HD / 2) + part * (4 * kPieces), off_ks = uint32_t(P) * HD + (key & 15) * (HD / 32) + (part * kPieces >> 2);
+  const uint32_t off_v = uint32_t(P) * (HD / 2) + (quad & 3) * (2 * HD) + (v_part * kPieces >> 2) * 16;
+  const uint32_t off_vs = uint32_t(P) * HD + uint32_t(P) * (HD / 32) + (quad & 3) * (HD / 8) + (v_part * kPieces >> 4) * 4;
+  const int v_shift = kPieces == 4 ? 0 : 8 * (v_part * kPieces & 3);   // to the thread's bytes of a piece
+  const int sub_k = key >> 4, sub_v = quad >> 2;
 
-  // the 16-token tiles of the keys in order, as in the decode kernel: the table is read a step ahead of the loads, these a step ahead of their use,
-  // without conditions (behind the last tile it is the last tile again, which is masked by its number)
+  // The 16-token tiles of the keys in order, as in the decode kernel: the table is read ahead of the loads, these ahead of their use, without
+  // conditions (behind the last tile it is the last tile again, which is masked by its number).  V of a step is loaded a step after its K.
   const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
   const int last_tile = len > 0 ? (len - 1) >> 4 : 0;
   const int tiles_per_page = P / 16;
@@ -129,63 +128,75 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
       in_page = turn ? 0 : in_page;
     }
   };
-  struct Raw {
-    u32x4 k, v;
-    uint32_t ks, vs;
-    int bad;   // of the four tiles, a bit each
-  };
-  auto load = [&]() {
-    Raw x = {};
+  u32x4 raw_k, raw_v;
+  uint32_t raw_ks, raw_vs;
+  const char *v_rows, *v_scales;   // of the step whose K was loaded last
+  int bad_k;                       // its tiles that lie on no page, a bit each
+  auto load_k = [&]() {
     const char *rows_of[4], *scales_of[4];
+    bad_k = 0;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
       const bool ok = uint32_t(id[y]) < uint32_t(bt.num_pages);
-      x.bad |= ok ? 0 : 1 << y;
+      bad_k |= ok ? 0 : 1 << y;
       const char* base = head + (ok ? id[y] : 0) * page_bytes;
       rows_of[y] = base + at[y] * (8 * HD);
       scales_of[y] = base + at[y] * (HD / 2);
     }
-    if (does_k) {
-      x.k = *reinterpret_cast<const u32x4*>(pick(sub_k, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_k);
-      x.ks = *reinterpret_cast<const uint8_t*>(pick(sub_k, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_ks);
+    const char* rows_k = pick(sub_k, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_k;
+    if constexpr (kPieces == 4) {
+      raw_k = *reinterpret_cast<const u32x4*>(rows_k);
+    } else if constexpr (kPieces == 2) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(rows_k);
+      raw_k = u32x4{x[0], x[1], 0, 0};
+    } else {
+      raw_k = u32x4{*reinterpret_cast<const uint32_t*>(rows_k), 0, 0, 0};
     }
-    if (does_v) {
-      x.v = *reinterpret_cast<const u32x4*>(pick(sub_v, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_v);
-      x.vs = *reinterpret_cast<const uint32_t*>(pick(sub_v, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_vs);
-    }
-    return x;
+    raw_ks = *reinterpret_cast<const uint8_t*>(pick(sub_k, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_ks);
+    v_rows = pick(sub_v, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_v;
+    v_scales = pick(sub_v, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_vs;
   };
-  auto stage = [&](Raw& x, int step, Fp4TileLds<HD>& lds) {
-    if (x.bad || (step + 1) * kTileKeys > len) {
-      // what lies in places that no token has been stored to must not be taken for numbers: weights of zero do not hide a NaN.  (Of K it does
-      // not matter, logits are masked.)
+  auto load_v = [&]() {
+    raw_v = *reinterpret_cast<const u32x4*>(v_rows);
+    raw_vs = *reinterpret_cast<const uint32_t*>(v_scales);
+  };
+  // What lies in places that no token has been stored to must not be taken for numbers: weights of zero do not hide a NaN.  (Of K it does not
+  // matter, logits are masked.)
+  auto clean_v = [&](int step, int bad) {
+    if (!bad && (step + 1) * kTileKeys <= len) return;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if ((x.bad >> sub_v & 1) || step * kTileKeys + quad * 4 + t >= len) x.v[t] = 0, x.vs = (x.vs & ~(255u << (8 * t))) | 127u << (8 * t);
-    }
-    if (does_k) {
-      const float s = __builtin_bit_cast(float, x.ks << 23);
-      u32x4* dst = reinterpret_cast<u32x4*>(lds.k + key_k * Fp4TileLds<HD>::kKeyStride + g * 32);
+    for (int t = 0; t < 4; ++t)
+      if ((bad >> sub_v & 1) || step * kTileKeys + quad * 4 + t >= len) raw_v[t] = 0, raw_vs = (raw_vs & ~(255u << (8 * t))) | 127u << (8 * t);
+  };
+  auto stage_k = [&](int piece, int slot) {
+    const float s = __builtin_bit_cast(float, raw_ks << 23);
+    u32x4* dst = reinterpret_cast<u32x4*>(lds.k[slot] + (key & 31) * Fp4TileLds<HD>::kKeyStride + part * (8 * kPieces));
+    const uint32_t w = raw_k[piece];
+    dst[piece] = u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
+  };
+  auto stage_v = [&](auto byte_tag, int buffer) {
+    constexpr int B = decltype(byte_tag)::value;
+    // tokens of 16 in the order of quads 0, 2, 1, 3
+    const int place = (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1);
+    _Float16* dst = lds.v[buffer] + v_part * (2 * kPieces) * Fp4TileLds<HD>::kChannelStride + place * 4;
+    const uint32_t x0 = fp4_pair<B>(raw_v[0] >> v_shift, fp4_scale(raw_vs, 0)), x1 = fp4_pair<B>(raw_v[1] >> v_shift, fp4_scale(raw_vs, 1));
+    const uint32_t x2 = fp4_pair<B>(raw_v[2] >> v_shift, fp4_scale(raw_vs, 2)), x3 = fp4_pair<B>(raw_v[3] >> v_shift, fp4_scale(raw_vs, 3));
+    *reinterpret_cast<u32x2*>(dst + (2 * B) * Fp4TileLds<HD>::kChannelStride) = u32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100), __builtin_amdgcn_perm(x3, x2, 0x05040100)};
+    *reinterpret_cast<u32x2*>(dst + (2 * B + 1) * Fp4TileLds<HD>::kChannelStride) =
+        u32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302)};
+  };
+  auto stage_all_k = [&](int slot) {
 #pragma unroll
-      for (int y = 0; y < 4; ++y) dst[y] = u32x4{fp4_pair<0>(x.k[y], s), fp4_pair<1>(x.k[y], s), fp4_pair<2>(x.k[y], s), fp4_pair<3>(x.k[y], s)};
+    for (int x = 0; x < kPieces; ++x) stage_k(x, slot);
+  };
+  auto stage_v_piece = [&](int piece, int buffer) {
+    if (piece == 0) stage_v(std::integral_constant<int, 0>{}, buffer);
+    if constexpr (kPieces > 1) {
+      if (piece == 1) stage_v(std::integral_constant<int, 1>{}, buffer);
     }
-    if (does_v) {
-      // tokens of 16 in the order of quads 0, 2, 1, 3
-      const int place = (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1);
-      _Float16* dst = lds.v + piece * 8 * Fp4TileLds<HD>::kChannelStride + place * 4;
-      const float s0 = fp4_scale(x.vs, 0), s1 = fp4_scale(x.vs, 1), s2 = fp4_scale(x.vs, 2), s3 = fp4_scale(x.vs, 3);
-      auto put = [&](auto byte_tag) {
-        constexpr int B = decltype(byte_tag)::value;
-        const uint32_t x0 = fp4_pair<B>(x.v[0], s0), x1 = fp4_pair<B>(x.v[1], s1), x2 = fp4_pair<B>(x.v[2], s2), x3 = fp4_pair<B>(x.v[3], s3);
-        *reinterpret_cast<u32x2*>(dst + (2 * B) * Fp4TileLds<HD>::kChannelStride) =
-            u32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100), __builtin_amdgcn_perm(x3, x2, 0x05040100)};
-        *reinterpret_cast<u32x2*>(dst + (2 * B + 1) * Fp4TileLds<HD>::kChannelStride) =
-            u32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302)};
-      };
-      put(std::integral_constant<int, 0>{});
-      put(std::integral_constant<int, 1>{});
-      put(std::integral_constant<int, 2>{});
-      put(std::integral_constant<int, 3>{});
+    if constexpr (kPieces > 2) {
+      if (piece == 2) stage_v(std::integral_constant<int, 2>{}, buffer);
+      if (piece == 3) stage_v(std::integral_constant<int, 3>{}, buffer);
     }
   };
 
@@ -223,74 +234,137 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void fp4_tile_kernel(Fp4Attenti
 #pragma unroll
   for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] = f32x16{};
 
-  auto compute = [&](int step, int bad, const Fp4TileLds<HD>& lds) {
-    const int tok0 = step * kTileKeys;
-    f32x16 s[2];
+  // Logits of 32 keys that a row does not see.
+  auto mask = [&](f32x16& s, int tok0, int bad) {   // bad: of the two 16-token tiles
+    if (tok0 + kChunk > wave_free || bad) {
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      s[tt] = f32x16{};
-      const _Float16* src = lds.k + (tt * 32 + row_lane) * Fp4TileLds<HD>::kKeyStride + half * 8;
-#pragma unroll
-      for (int st = 0; st < kSteps; ++st)
-        s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + st * 16), q[st], s[tt], 0, 0, 0);
+      for (int x = 0; x < 16; ++x) {
+        const int tok = tok0 + 8 * (x >> 2) + 4 * half + (x & 3);
+        s[x] = !(bad >> (x >> 3) & 1) && tok < lim ? s[x] : -__builtin_inff();
+      }
     }
-    if (tok0 + kTileKeys > wave_free || bad) {
+  };
+  // The reference maximum of a row whose logits exceed it by too much becomes the largest of them.
+  auto raise = [&](const f32x16& s) {
+    float top = s[0];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int tok = tok0 + tt * 32 + 8 * (x >> 2) + 4 * half + (x & 3);
-          s[tt][x] = !(bad >> (2 * tt + (x >> 3)) & 1) && tok < lim ? s[tt][x] : -__builtin_inff();
-        }
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int x = 1; x < 32; ++x) top = fmaxf(top, s[x >> 4][x & 15]);
+    for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
     top *= c;
-    if (__any(top > m + kMaxSlack)) {
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float raised = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - raised);
-      m = raised;
-      lsum *= alpha;
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float raised = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - raised);
+    m = raised;
+    lsum *= alpha;
 #pragma unroll
-      for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] *= alpha;
+    for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] *= alpha;
+  };
+
+  // One half of a step: logits of the next 32 keys (`ahead`, from chunk `slot`), next to the weights of these (`s`); then these' products with V
+  // (keys 32 * sub ... of `v`), next to the putting away of what has been loaded (`put`, kPieces times).  The order is written down
+  // and kept: a product every few other instructions, its operands read four products before.
+  auto half_step = [&](const f32x16& s, f32x16& ahead, const _Float16* k, const _Float16* v, auto&& put) {
+    constexpr int kLead = 4;
+    constexpr int kProductsV = 2 * kChannelTiles;
+    constexpr int kOrder = 0x4 | 0x10 | 0x20 | 0x40;   // scalar instructions and loads may move
+    const _Float16* ksrc = k + row_lane * Fp4TileLds<HD>::kKeyStride + half * 8;
+    const _Float16* vsrc = v + row_lane * Fp4TileLds<HD>::kChannelStride + half * 8;
+    h8 kf[kSteps], vf[kProductsV];
+    auto read_k = [&](int x) { kf[x] = *reinterpret_cast<const h8*>(ksrc + x * 16); };
+    auto read_v = [&](int x) { vf[x] = *reinterpret_cast<const h8*>(vsrc + (x % kChannelTiles) * 32 * Fp4TileLds<HD>::kChannelStride + (x / kChannelTiles) * 16); };
+    ahead = f32x16{};
+    uint32_t w[8];
+    float sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < kLead; ++x) read_k(x);
+    __builtin_amdgcn_sched_barrier(kOrder);
+    constexpr int kPer = 16 / kSteps;   // weights per product
+#pragma unroll
+    for (int x = 0; x < kSteps; ++x) {
+      if (x + kLead < kSteps) read_k(x + kLead);
+      else if (x + kLead - kSteps < kProductsV) read_v(x + kLead - kSteps);
+      ahead = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x], q[x], ahead, 0, 0, 0);
+#pragma unroll
+      for (int y = x * kPer; y < (x + 1) * kPer; y += 2) {
+        const float a0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -m)), a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y + 1], c, -m));
+        sum += a0 + a1;
+        w[y / 2] = pack_halves(a0, a1);
+      }
+      __builtin_amdgcn_sched_barrier(kOrder);
     }
-    h8 p[4];
+    // Whether the reference is too small shows in the sum of the weights: then each of them was too large at most by that (the products have not
+    // taken place, and the weights are computed again); no maximum is looked for before it is needed.
+    if (__any(sum > kSumLimit)) {
+      raise(s);
+      sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float w8[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) w8[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][(u & 1) * 8 + x], c, -m));
-      lsum += ((w8[0] + w8[1]) + (w8[2] + w8[3])) + ((w8[4] + w8[5]) + (w8[6] + w8[7]));
-      p[u] = __builtin_bit_cast(h8, u32x4{pack_halves(w8[0], w8[1]), pack_halves(w8[2], w8[3]), pack_halves(w8[4], w8[5]), pack_halves(w8[6], w8[7])});
+      for (int y = 0; y < 16; y += 2) {
+        const float a0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -m)), a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y + 1], c, -m));
+        sum += a0 + a1;
+        w[y / 2] = pack_halves(a0, a1);
+      }
     }
+    lsum += sum;
+    const h8 p[2] = {__builtin_bit_cast(h8, u32x4{w[0], w[1], w[2], w[3]}), __builtin_bit_cast(h8, u32x4{w[4], w[5], w[6], w[7]})};
 #pragma unroll
-    for (int ct = 0; ct < kChannelTiles; ++ct) {
-      const _Float16* src = lds.v + (ct * 32 + row_lane) * Fp4TileLds<HD>::kChannelStride + half * 8;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + u * 16), p[u], o[ct], 0, 0, 0);
+    for (int x = 0; x < kProductsV; ++x) {
+      if (x + kLead < kProductsV) read_v(x + kLead);
+      o[x % kChannelTiles] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[x], p[x / kChannelTiles], o[x % kChannelTiles], 0, 0, 0);
+      if (x % 2 == 0) put(x / 2);
+      __builtin_amdgcn_sched_barrier(kOrder);
     }
   };
 
-  // Two buffers: while the waves work on the keys in one, they put the next ones into the other; one barrier a step.
   if (k0 < k1) {
+    // K of the first two steps and V of the first one into LDS, K of the third and V of the second on their way
+    const int slot_of = key >> 5;   // which of a step's two chunks the thread's key is in
     next_tiles();
-    Raw now = load();
+    load_k();
     next_tiles();
-    int bad = now.bad;
-    stage(now, k0, buffers[0]);
-    now = load();
+    load_v();
+    int bad0 = bad_k, bad1;         // of this step and of the next
+    clean_v(k0, bad0);
+    stage_all_k(slot_of);
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) stage_v_piece(x, 0);
+    load_k();
+    next_tiles();
+    load_v();
+    bad1 = bad_k;
+    stage_all_k(2 + slot_of);
+    load_k();
     next_tiles();
     __syncthreads();
+    const bool idle = wave_first >= rows;
+    f32x16 s0, s1;
+    if (!idle) {
+      s0 = f32x16{};
+      const _Float16* src = lds.k[0] + row_lane * Fp4TileLds<HD>::kKeyStride + half * 8;
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + x * 16), q[x], s0, 0, 0, 0);
+      mask(s0, k0 * kTileKeys, bad0 & 3);
+    }
+    int chunk = 0;                  // slot of this step's first chunk
     for (int step = k0; step < k1; ++step) {
-      const int at_buffer = (step - k0) & 1;
-      const int bad_next = now.bad;
-      if (step + 1 < k1) stage(now, step + 1, buffers[at_buffer ^ 1]);
-      now = load();
+      const int buffer = (step - k0) & 1;
+      const int slot1 = chunk + 1 < kRing ? chunk + 1 : chunk + 1 - kRing, slot2 = chunk + 2 < kRing ? chunk + 2 : chunk + 2 - kRing;
+      const int slot4 = chunk + 4 < kRing ? chunk + 4 : chunk + 4 - kRing, slot5 = chunk;
+      const int write_slot = slot_of ? slot5 : slot4;
+      clean_v(step + 1, bad1);
+      if (!idle) {
+        half_step(s0, s1, lds.k[slot1], lds.v[buffer], [&](int x) { if (x < kPieces) stage_v_piece(x, buffer ^ 1); });
+        mask(s1, step * kTileKeys + kChunk, bad0 >> 2);
+        half_step(s1, s0, lds.k[slot2], lds.v[buffer] + kChunk, [&](int x) { if (x < kPieces) stage_k(x, write_slot); });
+      } else {
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) stage_v_piece(x, buffer ^ 1);
+        stage_all_k(write_slot);
+      }
+      bad0 = bad1;
+      bad1 = bad_k;
+      load_v();
+      load_k();
       next_tiles();
-      if (step * kTileKeys < wave_most) compute(step, bad, buffers[at_buffer]);
-      bad = bad_next;
+      if (!idle && step + 1 < k1) mask(s0, (step + 1) * kTileKeys, bad0 & 3);
+      chunk = slot2;
       __syncthreads();
     }
   }
