@@ -172,15 +172,22 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   s.splits = 1;
   if (s.tiles) {
     const int64_t seqs = c->pages.num_seqs;
-    // Eight waves share what it takes to bring the keys into LDS where that leaves a workgroup for every compute unit, four otherwise.
-    s.tile_waves = total * rep * c->num_kv_heads >= 256 * 256 && most_rows > 128 ? 8 : 4;
+    // Eight waves share what it takes to bring the keys into LDS where that leaves a workgroup for every compute unit and the rows see about as
+    // many keys each (2048 tokens of 4 x 8 heads behind 30K: four waves 1180 us, eight 1135); else four, whose smaller pieces
+    // leave less to wait for at the end (whole prompts of 8190 and 4095 tokens, 32 heads: 778 us, and 797 with eight).
+    s.tile_waves = total * rep * c->num_kv_heads >= 256 * 256 && most_rows > 128 && max_len >= 2 * max_new ? 8 : 4;
     const int64_t tile_rows = 32 * s.tile_waves;
     s.tile_blocks = int(uniform ? seqs * ((most_rows + tile_rows - 1) / tile_rows) : total * rep / tile_rows + (seqs < total ? seqs : total));
     const int64_t have = int64_t(s.tile_blocks) * c->num_kv_heads;
-    int64_t splits = (512 + have - 1) / have;
+    // Parts only where there are fewer workgroups than run at a time (one on a compute unit with eight waves, two with four): as many as make
+    // the last round of them fullest, each of 512 keys at least.
+    const int64_t at_once = s.tile_waves == 8 ? 256 : 512;
     const int64_t longest = (max_len + 511) / 512;
-    splits = splits > longest ? longest : splits;
-    s.splits = int(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+    double best = 0;
+    for (int64_t parts = 1; parts <= 64 && parts <= longest && (parts == 1 || have * (parts - 1) < at_once); ++parts) {
+      const double time = double((have * parts + at_once - 1) / at_once) / double(parts) + 0.01 * double(parts);
+      if (parts == 1 || time < best) best = time, s.splits = int(parts);
+    }
     if (s.splits > 1) s.tile_rows = size_t(s.splits) * size_t(total) * c->num_kv_heads * rep;
   }
   s.bytes = s.prefix_bytes + (s.part_rows + s.tile_rows) * (c->head_dim + 4) * sizeof(float) + 64;
