@@ -29,7 +29,7 @@ struct Fp4Attention {
   int32_t workers;              // waves of the decode kernel
   int32_t decode_rows;          // sequences with at most so many rows are the decode kernel's, the others the tile kernel's
   int32_t splits;               // parts that the tile kernel cuts the keys of a row into
-  int32_t* prefix;              // workspace: units of the sequences before b [num_seqs + 1]
+  int32_t* prefix;              // workspace: cost of the sequences before b, for one kv head [num_seqs + 1]
   float* part_ml;               // (m, l, l unrounded) of the partial states
   float* part_o;                // their weighted sums
   float* tile_ml;
@@ -46,10 +46,17 @@ __device__ __forceinline__ Fp4Seq decode_seq(const Fp4Attention& a, int b) {
   return {s.first, s.count * a.rep <= a.decode_rows ? s.count : 0, fp4_len(a.batch, b)};
 }
 
+// Operands of 16 query rows that a sequence needs in the decode kernel, its units of keys, and what they cost: a unit takes about as long as it has
+// operands (8 x 16K: 0.7, 1.2, 1.9 and 2.4 us with one to four).
+__device__ __forceinline__ int decode_operands(const Fp4Attention& a, const Fp4Seq& s) { return (s.n * a.rep + 15) >> 4; }
 __device__ __forceinline__ int decode_units(const Fp4Seq& s) { return s.n > 0 ? (s.len + kUnit - 1) / kUnit : 0; }
+__device__ __forceinline__ int decode_cost(const Fp4Attention& a, const Fp4Seq& s) { return decode_units(s) * decode_operands(a, s); }
 
-// Units of a wave of the decode kernel.
-__device__ __forceinline__ uint32_t unit_share(uint32_t units, int workers) { return (units + uint32_t(workers) - 1) / uint32_t(workers); }
+// A wave's share of the cost: not less than a unit's, so that a segment has units in every share that lies between its first and its last.
+__device__ __forceinline__ uint32_t cost_share(uint32_t cost, int workers) {
+  const uint32_t n = (cost + uint32_t(workers) - 1) / uint32_t(workers);
+  return n < 4 ? 4 : n;
+}
 
 __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
   const _Float16 a = _Float16(lo), b = _Float16(hi);

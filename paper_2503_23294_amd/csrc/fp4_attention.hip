@@ -74,16 +74,17 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode
   const uint32_t hq = number % heads, bi = number / heads;
   const int b = bi / uint32_t(most_new), i = bi % uint32_t(most_new);
   if (b >= bt.num_seqs) return;   // (kRows > 1 only, where nobody waits for anybody)
-  const int before = a.prefix[b], per_head = a.prefix[b + 1] - before;
-  const uint32_t units = uint32_t(a.prefix[bt.num_seqs]) * uint32_t(bt.num_kv_heads);
+  const uint32_t before = a.prefix[b], total = a.prefix[bt.num_seqs];
   const Fp4Seq s = decode_seq(a, b);
   if (i >= s.n) return;
   const uint32_t h = hq / uint32_t(a.rep);
   const int64_t row = int64_t(s.first + i) * heads + hq;
+  const uint32_t units = decode_units(s), per_unit = decode_operands(a, s);
   Merged<HD> r = {};
-  if (per_head > 0) {
-    const uint32_t share = unit_share(units, a.workers);
-    const uint32_t u0 = uint32_t(before) * uint32_t(bt.num_kv_heads) + h * uint32_t(per_head), u1 = u0 + uint32_t(per_head) - 1;
+  if (units > 0) {
+    // the waves that the segment's first and last unit belong to
+    const uint32_t share = cost_share(total * uint32_t(bt.num_kv_heads), a.workers);
+    const uint32_t u0 = before * uint32_t(bt.num_kv_heads) + h * units * per_unit, u1 = u0 + (units - 1) * per_unit;
     const uint32_t w0 = u0 / share, w1 = u1 / share;
     if (w0 == w1) return;   // its wave has finished it
     const int in_state = i * a.rep + int(hq - h * a.rep);
@@ -203,7 +204,7 @@ int check_attention(const cocktail_fp4_cache* c, int32_t num_q_heads, int64_t to
   if (total < 0 || total * num_q_heads > (int64_t(1) << 30)) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
   if (total && (max_new < 1 || max_new > total)) return fail(COCKTAIL_EINVAL, "max_new %d is not in 1 .. total (%lld)", max_new, (long long)total);
   const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
-  if (double(c->pages.num_seqs) * ((capacity + kUnit - 1) / kUnit) * c->num_kv_heads > 4.29e9)   // (numbers of units are 32 bits wide)
+  if (double(c->pages.num_seqs) * ((capacity + kUnit - 1) / kUnit) * c->num_kv_heads > 1.07e9)   // (costs, up to four times that, are 32 bits wide)
     return fail(COCKTAIL_EINVAL, "%d sequences of up to %lld tokens are too many for one call", c->pages.num_seqs, (long long)capacity);
   return COCKTAIL_OK;
 }

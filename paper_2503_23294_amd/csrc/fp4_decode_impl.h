@@ -1,8 +1,8 @@
 // Decode kernel of cocktail_fp4_attention: up to 32 query rows (new tokens x query heads of a kv head) per (sequence, kv head).
 //
 // Bound by memory: a key costs 2 * 17/32 D bytes and 4 D * rows operations.  What it takes to read at the rate of the memory:
-//  * Work is cut by tokens, not by sequences: the units of 32 tokens of all (sequence, kv head) segments are numbered, and every wave takes an
-//    equal share of consecutive ones, whatever the lengths are.  The numbering is made on the device from seq_lens, so that lengths can change
+//  * Work is cut by tokens, not by sequences: the units of 32 tokens of all (sequence, kv head) segments lie one behind the other, each as long as it
+//    costs, and every wave takes those that begin in its share of that line, whatever the lengths are.  The numbering is made on the device from seq_lens, so that lengths can change
 //    under a captured graph.  A segment inside one share is finished by its wave, the others leave a partial state per wave.
 //  * A lane's operands are whole pieces of memory: of K, 16 tokens x D/4 channels (lane = token t, quarter j) are one operand of a 16x16x32
 //    product S^T = K Q^T, the channels being taken in an order of the product's own (the same for Q); of V, lane (c, j) has channels
@@ -27,25 +27,25 @@ struct Fp4Tile {
   int ok;           // wave-uniform: the page is one
 };
 
-// Which units are whose: with up to 64 sequences every wave has them in its lanes, otherwise the workgroup has the units before every sequence
-// in LDS (pre[0 .. num_seqs]).
-struct Fp4Units {
+// What lies where on the line of costs: with up to 64 sequences every wave has them in its lanes, otherwise the workgroup has what is before every
+// sequence in LDS (pre[0 .. num_seqs]), for one kv head.
+struct Fp4Line {
   Fp4Seq seq;        // of sequence `lane`
-  int units, before; // its units, and those before it
+  int cost, before;
   uint32_t total;    // of all sequences and kv heads
 };
 
-__device__ __forceinline__ Fp4Units number_units(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
+__device__ __forceinline__ Fp4Line make_line(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Fp4Units r = {};
+  Fp4Line r = {};
   int run = 0;
   if (a.batch.num_seqs <= 64) {
     if (lane < a.batch.num_seqs) {
       r.seq = decode_seq(a, lane);
-      r.units = decode_units(r.seq);
+      r.cost = decode_cost(a, r.seq);
     }
-    const int upto = wave_prefix(r.units);
-    r.before = upto - r.units;
+    const int upto = wave_prefix(r.cost);
+    r.before = upto - r.cost;
     run = __builtin_amdgcn_readlane(upto, 63);
     if (blockIdx.x == 0 && wave == 0) {
       if (lane < a.batch.num_seqs) a.prefix[lane] = r.before;
@@ -54,7 +54,7 @@ __device__ __forceinline__ Fp4Units number_units(const Fp4Attention& a, int32_t*
   } else {
     for (int base = 0; base < a.batch.num_seqs; base += 64 * kDecodeWaves) {
       const int b = base + threadIdx.x;
-      const int v = b < a.batch.num_seqs ? decode_units(decode_seq(a, b)) : 0;
+      const int v = b < a.batch.num_seqs ? decode_cost(a, decode_seq(a, b)) : 0;
       const int x = wave_prefix(v);
       __syncthreads();
       if (lane == 63) scratch[wave] = x;
@@ -75,20 +75,20 @@ __device__ __forceinline__ Fp4Units number_units(const Fp4Attention& a, int32_t*
   return r;
 }
 
-// The sequence of unit u: the last one with units that has no more than u before it.
+// The sequence at place u of the line: the last one that costs anything and has no more than u before it.
 struct Fp4Place {
-  int b, before, per_head;
+  int b, before, cost;   // cost of a kv head
   Fp4Seq seq;
 };
-__device__ __forceinline__ Fp4Place find_unit(const Fp4Attention& a, const Fp4Units& units, const int32_t* pre, uint32_t u) {
+__device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4Line& line, const int32_t* pre, uint32_t u) {
   Fp4Place p;
   const uint32_t heads = a.batch.num_kv_heads;
   if (a.batch.num_seqs <= 64) {
-    const uint64_t candidates = __ballot(units.units > 0 && uint32_t(units.before) * heads <= u);
+    const uint64_t candidates = __ballot(line.cost > 0 && uint32_t(line.before) * heads <= u);
     p.b = 63 - __builtin_clzll(candidates);
-    p.before = __builtin_amdgcn_readlane(units.before, p.b);
-    p.per_head = __builtin_amdgcn_readlane(units.units, p.b);
-    p.seq = {__builtin_amdgcn_readlane(units.seq.first, p.b), __builtin_amdgcn_readlane(units.seq.n, p.b), __builtin_amdgcn_readlane(units.seq.len, p.b)};
+    p.before = __builtin_amdgcn_readlane(line.before, p.b);
+    p.cost = __builtin_amdgcn_readlane(line.cost, p.b);
+    p.seq = {__builtin_amdgcn_readlane(line.seq.first, p.b), __builtin_amdgcn_readlane(line.seq.n, p.b), __builtin_amdgcn_readlane(line.seq.len, p.b)};
   } else {
     int b = 0, e = a.batch.num_seqs;
     while (e - b > 1) {
@@ -96,10 +96,10 @@ __device__ __forceinline__ Fp4Place find_unit(const Fp4Attention& a, const Fp4Un
       if (uint32_t(pre[m]) * heads <= u) b = m;
       else e = m;
     }
-    // (of sequences with the same number before them the search ends at the last, which is the one with units)
+    // (of sequences with the same before them the search ends at the last, which is the one that costs something)
     p.b = __builtin_amdgcn_readfirstlane(b);
     p.before = __builtin_amdgcn_readfirstlane(pre[p.b]);
-    p.per_head = __builtin_amdgcn_readfirstlane(pre[p.b + 1]) - p.before;
+    p.cost = __builtin_amdgcn_readfirstlane(pre[p.b + 1]) - p.before;
     const Fp4Seq s = decode_seq(a, p.b);
     p.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
   }
@@ -115,15 +115,16 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
   const int lane = threadIdx.x & 63;
   const int c16 = lane & 15, j = lane >> 4;
   const Fp4Batch& bt = a.batch;
-  const Fp4Units units = number_units(a, pre, scratch);
-  const uint32_t share = unit_share(units.total, a.workers);
+  const Fp4Line line = make_line(a, pre, scratch);
+  const uint32_t share = cost_share(line.total, a.workers);
   const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
   uint32_t u = w * share;
-  const uint32_t end = u + share < units.total ? u + share : units.total;
+  const uint32_t end = u + share < line.total ? u + share : line.total;
   if (u >= end) return;
   // read once and not again before hundreds of MB have passed: past the caches, which then read faster (128K, 40 heads: 130 -> 111 us); what
-  // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches)
-  const bool stream = uint64_t(units.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
+  // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches).  With more than one
+  // operand of queries the memory is not what is waited for.
+  const bool stream = RT == 1 && uint64_t(line.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
   // byte offsets of a lane's pieces in 16 tokens
@@ -134,12 +135,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
 
   bool first_segment = true;
   while (u < end) {
-    const Fp4Place place = find_unit(a, units, pre, u);
-    const int b = place.b, per_head = place.per_head;
+    const Fp4Place place = find_place(a, line, pre, u);
+    const int b = place.b, n = place.seq.n, len = place.seq.len, rows = n * a.rep;
+    const uint32_t cost = place.cost, per_unit = decode_operands(a, place.seq);
     const uint32_t local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
-    const int h = local / uint32_t(per_head), u0 = local - uint32_t(h) * per_head;
-    const int u1 = end - u < uint32_t(per_head - u0) ? u0 + int(end - u) : per_head;
-    const int n = place.seq.n, len = place.seq.len, rows = n * a.rep;
+    const int h = local / cost;
+    const uint32_t c0 = local - uint32_t(h) * cost, c1 = end - u < cost - c0 ? c0 + (end - u) : cost;
+    u += c1 - c0;
+    // the units that begin in c0 .. c1 - 1
+    const int u0 = (c0 + per_unit - 1) / per_unit, u1 = (c1 + per_unit - 1) / per_unit;
+    if (u0 == u1) {
+      first_segment = false;
+      continue;
+    }
 
     // the queries: lane (row c16, quarter j) has the channels that its K pieces have
     u32x4 raw[RT][kSteps] = {};
@@ -175,7 +183,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
     next_tile(id1, at1);
     const char* head = bt.pool + h * run;
     const int64_t page_bytes = run * bt.num_kv_heads;
-    auto load_tile = [&](auto policy, Fp4Tile<HD>& t, int id, int at) {
+    auto load_tile = [&](auto policy, Fp4Tile<HD>& t, int id, int at) __attribute__((always_inline)) {
       constexpr int kPolicy = decltype(policy)::value;
       // a resource per page: the address is a base in scalar registers, an offset of the lane that never changes and one of the tile; a page
       // that is none has no bytes, and reads of it give zeros
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
       t.k_scale = __builtin_amdgcn_raw_buffer_load_b8(rs, off_ks, scales, 0);
       t.v_scale = __builtin_amdgcn_raw_buffer_load_b32(rs, off_vs, scales, 0);
     };
-    auto load_unit = [&](auto policy, Fp4Tile<HD>& ta, Fp4Tile<HD>& tb) {
+    auto load_unit = [&](auto policy, Fp4Tile<HD>& ta, Fp4Tile<HD>& tb) __attribute__((always_inline)) {
       load_tile(policy, ta, id0, at0);
       load_tile(policy, tb, id1, at1);
       next_tile(id0, at0);
@@ -237,19 +245,20 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
     }
     const int free_below = len - n + 1;   // tokens that every query sees
 
-    auto compute = [&](Fp4Tile<HD>& ta, Fp4Tile<HD>& tb, int tok0) {
+    auto compute = [&](auto operands, Fp4Tile<HD>& ta, Fp4Tile<HD>& tb, int tok0) __attribute__((always_inline)) {
+      constexpr int kLive = decltype(operands)::value;   // of the RT operands of queries
       // logits
-      f32x4 s[RT][2];
+      f32x4 s[kLive][2];
       {
         const float sa = __builtin_bit_cast(float, ta.k_scale << 23), sb = __builtin_bit_cast(float, tb.k_scale << 23);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{};
+        for (int rt = 0; rt < kLive; ++rt) s[rt][0] = s[rt][1] = f32x4{};
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) {
           const u32x4 wa = {fp4_pair<0>(ta.k[st], sa), fp4_pair<1>(ta.k[st], sa), fp4_pair<2>(ta.k[st], sa), fp4_pair<3>(ta.k[st], sa)};
           const u32x4 wb = {fp4_pair<0>(tb.k[st], sb), fp4_pair<1>(tb.k[st], sb), fp4_pair<2>(tb.k[st], sb), fp4_pair<3>(tb.k[st], sb)};
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
+          for (int rt = 0; rt < kLive; ++rt) {
             s[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wa), q[rt][st], s[rt][0], 0, 0, 0);
             s[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wb), q[rt][st], s[rt][1], 0, 0, 0);
           }
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
+          for (int rt = 0; rt < kLive; ++rt) {
             s[rt][0][x] = ta.ok && ka + x < lim[rt] ? s[rt][0][x] : -__builtin_inff();
             s[rt][1][x] = tb.ok && kb + x < lim[rt] ? s[rt][1][x] : -__builtin_inff();
           }
@@ -270,9 +279,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
         }
       }
       // weights
-      h8 p[RT];
+      h8 p[kLive];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
+      for (int rt = 0; rt < kLive; ++rt) {
         float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
                           fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3]))) * c[rt];
         if (__any(top > m[rt] + kMaxSlack)) {
@@ -296,7 +305,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
       // weighted sums
       const float va0 = fp4_scale(ta.v_scale, 0), va1 = fp4_scale(ta.v_scale, 1), va2 = fp4_scale(ta.v_scale, 2), va3 = fp4_scale(ta.v_scale, 3);
       const float vb0 = fp4_scale(tb.v_scale, 0), vb1 = fp4_scale(tb.v_scale, 1), vb2 = fp4_scale(tb.v_scale, 2), vb3 = fp4_scale(tb.v_scale, 3);
-      auto pair_of_channels = [&](auto byte_tag, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, int ct) {
+      auto pair_of_channels = [&](auto byte_tag, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, int ct) __attribute__((always_inline)) {
         constexpr int B = decltype(byte_tag)::value;
         const uint32_t x0 = fp4_pair<B>(a0, va0), x1 = fp4_pair<B>(a1, va1), x2 = fp4_pair<B>(a2, va2), x3 = fp4_pair<B>(a3, va3);
         const uint32_t y0 = fp4_pair<B>(b0, vb0), y1 = fp4_pair<B>(b1, vb1), y2 = fp4_pair<B>(b2, vb2), y3 = fp4_pair<B>(b3, vb3);
@@ -305,7 +314,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
         const u32x4 odd = {__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302), __builtin_amdgcn_perm(y1, y0, 0x07060302),
                            __builtin_amdgcn_perm(y3, y2, 0x07060302)};
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
+        for (int rt = 0; rt < kLive; ++rt) {
           o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, even), p[rt], o[rt][ct], 0, 0, 0);
           o[rt][ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, odd), p[rt], o[rt][ct + 1], 0, 0, 0);
         }
@@ -325,22 +334,30 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
     };
 
     // the next unit is on its way while one is worked on
-    auto walk = [&](auto policy) {
+    auto walk = [&](auto policy, auto operands) __attribute__((always_inline)) {
       for (int k = u0;;) {
         load_unit(policy, y0, y1);
-        compute(x0, x1, k * kUnit);
+        compute(operands, x0, x1, k * kUnit);
         if (++k >= u1) break;
         load_unit(policy, x0, x1);
-        compute(y0, y1, k * kUnit);
+        compute(operands, y0, y1, k * kUnit);
         if (++k >= u1) break;
       }
     };
-    if (stream) walk(std::integral_constant<int, 2>{});
-    else walk(std::integral_constant<int, 0>{});
+    if constexpr (RT == 1) {
+      if (stream) walk(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+      else walk(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+    } else {
+      const std::integral_constant<int, 0> cached;
+      if (per_unit == 1) walk(cached, std::integral_constant<int, 1>{});
+      else if (RT == 2 || per_unit == 2) walk(cached, std::integral_constant<int, 2>{});
+      else if (RT == 3 || per_unit == 3) walk(cached, std::integral_constant<int, (RT < 3 ? RT : 3)>{});
+      else walk(cached, std::integral_constant<int, RT>{});
+    }
 
     // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
     // each end, so two places per wave are enough
-    const bool whole = u0 == 0 && u1 == per_head;
+    const bool whole = u0 == 0 && u1 == decode_units(place.seq);
     const int64_t slot = 2 * int64_t(w) + (first_segment ? 0 : 1);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -387,7 +404,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
       }
     }
     first_segment = false;
-    u += u1 - u0;
   }
 }
 

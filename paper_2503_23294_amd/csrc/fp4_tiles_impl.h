@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   const int tiles_per_page = P / 16;
   int next16 = 4 * k0, col = next16 / tiles_per_page, in_page = next16 - col * tiles_per_page;
   int id[4], at[4];
-  auto next_tiles = [&]() {
+  auto next_tiles = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       id[x] = table_entry(table + col);
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   uint32_t raw_ks, raw_vs;
   const char *v_rows, *v_scales;   // of the step whose K was loaded last
   int bad_k;                       // its tiles that lie on no page, a bit each
-  auto load_k = [&]() {
+  auto load_k = [&]() __attribute__((always_inline)) {
     const char *rows_of[4], *scales_of[4];
     bad_k = 0;
 #pragma unroll
@@ -156,25 +156,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
     v_rows = pick(sub_v, rows_of[0], rows_of[1], rows_of[2], rows_of[3]) + off_v;
     v_scales = pick(sub_v, scales_of[0], scales_of[1], scales_of[2], scales_of[3]) + off_vs;
   };
-  auto load_v = [&]() {
+  auto load_v = [&]() __attribute__((always_inline)) {
     raw_v = *reinterpret_cast<const u32x4*>(v_rows);
     raw_vs = *reinterpret_cast<const uint32_t*>(v_scales);
   };
   // What lies in places that no token has been stored to must not be taken for numbers: weights of zero do not hide a NaN.  (Of K it does not
   // matter, logits are masked.)
-  auto clean_v = [&](int step, int bad) {
+  auto clean_v = [&](int step, int bad) __attribute__((always_inline)) {
     if (!bad && (step + 1) * kTileKeys <= len) return;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       if ((bad >> sub_v & 1) || step * kTileKeys + quad * 4 + t >= len) raw_v[t] = 0, raw_vs = (raw_vs & ~(255u << (8 * t))) | 127u << (8 * t);
   };
-  auto stage_k = [&](int piece, int slot) {
+  auto stage_k = [&](int piece, int slot) __attribute__((always_inline)) {
     const float s = __builtin_bit_cast(float, raw_ks << 23);
     u32x4* dst = reinterpret_cast<u32x4*>(lds.k[slot] + (key & 31) * Fp4TileLds<HD>::kKeyStride + part * (8 * kPieces));
     const uint32_t w = raw_k[piece];
     dst[piece] = u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
   };
-  auto stage_v = [&](auto byte_tag, int buffer) {
+  auto stage_v = [&](auto byte_tag, int buffer) __attribute__((always_inline)) {
     constexpr int B = decltype(byte_tag)::value;
     // tokens of 16 in the order of quads 0, 2, 1, 3
     const int place = (quad & ~3) | ((quad & 1) << 1) | ((quad >> 1) & 1);
@@ -185,11 +185,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
     *reinterpret_cast<u32x2*>(dst + (2 * B + 1) * Fp4TileLds<HD>::kChannelStride) =
         u32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302), __builtin_amdgcn_perm(x3, x2, 0x07060302)};
   };
-  auto stage_all_k = [&](int slot) {
+  auto stage_all_k = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) stage_k(x, slot);
   };
-  auto stage_v_piece = [&](int piece, int buffer) {
+  auto stage_v_piece = [&](int piece, int buffer) __attribute__((always_inline)) {
     if (piece == 0) stage_v(std::integral_constant<int, 0>{}, buffer);
     if constexpr (kPieces > 1) {
       if (piece == 1) stage_v(std::integral_constant<int, 1>{}, buffer);
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] = f32x16{};
 
   // Logits of 32 keys that a row does not see.
-  auto mask = [&](f32x16& s, int tok0, int bad) {   // bad: of the two 16-token tiles
+  auto mask = [&](f32x16& s, int tok0, int bad) __attribute__((always_inline)) {   // bad: of the two 16-token tiles
     if (tok0 + kChunk > wave_free || bad) {
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
     }
   };
   // The reference maximum of a row whose logits exceed it by too much becomes the largest of them.
-  auto raise = [&](const f32x16& s) {
+  auto raise = [&](const f32x16& s) __attribute__((always_inline)) {
     float top = s[0];
 #pragma unroll
     for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   // One half of a step: logits of the next 32 keys (`ahead`, from chunk `slot`), next to the weights of these (`s`); then these' products with V
   // (keys 32 * sub ... of `v`), next to the putting away of what has been loaded (`put`, kPieces times).  The order is written down
   // and kept: a product every few other instructions, its operands read four products before.
-  auto half_step = [&](const f32x16& s, f32x16& ahead, const _Float16* k, const _Float16* v, auto&& put) {
+  auto half_step = [&](const f32x16& s, f32x16& ahead, const _Float16* k, const _Float16* v, auto&& put) __attribute__((always_inline)) {
     constexpr int kLead = 4;
     constexpr int kProductsV = 2 * kChannelTiles;
     constexpr int kOrder = 0x4 | 0x10 | 0x20 | 0x40;   // scalar instructions and loads may move
