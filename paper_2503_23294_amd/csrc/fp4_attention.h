@@ -83,16 +83,20 @@ __device__ __forceinline__ int table_entry(const int32_t* p) {
   return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uint64_t>(p));
 }
 
-// Inclusive prefix sum over the lanes of a wave, without a trip through shared memory: shifts inside rows of 16, then the last lane of a row
-// to the rows behind it.
-__device__ __forceinline__ int wave_prefix(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
+// A row's joined state: reference maximum, sums of the weights rounded and unrounded, a lane's channels.
+template <int HD>
+struct Merged {
+  float top, l, lsum, o[HD / 64];
+};
+template <int HD>
+__device__ __forceinline__ void write_merged(const Fp4Attention& a, const Merged<HD>& r, int64_t row, int lane) {
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  if constexpr (HD == 128) {
+    reinterpret_cast<uint32_t*>(a.out)[row * 64 + lane] = pack_out(r.o[0] * inv, r.o[1] * inv, a.bf16);
+  } else {
+    reinterpret_cast<uint16_t*>(a.out)[row * 64 + lane] = uint16_t(pack_out(r.o[0] * inv, 0.f, a.bf16));
+  }
+  if (a.lse && lane == 0) a.lse[row] = r.l == 0.f ? -__builtin_inff() : (r.top + __builtin_amdgcn_logf(r.lsum)) * kLn2;
 }
 
 }  // namespace cocktail

@@ -12,10 +12,6 @@ namespace cocktail {
 // Sum of a row's partial states: `parts` of them, the first at row `first_slot` of the arrays and the others at second_slot, second_slot + step ...
 // Wave `wave` of `waves` takes every waves-th; o: the lane's channels, l and lsum: whole sums (in every wave).
 template <int HD>
-struct Merged {
-  float top, l, lsum, o[HD / 64];
-};
-template <int HD>
 __device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* po, int64_t first_slot, int64_t second_slot, int64_t step, int parts,
                                                   int wave, int waves, int lane) {
   constexpr int kPer = HD / 64;
@@ -48,17 +44,6 @@ __device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* 
     r.lsum += __shfl_xor(r.lsum, d);
   }
   return r;
-}
-
-template <int HD>
-__device__ __forceinline__ void write_merged(const Fp4Attention& a, const Merged<HD>& r, int64_t row, int lane) {
-  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
-  if constexpr (HD == 128) {
-    reinterpret_cast<uint32_t*>(a.out)[row * 64 + lane] = pack_out(r.o[0] * inv, r.o[1] * inv, a.bf16);
-  } else {
-    reinterpret_cast<uint16_t*>(a.out)[row * 64 + lane] = uint16_t(pack_out(r.o[0] * inv, 0.f, a.bf16));
-  }
-  if (a.lse && lane == 0) a.lse[row] = r.l == 0.f ? -__builtin_inff() : (r.top + __builtin_amdgcn_logf(r.lsum)) * kLn2;
 }
 
 // Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves of its segment left, if there were several, and
@@ -141,7 +126,7 @@ namespace {
 
 // What a call launches, from what the host knows: bounds, no lengths.
 struct Split {
-  bool decode, tiles;
+  bool decode, whole, tiles;
   int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
   size_t prefix_bytes, part_rows, tile_rows, bytes;
 };
@@ -167,6 +152,12 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
     const int64_t fill = s.row_tiles == 1 ? 2048 : 1024;
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
+    // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 300, 1000, 2048 tokens 12.2, 12.2, 11.5 us in two launches,
+    // 5.7, 7.5, 10.9 in one; 4096: 12.0 and 17.9), and up to 6K where the segments fill the chip by themselves, once or twice (128, 256, 512
+    // of 4096 tokens: 23.0, 32.6, 57.3 and 19.5, 25.7, 49.2; 512 of 8192: 104 and 109; 1024 of 4096: 105 and 112).
+    const int64_t segments = seqs * c->num_kv_heads;
+    s.whole = s.row_tiles == 1 && max_len <= (segments >= 128 && segments <= 512 ? 6144 : 2048);
+    if (s.whole) workers = 0;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
   }
@@ -263,15 +254,17 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
   hipError_t e = hipSuccess;
   if (s.decode) {
     typedef void (*Kernel)(Fp4Attention);
-    static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1>, fp4_decode_kernel<64, 2>, fp4_decode_kernel<64, 3>, fp4_decode_kernel<64, 4>},
-                                         {fp4_decode_kernel<128, 1>, fp4_decode_kernel<128, 2>, fp4_decode_kernel<128, 3>, fp4_decode_kernel<128, 4>}};
-    const Kernel kernel = kernels[hd == 128][s.row_tiles - 1];
-    e = launch_lds(kernel, dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
+    static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1, false>, fp4_decode_kernel<64, 2, false>, fp4_decode_kernel<64, 3, false>, fp4_decode_kernel<64, 4, false>},
+                                         {fp4_decode_kernel<128, 1, false>, fp4_decode_kernel<128, 2, false>, fp4_decode_kernel<128, 3, false>, fp4_decode_kernel<128, 4, false>}};
+    if (s.whole)
+      e = launch(hd == 128 ? fp4_decode_kernel<128, 1, true> : fp4_decode_kernel<64, 1, true>, dim3(cache->pages.num_seqs * cache->num_kv_heads), dim3(64 * kWholeWaves), st, a);
+    else
+      e = launch_lds(kernels[hd == 128][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }
   if (e == hipSuccess && s.tiles)
     e = launch(s.tile_waves == 8 ? (hd == 128 ? fp4_tile_kernel<128, 8> : fp4_tile_kernel<64, 8>) : (hd == 128 ? fp4_tile_kernel<128, 4> : fp4_tile_kernel<64, 4>),
                dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * s.tile_waves), st, a);
-  if (e == hipSuccess && s.decode) {
+  if (e == hipSuccess && s.decode && !s.whole) {
     const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;
     // states that a row has, about: many of them are read by many waves at a time (40 heads, 51 states each: 8.8 us by four waves), a few by one

@@ -43,6 +43,18 @@ __device__ __forceinline__ int fp4_len(const Fp4Batch& a, int b) {
   return n < 0 ? 0 : n > most ? most : n;
 }
 
+// Inclusive prefix sum over the lanes of a wave, without a trip through shared memory: shifts inside rows of 16, then the last lane of a row
+// to the rows behind it.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
 // Value in 0 .. 255 of byte k of a word, as the float 2^(value - 127).
 __device__ __forceinline__ float fp4_scale(uint32_t word, int k) { return __builtin_bit_cast(float, ((word >> (8 * k)) & 255u) << 23); }
 

@@ -106,25 +106,34 @@ __device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4L
   return p;
 }
 
-template <int HD, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
+// WHOLE: a workgroup of kWholeWaves waves has one segment and shares it out among them, their states are joined in LDS: one launch, for short contexts.
+constexpr int kWholeWaves = 8;
+
+template <int HD, int RT, bool WHOLE>
+__global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
   __shared__ int32_t scratch[kDecodeWaves + 1];
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j = lane >> 4;
   const Fp4Batch& bt = a.batch;
-  const Fp4Line line = make_line(a, pre, scratch);
-  const uint32_t share = cost_share(line.total, a.workers);
-  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
-  uint32_t u = w * share;
-  const uint32_t end = u + share < line.total ? u + share : line.total;
-  if (u >= end) return;
-  // read once and not again before hundreds of MB have passed: past the caches, which then read faster (128K, 40 heads: 130 -> 111 us); what
-  // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches).  With more than one
-  // operand of queries the memory is not what is waited for.
-  const bool stream = RT == 1 && uint64_t(line.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
+  Fp4Line line = {};
+  int w = 0;
+  uint32_t u = 0, end = 1;
+  bool stream = false;
+  if constexpr (!WHOLE) {
+    line = make_line(a, pre, scratch);
+    const uint32_t share = cost_share(line.total, a.workers);
+    w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+    u = w * share;
+    end = u + share < line.total ? u + share : line.total;
+    if (u >= end) return;
+    // read once and not again before hundreds of MB have passed: past the caches, which then read faster (128K, 40 heads: 130 -> 111 us); what
+    // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches).  With more than one
+    // operand of queries the memory is not what is waited for.
+    stream = RT == 1 && uint64_t(line.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
+  }
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
   // byte offsets of a lane's pieces in 16 tokens
@@ -135,18 +144,34 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
 
   bool first_segment = true;
   while (u < end) {
-    const Fp4Place place = find_place(a, line, pre, u);
+    Fp4Place place;
+    int h, u0, u1;
+    if constexpr (WHOLE) {
+      place.b = int(blockIdx.x) / bt.num_kv_heads;
+      h = int(blockIdx.x) - place.b * bt.num_kv_heads;
+      const Fp4Seq s = decode_seq(a, place.b);
+      place.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+      if (place.seq.n == 0) return;
+      const uint32_t units = decode_units(place.seq);
+      u0 = units * wave / kWholeWaves;
+      u1 = units * (wave + 1) / kWholeWaves;
+      u = end;
+    } else {
+      place = find_place(a, line, pre, u);
+    }
     const int b = place.b, n = place.seq.n, len = place.seq.len, rows = n * a.rep;
-    const uint32_t cost = place.cost, per_unit = decode_operands(a, place.seq);
-    const uint32_t local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
-    const int h = local / cost;
-    const uint32_t c0 = local - uint32_t(h) * cost, c1 = end - u < cost - c0 ? c0 + (end - u) : cost;
-    u += c1 - c0;
-    // the units that begin in c0 .. c1 - 1
-    const int u0 = (c0 + per_unit - 1) / per_unit, u1 = (c1 + per_unit - 1) / per_unit;
-    if (u0 == u1) {
-      first_segment = false;
-      continue;
+    const uint32_t per_unit = decode_operands(a, place.seq);
+    if constexpr (!WHOLE) {
+      const uint32_t cost = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
+      h = local / cost;
+      const uint32_t c0 = local - uint32_t(h) * cost, c1 = end - u < cost - c0 ? c0 + (end - u) : cost;
+      u += c1 - c0;
+      // the units that begin in c0 .. c1 - 1
+      u0 = (c0 + per_unit - 1) / per_unit, u1 = (c1 + per_unit - 1) / per_unit;
+      if (u0 == u1) {
+        first_segment = false;
+        continue;
+      }
     }
 
     // the queries: lane (row c16, quarter j) has the channels that its K pieces have
@@ -165,7 +190,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
     // (the last ones are then loaded again): with loads under a condition, the number of those in flight is not known when the code is made,
     // and every wait becomes one for all of them.
     const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
-    const int last_tile = 2 * u1 - 1 < (len + 15) / 16 - 1 ? 2 * u1 - 1 : (len + 15) / 16 - 1;
+    const int tiles = (len + 15) / 16;
+    const int last_tile = 2 * u1 < tiles ? 2 * u1 - 1 : tiles - 1;
     const int tiles_per_page = P / 16;
     int tile = 2 * u0, col = tile / tiles_per_page, in_page = tile - col * tiles_per_page;   // of the table read
     auto next_tile = [&](int& id, int& at) {
@@ -344,7 +370,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
         if (++k >= u1) break;
       }
     };
-    if constexpr (RT == 1) {
+    if (WHOLE && u0 == u1) {
+      // (a wave without keys has the state of none)
+    } else if constexpr (WHOLE) {
+      walk(std::integral_constant<int, 0>{}, std::integral_constant<int, RT>{});
+    } else if constexpr (RT == 1) {
       if (stream) walk(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
       else walk(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
     } else {
@@ -357,7 +387,45 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void fp4_decode
 
     // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
     // each end, so two places per wave are enough
-    const bool whole = u0 == 0 && u1 == decode_units(place.seq);
+    if constexpr (WHOLE) {
+      __shared__ float states[kWholeWaves][16 * RT][HD + 4];   // sums, then (m, l, l unrounded)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float sum = lsum[rt];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        float* dst = states[wave][rt * 16 + c16];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < kChannelTiles / 4; ++y)
+            *reinterpret_cast<f32x4*>(dst + j * (HD / 4) + x * kChannelTiles + 4 * y) =
+                f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
+        if (j == 0) dst[HD] = m[rt], dst[HD + 1] = l[rt][0], dst[HD + 2] = sum;
+      }
+      __syncthreads();
+      // a wave joins every eighth row
+      for (int r = wave; r < rows; r += kWholeWaves) {
+        float top = kNoMax;
+#pragma unroll
+        for (int v = 0; v < kWholeWaves; ++v) top = fmaxf(top, states[v][r][HD]);
+        Merged<HD> x = {};
+        x.top = top;
+#pragma unroll
+        for (int v = 0; v < kWholeWaves; ++v) {
+          const float* src = states[v][r];
+          const float weight = __builtin_amdgcn_exp2f(src[HD] - top);
+          x.l += weight * src[HD + 1];
+          x.lsum += weight * src[HD + 2];
+#pragma unroll
+          for (int y = 0; y < HD / 64; ++y) x.o[y] += weight * src[lane * (HD / 64) + y];
+        }
+        const int i = r / a.rep;
+        write_merged<HD>(a, x, int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep, lane);
+      }
+      return;
+    }
+    const bool whole = u0 == 0 && u1 == int(decode_units(place.seq));
     const int64_t slot = 2 * int64_t(w) + (first_segment ? 0 : 1);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {

@@ -6,9 +6,6 @@
 
 namespace cocktail {
 
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr int kRowsPerThread = COCKTAIL_MAX_SEQS / kPlanThreads;
-
 // Workspace: [0] number of pages to move, then the moves (from, to), then a list of pages / the new number of every page.
 struct PageWork {
   int32_t* count;
@@ -24,173 +21,183 @@ inline PageWork page_work(void* workspace, int num_seqs, int num_pages) {
   return {w, w + 16, w + 16 + 2 * size_t(num_seqs > num_pages ? num_seqs : num_pages)};
 }
 
-// Exclusive prefix of v over the threads of the workgroup, and the sum; every thread gets both.  `lds`: kPlanWaves + 1 ints.
+// Exclusive prefix of v over the threads of the workgroup, and the sum; every thread gets both.  `lds`: THREADS / 64 ints, not the same in two
+// calls one behind the other (so that one barrier is enough).
+template <int THREADS>
 __device__ __forceinline__ int block_prefix(int v, int* sum, int* lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  __syncthreads();   // what the call before left in `lds` has been read
-  if (lane == 63) lds[wave] = x;
+  constexpr int kWaves = THREADS / 64;
+  const int wave = threadIdx.x >> 6;
+  const int x = wave_prefix(v);
+  if ((threadIdx.x & 63) == 63) lds[wave] = x;
   __syncthreads();
   int before = 0, all = 0;
-  for (int w = 0; w < kPlanWaves; ++w) {
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
     const int n = lds[w];
-    if (w < wave) before += n;
+    before += w < wave ? n : 0;
     all += n;
   }
   *sum = all;
   return before + x - v;
 }
 
-// One workgroup.  Thread t has rows t * kRowsPerThread + i, so that prefixes over the rows are prefixes over the threads.
-__global__ __launch_bounds__(kPlanThreads) void pages_resize_kernel(cocktail_page_table p, const int32_t* __restrict__ delta, PageWork w, int copy) {
-  extern __shared__ int32_t lds[];                 // tail[num_seqs], first[num_seqs + 1], scratch
-  int32_t* tail_of = lds;
-  int32_t* first = lds + p.num_seqs;
-  int32_t* scratch = first + p.num_seqs + 1;
-  __shared__ int any_shared, too_short;   // too_short: 1 columns, 2 pools
-  const int tid = threadIdx.x;
-  if (tid == 0) any_shared = too_short = 0;
-  __syncthreads();
-  int64_t len1[kRowsPerThread];
-  int have[kRowsPerThread], need[kRowsPerThread], held[kRowsPerThread];
-  int fresh_sum = 0;
+// References of 16 consecutive pages, a word each; pages behind the last one count as held.
+struct Refs16 {
+  int r[16];
+};
+__device__ __forceinline__ Refs16 load_refs(const cocktail_page_table& p, int64_t page) {
+  Refs16 x;
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    const int b = tid * kRowsPerThread + i;
+  for (int i = 0; i < 16; ++i) x.r[i] = page + i < p.num_pages ? p.refs[page + i] : 1;
+  return x;
+}
+
+// One workgroup, for it is a matter of a few dependent reads: lengths, last pages, their holders, free pages.  Thread t has rows t * ROWS + i, so that
+// prefixes over the rows are prefixes over the threads.  A step of 64 sequences: 18 us with 1024 threads that read everything again where it
+// was needed, now with 256 threads, lists in shared memory and the references read before anything is known 8 us.
+constexpr int kListInLds = 2048;
+template <int THREADS, int ROWS>
+__global__ __launch_bounds__(THREADS) void pages_resize_kernel(cocktail_page_table p, const int32_t* __restrict__ delta, PageWork w, int copy) {
+  constexpr int kMost = THREADS * ROWS;
+  __shared__ int32_t tail_of[kMost], first[kMost], start_of[kMost], lds_list[kListInLds], scratch[4][THREADS / 64];
+  __shared__ int any_shared, failed;   // failed: 1 columns, 2 pools
+  const int tid = threadIdx.x;
+  Refs16 refs = load_refs(p, int64_t(tid) * 16);
+  if (tid == 0) any_shared = failed = 0;
+  int64_t len1[ROWS];
+  int have[ROWS], need[ROWS], tail[ROWS], held[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int b = tid * ROWS + i;
     have[i] = need[i] = held[i] = 0;
     len1[i] = 0;
+    tail[i] = -1;
     if (b >= p.num_seqs) continue;
     const int d = delta[b];
-    int len0 = p.seq_lens[b];
-    len0 = len0 < 0 ? 0 : len0;
-    len1[i] = int64_t(len0) + d < 0 ? 0 : int64_t(len0) + d;
-    have[i] = int((int64_t(len0) + p.page_size - 1) / p.page_size);
+    const int len0 = max(p.seq_lens[b], 0);
+    len1[i] = max(int64_t(len0) + d, int64_t(0));
+    have[i] = min(int((int64_t(len0) + p.page_size - 1) / p.page_size), p.table_stride);
     const int64_t want = (len1[i] + p.page_size - 1) / p.page_size;
-    if (have[i] > p.table_stride) have[i] = p.table_stride;
-    if (want > p.table_stride) too_short = 1;   // (every thread that writes this writes the same)
-    need[i] = want > p.table_stride ? p.table_stride : int(want);
-    int tail = -1;
-    if (d > 0 && len0 % p.page_size && have[i] > 0) {
-      tail = p.table[int64_t(b) * p.table_stride + have[i] - 1];
-      if (uint32_t(tail) >= uint32_t(p.num_pages)) tail = -1;
-      else held[i] = p.refs[tail];
-      if (held[i] > 1) any_shared = 1;
-    }
-    tail_of[b] = tail;
+    need[i] = want > p.table_stride ? -1 : int(want);
+    if (d > 0 && len0 % p.page_size && have[i] > 0) tail[i] = p.table[int64_t(b) * p.table_stride + have[i] - 1];
+    if (uint32_t(tail[i]) >= uint32_t(p.num_pages)) tail[i] = -1;
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int b = tid * ROWS + i;
+    if (tail[i] >= 0) held[i] = p.refs[tail[i]];
+    tail_of[b] = tail[i];
   }
   __syncthreads();
-  if (any_shared && !copy) too_short = 2;   // a copy would be due and there is nothing to copy: every thread writes the same
-  bool copies[kRowsPerThread];
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    const int b = tid * kRowsPerThread + i;
+  for (int i = 0; i < ROWS; ++i) {
+    if (held[i] > 1) any_shared = 1;   // (every thread that writes these writes the same)
+    if (need[i] < 0) failed = 1;
+  }
+  __syncthreads();
+  if (any_shared && !copy) failed = 2;
+  bool copies[ROWS];
+  int fresh[ROWS], fresh_sum = 0, ncopies = 0;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int b = tid * ROWS + i;
     copies[i] = false;
-    if (any_shared && held[i] > 1) {
+    if (held[i] > 1) {
       int alike = 0;
       bool later = false;
-      for (int c = 0; c < p.num_seqs; ++c)
-        if (tail_of[c] == tail_of[b]) {
-          ++alike;
-          later |= c > b;
-        }
+#pragma unroll 8
+      for (int c = 0; c < p.num_seqs; ++c) {
+        const bool same = tail_of[c] == tail[i];
+        alike += same ? 1 : 0;
+        later |= same && c > b;
+      }
       copies[i] = later || held[i] > alike;
     }
-    fresh_sum += (copies[i] ? 1 : 0) + (need[i] > have[i] ? need[i] - have[i] : 0);
+    fresh[i] = (copies[i] ? 1 : 0) + max(need[i] - have[i], 0);
+    fresh_sum += fresh[i];
+    ncopies += copies[i] ? 1 : 0;
   }
-  int total;
-  int at = block_prefix(fresh_sum, &total, scratch);
+  int total, nmoves;
+  int at = block_prefix<THREADS>(fresh_sum, &total, scratch[0]);
+  int move = block_prefix<THREADS>(ncopies, &nmoves, scratch[1]);
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    const int b = tid * kRowsPerThread + i;
-    if (b >= p.num_seqs) break;
-    first[b] = at;
-    at += (copies[i] ? 1 : 0) + (need[i] > have[i] ? need[i] - have[i] : 0);
+  for (int i = 0; i < ROWS; ++i) {
+    first[tid * ROWS + i] = at;
+    start_of[tid * ROWS + i] = have[i] - (copies[i] ? 1 : 0);   // column of the first page that it takes: a copy replaces the last one
+    at += fresh[i];
   }
-  if (tid == 0) first[p.num_seqs] = total;
-  __syncthreads();
-  // the lowest free pages, as many as are needed
+  // the lowest free pages, as many as are needed; the next references are on their way while some are counted
+  const bool in_lds = total <= kListInLds;
   int found = 0;
-  if (!too_short)
-    for (int64_t base = 0; base < p.num_pages && found < total; base += kPlanThreads * 4) {
-      int free[4], mine = 0, sum;
+  if (!failed && total)
+    for (int64_t base = 0, turn = 0;; ++turn) {
+      const int64_t page = base + int64_t(tid) * 16;
+      int mine = 0, sum;
+      const Refs16 now = refs;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t page = base + tid * 4 + i;
-        free[i] = page < p.num_pages && p.refs[page] == 0;
-        mine += free[i];
-      }
-      int k = found + block_prefix(mine, &sum, scratch);
+      for (int i = 0; i < 16; ++i) mine += now.r[i] == 0 ? 1 : 0;
+      base += THREADS * 16;
+      const bool more = base < p.num_pages;
+      if (more) refs = load_refs(p, base + int64_t(tid) * 16);
+      int k = found + block_prefix<THREADS>(mine, &sum, scratch[2 + (turn & 1)]);
+      if (mine)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (free[i]) {
-          if (k < total) w.list[k] = int(base) + tid * 4 + i;
-          ++k;
-        }
+        for (int i = 0; i < 16; ++i)
+          if (now.r[i] == 0) {
+            if (k < total) {
+              if (in_lds) lds_list[k] = int(page) + i;
+              else w.list[k] = int(page) + i;
+            }
+            ++k;
+          }
       found += sum;
+      if (found >= total || !more) break;
     }
-  if (too_short || found < total) {
+  __syncthreads();   // the list and first[] are there
+  if (failed || found < total) {
     if (tid == 0) {
-      p.status[0] = too_short ? -too_short : total - found;
+      p.status[0] = failed ? -failed : total - found;
       w.count[0] = 0;
     }
     return;
   }
-  __syncthreads();   // the list is there
   // fresh pages: thread by thread over all of them, since one sequence may take thousands
-  for (int k = tid; k < total; k += kPlanThreads) {
-    int b = 0, e = p.num_seqs;
+  for (int k = tid; k < total; k += THREADS) {
+    int b = 0, e = kMost;
     while (e - b > 1) {
       const int m = (b + e) >> 1;
       if (first[m] <= k) b = m;
       else e = m;
     }
-    // rows before b that take nothing have the same first[]; the search ends at the last of them, which is the one that does
-    const int page = w.list[k];
-    const int len0 = p.seq_lens[b] < 0 ? 0 : p.seq_lens[b];
-    const int h = int((int64_t(len0) + p.page_size - 1) / p.page_size);
-    const int64_t l1 = int64_t(len0) + delta[b];
-    const int lacking = int((l1 + p.page_size - 1) / p.page_size) - h;
-    const int own = first[b + 1] - first[b] - (lacking > 0 ? lacking : 0);   // 1 if the first is a copy
-    const int col = h - own + (k - first[b]);
-    p.table[int64_t(b) * p.table_stride + col] = page;
+    // (rows before b that take nothing have the same first[]; the search ends at the last of them, which is the one that does)
+    const int page = in_lds ? lds_list[k] : w.list[k];
     p.refs[page] = 1;
+    p.table[int64_t(b) * p.table_stride + start_of[b] + (k - first[b])] = page;
   }
-  // copies: the old page has one holder less
-  int ncopies = 0, nmoves;
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) ncopies += copies[i] ? 1 : 0;
-  int m = block_prefix(ncopies, &nmoves, scratch);
-#pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    const int b = tid * kRowsPerThread + i;
-    if (!copies[i]) continue;
-    w.moves[2 * m] = tail_of[b];
-    w.moves[2 * m + 1] = w.list[first[b]];
-    ++m;
-    atomicAdd(&p.refs[tail_of[b]], -1);
+  for (int i = 0; i < ROWS; ++i) {
+    const int b = tid * ROWS + i;
+    if (b >= p.num_seqs) continue;
+    p.seq_lens[b] = int(len1[i]);
+    if (copies[i]) {
+      w.moves[2 * move] = tail[i];
+      w.moves[2 * move + 1] = in_lds ? lds_list[first[b]] : w.list[first[b]];
+      ++move;
+      atomicAdd(&p.refs[tail[i]], -1);
+    }
   }
   if (tid == 0) {
-    w.count[0] = copy ? nmoves : 0;
+    w.count[0] = nmoves;
     p.status[0] = 0;
   }
-  // pages that are given back: a wave per row; `first` now says which columns
+  // pages that are given back: a wave per row
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
-    const int b = tid * kRowsPerThread + i;
-    if (b >= p.num_seqs) break;
-    tail_of[b] = need[i];
-    first[b] = have[i];
-    p.seq_lens[b] = int(len1[i]);
-  }
+  for (int i = 0; i < ROWS; ++i) tail_of[tid * ROWS + i] = max(need[i], 0);
   __syncthreads();
-  for (int b = tid >> 6; b < p.num_seqs; b += kPlanWaves)
-    for (int c = tail_of[b] + (tid & 63); c < first[b]; c += 64) {
+  for (int b = tid >> 6; b < p.num_seqs; b += THREADS / 64)
+    for (int c = tail_of[b] + (tid & 63); c < start_of[b]; c += 64) {
       int32_t* entry = p.table + int64_t(b) * p.table_stride + c;
       const int page = *entry;
       if (uint32_t(page) < uint32_t(p.num_pages)) atomicAdd(&p.refs[page], -1);
@@ -231,15 +238,20 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(cocktail_page_table p, 
 }
 
 // One workgroup: where every page in use goes.
-__global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(cocktail_page_table p, PageWork w) {
-  __shared__ int scratch[kPlanWaves + 1];
+constexpr int kCompactThreads = 1024;
+__global__ __launch_bounds__(kCompactThreads) void pages_compact_kernel(cocktail_page_table p, PageWork w) {
+  __shared__ int scratch[4][kCompactThreads / 64];
   const int tid = threadIdx.x;
   int mine = 0, used;
-  for (int64_t i = tid; i < p.num_pages; i += kPlanThreads) mine += p.refs[i] != 0;
-  block_prefix(mine, &used, scratch);
+  for (int64_t page = int64_t(tid) * 16; page < p.num_pages; page += kCompactThreads * 16) {
+    const Refs16 x = load_refs(p, page);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mine += x.r[i] != 0 && page + i < p.num_pages ? 1 : 0;
+  }
+  block_prefix<kCompactThreads>(mine, &used, scratch[0]);
   int holes = 0, movers = 0;
-  for (int64_t base = 0; base < p.num_pages; base += kPlanThreads * 4) {
-    int kind[4], h = 0, m = 0, hsum, msum;
+  for (int64_t base = 0, turn = 0; base < p.num_pages; base += kCompactThreads * 4, ++turn) {
+    int kind[4], h = 0, m = 0, sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t page = base + tid * 4 + i;
@@ -251,17 +263,19 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(cocktail_pa
         w.list[page] = int(page);
       }
     }
-    int hk = holes + block_prefix(h, &hsum, scratch), mk = movers + block_prefix(m, &msum, scratch);
+    // both numbers in one word: at most 2^12 of each in a turn
+    const int before = block_prefix<kCompactThreads>(h | m << 16, &sum, scratch[2 + (turn & 1)]);
+    int hk = holes + (before & 0xffff), mk = movers + (before >> 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (kind[i] == 1) w.moves[2 * hk++ + 1] = int(base) + tid * 4 + i;
       if (kind[i] == 2) w.moves[2 * mk++] = int(base) + tid * 4 + i;
     }
-    holes += hsum;
-    movers += msum;
+    holes += sum & 0xffff;
+    movers += sum >> 16;
   }
   __syncthreads();
-  for (int k = tid; k < movers; k += kPlanThreads) w.list[w.moves[2 * k]] = w.moves[2 * k + 1];
+  for (int k = tid; k < movers; k += kCompactThreads) w.list[w.moves[2 * k]] = w.moves[2 * k + 1];
   if (tid == 0) w.count[0] = movers;
 }
 
@@ -362,8 +376,10 @@ extern "C" int cocktail_pages_resize(const cocktail_page_table* pages, const int
   if (reinterpret_cast<uintptr_t>(delta) & 3) return fail(COCKTAIL_EALIGN, "delta must be 4-byte aligned");
   hipStream_t st = static_cast<hipStream_t>(stream);
   const PageWork w = page_work(workspace, pages->num_seqs, pages->num_pages);
-  const size_t lds = sizeof(int32_t) * (2 * size_t(pages->num_seqs) + 1 + kPlanWaves + 1);
-  hipError_t e = launch_lds(pages_resize_kernel, dim3(1), dim3(kPlanThreads), lds, st, *pages, delta, w, num_pools > 0);
+  // few rows and few pages: fewer threads wait for each other
+  hipError_t e = pages->num_seqs <= 256 && pages->num_pages <= 16384
+                     ? launch(pages_resize_kernel<256, 1>, dim3(1), dim3(256), st, *pages, delta, w, int(num_pools > 0))
+                     : launch(pages_resize_kernel<1024, COCKTAIL_MAX_SEQS / 1024>, dim3(1), dim3(1024), st, *pages, delta, w, int(num_pools > 0));
   if (e == hipSuccess && num_pools) {
     const int64_t items = int64_t(pages->num_seqs) * num_pools * ((page_bytes + 16383) / 16384);
     e = launch(pages_move_kernel, dim3(uint32_t(items < 2048 ? items : 2048)), dim3(256), st, list, num_pools, page_bytes, w.count, w.moves, nullptr, *pages);
@@ -392,7 +408,7 @@ extern "C" int cocktail_pages_compact(const cocktail_page_table* pages, void* co
   if (int rc = check_pools(pages, pools, num_pools, page_bytes, workspace, workspace_bytes, &list)) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const PageWork w = page_work(workspace, pages->num_seqs, pages->num_pages);
-  hipError_t e = launch(pages_compact_kernel, dim3(1), dim3(kPlanThreads), st, *pages, w);
+  hipError_t e = launch(pages_compact_kernel, dim3(1), dim3(kCompactThreads), st, *pages, w);
   if (e == hipSuccess)
     e = launch(pages_move_kernel, dim3(2048), dim3(256), st, list, num_pools, page_bytes, w.count, w.moves, w.list, *pages);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "compact launch failed: %s", hipGetErrorString(e));

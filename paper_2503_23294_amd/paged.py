@@ -81,20 +81,13 @@ class PageTable:
         _int32("status", status, (4,), dev)
         self.table, self.seq_lens, self.refs, self.status = table, seq_lens, refs, status
         self.page_size, self.device = page_size, dev
+        self.num_seqs, self.num_pages = int(table.shape[0]), int(refs.shape[0])
         self.desc = _lib.PageTableDesc(table.data_ptr(), seq_lens.data_ptr(), refs.data_ptr(), status.data_ptr(), table.shape[0],
                                        table.shape[1], page_size, refs.shape[0])
         need = C.c_size_t(0)
         check(lib().cocktail_pages_workspace(C.byref(self.desc), C.byref(need)))   # also checks the sizes
         self.workspace_bytes = int(need.value)
         self.workspaces = _Workspaces(dev)
-
-    @property
-    def num_seqs(self) -> int:
-        return int(self.table.shape[0])
-
-    @property
-    def num_pages(self) -> int:
-        return int(self.refs.shape[0])
 
 
 class Fp4Cache:
@@ -117,19 +110,26 @@ class Fp4Cache:
         self.workspace_bytes = {}   # by the sizes of the call
 
 
+_POOL_ARRAYS = {}   # ctypes array types by length
+
+
 def _pool_list(pages: PageTable, pools: Sequence[torch.Tensor]):
     """ctypes array of the pools' addresses, their number and the bytes of a page."""
-    bytes_per_page = 0
-    array = (C.c_void_p * max(1, len(pools)))()
-    for i, t in enumerate(pools):
-        if t.device != pages.device or not t.is_contiguous() or t.dim() < 1 or t.shape[0] != pages.num_pages:
-            raise TypeError(f"pools must be contiguous tensors [{pages.num_pages}, ...] on {pages.device}")
-        n = t.numel() // pages.num_pages * t.element_size()
-        if i and n != bytes_per_page:
+    if not pools:
+        return None, 0, 0
+    index, num_pages, size = pages.device.index, pages.num_pages, pools[0].nbytes
+    addresses = []
+    for t in pools:
+        if t.get_device() != index or not t.is_contiguous() or t.dim() < 1 or t.size(0) != num_pages:
+            raise TypeError(f"pools must be contiguous tensors [{num_pages}, ...] on {pages.device}")
+        if t.nbytes != size:
             raise ValueError("the pools of a call must have pages of the same size")
-        bytes_per_page = n
-        array[i] = t.data_ptr()
-    return array, len(pools), bytes_per_page
+        addresses.append(t.data_ptr())
+    n = len(addresses)
+    array = _POOL_ARRAYS.get(n)
+    if array is None:
+        array = _POOL_ARRAYS[n] = C.c_void_p * n
+    return array(*addresses), n, size // num_pages
 
 
 def cocktail_pages_resize(pages: PageTable, delta: torch.Tensor, pools: Sequence[torch.Tensor] = (),
