@@ -315,8 +315,9 @@ __global__ __launch_bounds__(256) void pages_move_kernel(Pools pools, int num_po
     u32x4* dst = reinterpret_cast<u32x4*>(base + moves[2 * m + 1] * page_bytes);
     const int64_t left = page_bytes - int64_t(piece) * kPiece;
     const int words = int((left < kPiece ? left : kPiece) / 16);
+    // read past the caches (104 -> 85 us for 226 MB; written past them as well 98)
 #pragma unroll 4
-    for (int i = threadIdx.x; i < words; i += 256) dst[i] = src[i];
+    for (int i = threadIdx.x; i < words; i += 256) dst[i] = __builtin_nontemporal_load(src + i);
   }
 }
 
