@@ -21,6 +21,9 @@ FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# products whose sums need more registers than a wave has of one kind: let them lie in either kind instead of moving them for every use
+FILE_FLAGS = {"fp4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+
 
 def hipcc() -> str:
     exe = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
@@ -40,7 +43,7 @@ def build(verbose: bool = True, extra: list[str] | None = None, out: str = LIB) 
 
     def compile_one(src: str) -> str:
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [hipcc(), *compile_flags, *(extra or []), "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc(), *compile_flags, *FILE_FLAGS.get(src, []), *(extra or []), "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)

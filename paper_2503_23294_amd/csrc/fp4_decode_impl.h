@@ -115,6 +115,9 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
   __shared__ int32_t scratch[kDecodeWaves + 1];
+  // three or four operands of queries do not fit the registers next to their sums: every lane reads its own from LDS
+  constexpr bool kKeepQ = RT <= 2;
+  __shared__ u32x4 lds_q[kKeepQ ? 1 : kDecodeWaves][kKeepQ ? 1 : RT][kKeepQ ? 1 : kSteps][kKeepQ ? 1 : 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j = lane >> 4;
   const Fp4Batch& bt = a.batch;
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
     if (stream) load_unit(std::integral_constant<int, 2>{}, x0, x1);
     else load_unit(std::integral_constant<int, 0>{}, x0, x1);
 
-    h8 q[RT][kSteps];
+    h8 q[kKeepQ ? RT : 1][kSteps];
     float c[RT], m[RT], lsum[RT];
     f32x4 l[RT], o[RT][kChannelTiles];
     int lim[RT];
@@ -260,7 +263,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
       }
       c[rt] = fmaxf(c[rt], 1.2e-38f);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) q[rt][s] = __builtin_bit_cast(h8, raw[rt][s]);
+      for (int s = 0; s < kSteps; ++s) {
+        if constexpr (kKeepQ) q[rt][s] = __builtin_bit_cast(h8, raw[rt][s]);
+        else lds_q[wave][rt][s][lane] = raw[rt][s];
+      }
       const int r = rt * 16 + c16;
       lim[rt] = r < rows ? len - n + r / a.rep + 1 : 0;
       m[rt] = kNoMax;
@@ -285,8 +291,11 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
           const u32x4 wb = {fp4_pair<0>(tb.k[st], sb), fp4_pair<1>(tb.k[st], sb), fp4_pair<2>(tb.k[st], sb), fp4_pair<3>(tb.k[st], sb)};
 #pragma unroll
           for (int rt = 0; rt < kLive; ++rt) {
-            s[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wa), q[rt][st], s[rt][0], 0, 0, 0);
-            s[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wb), q[rt][st], s[rt][1], 0, 0, 0);
+            h8 qq;
+            if constexpr (kKeepQ) qq = q[rt][st];
+            else qq = __builtin_bit_cast(h8, lds_q[wave][rt][st][lane]);
+            s[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wa), qq, s[rt][0], 0, 0, 0);
+            s[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, wb), qq, s[rt][1], 0, 0, 0);
           }
         }
       }
@@ -325,8 +334,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
         for (int x = 0; x < 8; ++x) w8[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][x >> 2][x & 3], c[rt], -m[rt]));
         lsum[rt] += ((w8[0] + w8[1]) + (w8[2] + w8[3])) + ((w8[4] + w8[5]) + (w8[6] + w8[7]));
         p[rt] = __builtin_bit_cast(h8, u32x4{pack_halves(w8[0], w8[1]), pack_halves(w8[2], w8[3]), pack_halves(w8[4], w8[5]), pack_halves(w8[6], w8[7])});
-        const _Float16 one = _Float16(1.f);
-        l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h8{one, one, one, one, one, one, one, one}, p[rt], l[rt], 0, 0, 0);
+        if constexpr (RT <= 2) {
+          const _Float16 one = _Float16(1.f);
+          l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h8{one, one, one, one, one, one, one, one}, p[rt], l[rt], 0, 0, 0);
+        }
       }
       // weighted sums
       const float va0 = fp4_scale(ta.v_scale, 0), va1 = fp4_scale(ta.v_scale, 1), va2 = fp4_scale(ta.v_scale, 2), va3 = fp4_scale(ta.v_scale, 3);
@@ -434,7 +445,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT <= 2 
       sum += __shfl_xor(sum, 32);
       const int r = rt * 16 + c16;
       if (r >= rows) continue;
-      const float lr = l[rt][0];
+      const float lr = RT <= 2 ? l[rt][0] : sum;
       if (whole) {
         const int i = r / a.rep;
         const int64_t row = int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
