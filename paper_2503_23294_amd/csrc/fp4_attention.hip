@@ -30,12 +30,22 @@ __device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* 
       r.lsum += w * x[2];
     }
     const int n = parts - base < 64 ? parts - base : 64;
-#pragma unroll 8
-    for (int k = wave; k < n; k += waves) {
-      const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k));
-      const float* src = po + slot(base + k) * HD + lane * kPer;
+    // eight states at a time on their way; behind the last one it is the last one again, with no weight
+    for (int k = wave; k < n; k += 8 * waves) {
+      float x[8][kPer];
 #pragma unroll
-      for (int x = 0; x < kPer; ++x) r.o[x] += wk * src[x];
+      for (int i = 0; i < 8; ++i) {
+        const float* src = po + slot(base + min(k + i * waves, n - 1)) * HD + lane * kPer;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) x[i][y] = src[y];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = k + i * waves;
+        const float wk = at < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(at, n - 1))) : 0.f;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) r.o[y] += at < n ? wk * x[i][y] : 0.f;
+      }
     }
   }
 #pragma unroll
@@ -267,10 +277,13 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
   if (e == hipSuccess && s.decode && !s.whole) {
     const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;
-    // states that a row has, about: many of them are read by many waves at a time (40 heads, 51 states each: 8.8 us by four waves), a few by one
+    // states that a row has, about: many of them are read by many waves at a time (40 rows of 51 states: 8.8 us by four waves, 5.6 by sixteen; 1024 rows of
+    // 32: calls of 43.6 us by one wave a row, 36.9 by four; 3072 of 16: 60.5 and 62), a few by one
     const int parts = s.workers / (cache->pages.num_seqs * cache->num_kv_heads);
     if (parts >= 16 && most <= 512)
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
+    else if (parts >= 12 && most <= 3072)
+      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 4> : fp4_merge_decode_kernel<64, 4>, dim3(most), dim3(256), st, a, most_new);
     else
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 1> : fp4_merge_decode_kernel<64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
   }
