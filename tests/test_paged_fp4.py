@@ -158,7 +158,8 @@ class Batch:
         need = [-(-t // page) for t in lens]
         pages = sum(need) + spare
         ids = rng.permutation(pages).astype(np.int32)
-        table = np.full((len(lens), max(need + [1]) + 1), -1, np.int32)
+        # room for long contexts, so that calls that name no length are cut as for those
+        table = np.full((len(lens), max(max(need) + 1, 20000 // page)), -1, np.int32)
         at = 0
         for b, k in enumerate(need):
             table[b, :k] = ids[at:at + k]
@@ -328,11 +329,16 @@ CASES = [
     ([1500, 40, 333, 2], [1, 40, 7, 2], 2, 6, 128, 16),      # both kernels in one call
     ([500, 130], [500, 130], 2, 3, 128, 256),                # prompts
     ([257, 64, 1, 0, 191], [257, 64, 1, 0, 100], 1, 2, 64, 16),
-    ([2000], [33], 1, 1, 128, 16),                           # few rows, many keys: the keys of a row are cut
-    ([900, 3], [1, 1], 1, 64, 128, 16),                      # 64 heads per kv head: the tile kernel
-    ([3000, 10], [5, 10], 1, 40, 64, 80),
+    ([2000], [33], 1, 1, 128, 16),                           # few rows, many keys
+    ([900, 3], [1, 1], 1, 64, 128, 16),                      # 64 heads per kv head
+    ([3000, 10], [5, 10], 1, 40, 64, 80),                    # the keys of a row are cut
     ([100] * 70, [1] * 70, 1, 2, 128, 16),
     ([5] * 300, [1] * 300, 2, 2, 64, 16),
+    ([640, 33, 100, 0, 2000, 7], [1, 2, 3, 4, 4, 1], 2, 16, 128, 32),      # one to four operands in one call
+    ([640, 33, 100, 0, 2000, 7], [12, 2, 7, 4, 9, 1], 1, 5, 64, 16),
+    ([37 * i % 400 for i in range(90)], [1 + i % 3 for i in range(90)], 1, 16, 128, 16),   # the same, found in shared memory
+    ([150 + i % 7 for i in range(80)], [i % 80 for i in range(80)], 1, 2, 128, 16),         # prompts among many sequences
+    ([4100, 4096], [70, 65], 2, 2, 64, 64),
 ]
 
 
@@ -349,12 +355,55 @@ def test_attention(case, dtype):
     if uniform:
         calls.append(dict())
     calls.append(dict(starts=B.starts(new), max_new=max(new), max_len=max(lens)))
+    calls.append(dict(starts=B.starts(new), max_new=max(new), max_len=1))       # a bad guess
     for more in calls:
         out, lse = ck.cocktail_fp4_attention(B.cache, q, **more)
         B.check(q, new, out, lse)
         again, lse2 = ck.cocktail_fp4_attention(B.cache, q, **more)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
     assert torch.equal(B.pages.status.cpu(), torch.zeros(4, dtype=torch.int32))
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,new,rep", [([1100, 700], [512, 300], 32), ([700, 333], [700, 333], 24)])
+def test_attention_of_many_rows(lens, new, rep, d):
+    """Enough rows for workgroups of eight waves, and of four without cut keys."""
+    B = Batch(lens, 4, d, 48, torch.float16, seed=d, spread=2.0)
+    B.store_all()
+    q = B.query(new, rep)
+    out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=max(new), max_len=max(lens))
+    B.check(q, new, out, lse)
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 3, 100])
+def test_attention_over_a_cache_beyond_the_last_cache(new):
+    """285 MB of keys and values: read past the caches where a row's keys are read once.  Reference in binary64 on the device, from the cache's own
+    values (what they are is the store's test)."""
+    dev, t, h, d, rep = torch.device("cuda:0"), 262144 + 17, 8, 128, 4
+    pages = ck.PageTable(1, t, -(-t // 64), 64, dev)
+    cache = ck.Fp4Cache(pages, h, d)
+    ck.cocktail_pages_resize(pages, torch.tensor([t], dtype=torch.int32).to(dev))
+    k, v = (torch.randn(t, h, d, device=dev, dtype=torch.float16) for _ in range(2))
+    ck.cocktail_fp4_store(cache, k, v)
+    k, v = ck.cocktail_fp4_gather(cache, t)
+    q = torch.randn(new, h * rep, d, device=dev, dtype=torch.float16)
+    q[:, 0] = 3 * k[t // 2, 0]                        # a row that looks at one key
+    out, lse = ck.cocktail_fp4_attention(cache, q)
+    for i in range(h * rep):
+        kk, vv = k[:, i // rep].double(), v[:, i // rep].double()
+        s = q[:, i].double() @ kk.t() / math.sqrt(d)
+        s.masked_fill_(torch.arange(t, device=dev)[None] > torch.arange(t - new, t, device=dev)[:, None], -math.inf)
+        w = torch.softmax(s, dim=1)
+        want, mean_v = w @ vv, w @ vv.abs()
+        # the result's rounding; the weights', in the sum over V and in the normaliser (2^-11 each), with logits of up to 40 in size, whose products and
+        # sums in binary32 are off by 132 * 2^-24 * 40 = 3.2e-4, and sums over the keys in parts of a few thousand; weights that are fp16
+        # subnormals: 2^-25 of the largest each, against a sum of `total` largest
+        total = torch.exp(torch.logsumexp(s, dim=1) - s.amax(dim=1))
+        bound = 2.0 ** -11 * want.abs() + (2.0 ** -10 + 2 * 3.2e-4 + 4096 * 2.0 ** -24) * mean_v + (t * 2.0 ** -25 * vv.abs().max() / total)[:, None]
+        assert ((out[:, i].double() - want).abs() <= bound).all(), i
+        assert ((lse[:, i].double() - torch.logsumexp(s, dim=1)).abs() <= 3.2e-4 + 4096 * 2.0 ** -24 + 2.0 ** -17).all()
 
 
 @gpu
