@@ -163,10 +163,10 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
     // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 300, 1000, 2048 tokens 12.2, 12.2, 11.5 us in two launches,
-    // 5.7, 7.5, 10.9 in one; 4096: 12.0 and 17.9), and up to 6K where the segments fill the chip by themselves, once or twice (128, 256, 512
-    // of 4096 tokens: 23.0, 32.6, 57.3 and 19.5, 25.7, 49.2; 512 of 8192: 104 and 109; 1024 of 4096: 105 and 112).
+    // 5.7, 7.5, 10.8 in one; 4096: 12.0 and 17.9), and up to 6K where the segments fill the chip by themselves (128, 256, 512, 1024 of 4096 tokens:
+    // 23.0, 32.6, 57.3, 104.7 and 19.6, 25.5, 46.7, 101.5; of 8192 the same within 3 %, but there one long sequence among short ones would be waited for).
     const int64_t segments = seqs * c->num_kv_heads;
-    s.whole = s.row_tiles == 1 && max_len <= (segments >= 128 && segments <= 512 ? 6144 : 2048);
+    s.whole = s.row_tiles == 1 && max_len <= (segments >= 128 ? 6144 : 2048);
     if (s.whole) workers = 0;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
