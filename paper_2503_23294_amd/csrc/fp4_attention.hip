@@ -9,6 +9,18 @@
 
 namespace cocktail {
 
+// The sequence of new token t: the last one that does not start behind it (those before it with the same start are empty).
+__device__ __forceinline__ int seq_of_row(const Fp4Batch& bt, int t) {
+  if (!bt.starts) return t / bt.uniform;
+  int b = 0, e = bt.num_seqs;
+  while (e - b > 1) {
+    const int mid = (b + e) >> 1;
+    if (bt.starts[mid] <= t) b = mid;
+    else e = mid;
+  }
+  return b;
+}
+
 // Sum of a row's partial states: `parts` of them, the first at row `first_slot` of the arrays and the others at second_slot, second_slot + step ...
 // Wave `wave` of `waves` takes every waves-th; o: the lane's channels, l and lsum: whole sums (in every wave).
 template <int HD>
@@ -57,7 +69,8 @@ __device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* 
 }
 
 // Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves of its segment left, if there were several, and
-// writes rows without keys.  WAVES waves for a row, at least four to a workgroup.
+// writes rows without keys.  WAVES waves for a row, at least four to a workgroup.  Numbered by sequence, most_new tokens each, or, where most of those
+// would have no token, by new token (most_new 0), which is looked for among the sequences.
 template <int HD, int WAVES>
 __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode_kernel(Fp4Attention a, int most_new) {
   constexpr int kPer = HD / 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
@@ -67,11 +80,12 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode
   const uint32_t heads = bt.num_kv_heads * a.rep;
   const uint32_t number = blockIdx.x * kRows + (WAVES < 4 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0);
   const uint32_t hq = number % heads, bi = number / heads;
-  const int b = bi / uint32_t(most_new), i = bi % uint32_t(most_new);
-  if (b >= bt.num_seqs) return;   // (kRows > 1 only, where nobody waits for anybody)
+  if (bi >= uint32_t(most_new ? bt.num_seqs * most_new : bt.total)) return;   // (kRows > 1 only, where nobody waits for anybody)
+  const int b = most_new ? bi / uint32_t(most_new) : seq_of_row(bt, bi);
   const uint32_t before = a.prefix[b], total = a.prefix[bt.num_seqs];
   const Fp4Seq s = decode_seq(a, b);
-  if (i >= s.n) return;
+  const int i = most_new ? bi % uint32_t(most_new) : int(bi) - s.first;
+  if (i < 0 || i >= s.n) return;
   const uint32_t h = hq / uint32_t(a.rep);
   const int64_t row = int64_t(s.first + i) * heads + hq;
   const uint32_t units = decode_units(s), per_unit = decode_operands(a, s);
@@ -109,18 +123,7 @@ __global__ __launch_bounds__(256) void fp4_merge_tiles_kernel(Fp4Attention a) {
   const int heads = bt.num_kv_heads * a.rep;
   const int row = __builtin_amdgcn_readfirstlane(int(blockIdx.x * 4 + (threadIdx.x >> 6)));
   if (row >= bt.total * heads) return;
-  const int t = row / heads;
-  int b = 0;
-  if (bt.starts) {
-    int e = bt.num_seqs;   // the last sequence that does not start behind t (those before it with the same start are empty)
-    while (e - b > 1) {
-      const int mid = (b + e) >> 1;
-      if (bt.starts[mid] <= t) b = mid;
-      else e = mid;
-    }
-  } else {
-    b = t / bt.uniform;
-  }
+  const int t = row / heads, b = seq_of_row(bt, t);
   const Fp4Span s = fp4_span(bt, b);
   // not the rows of a sequence with a bad range, or of the decode kernel
   if (t < s.first || t >= s.first + s.count || s.count * a.rep <= a.decode_rows) return;
@@ -138,6 +141,7 @@ namespace {
 struct Split {
   bool decode, whole, tiles;
   int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
+  int64_t active;   // sequences that have queries at most
   size_t prefix_bytes, part_rows, tile_rows, bytes;
 };
 
@@ -146,6 +150,7 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
   if (max_len <= 0 || max_len > capacity) max_len = capacity;
   const int64_t most_rows = max_new * rep;
+  s.active = c->pages.num_seqs < total ? c->pages.num_seqs : total;
   // a batch may hold sequences for either kernel unless every sequence has the same number of queries
   s.tiles = most_rows > kDecodeRows;
   s.decode = !s.tiles || (!uniform && rep <= kDecodeRows);
@@ -156,7 +161,7 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
     // queries (8 x 16K, 32 rows: 2048 waves 53 us, 1024 48 us; their states are larger and the matrix cores have more to do); and four units at
     // least for a wave, at half a microsecond each: with fewer the states cost more than that (8 heads, 16K: 2, 4, 8 units 20.8, 15.4, 15.0 us;
     // 2K: 10.2, 10.9, 14.7).
-    const int64_t seqs = c->pages.num_seqs < total ? c->pages.num_seqs : total;
+    const int64_t seqs = s.active;
     const int64_t units = seqs * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
     int64_t workers = (units + 3) / 4;
     const int64_t fill = s.row_tiles == 1 ? 2048 : 1024;
@@ -267,7 +272,7 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1, false>, fp4_decode_kernel<64, 2, false>, fp4_decode_kernel<64, 3, false>, fp4_decode_kernel<64, 4, false>},
                                          {fp4_decode_kernel<128, 1, false>, fp4_decode_kernel<128, 2, false>, fp4_decode_kernel<128, 3, false>, fp4_decode_kernel<128, 4, false>}};
     if (s.whole)
-      e = launch(hd == 128 ? fp4_decode_kernel<128, 1, true> : fp4_decode_kernel<64, 1, true>, dim3(cache->pages.num_seqs * cache->num_kv_heads), dim3(64 * kWholeWaves), st, a);
+      e = launch(hd == 128 ? fp4_decode_kernel<128, 1, true> : fp4_decode_kernel<64, 1, true>, dim3(uint32_t(s.active) * cache->num_kv_heads), dim3(64 * kWholeWaves), st, a);
     else
       e = launch_lds(kernels[hd == 128][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }
@@ -275,11 +280,12 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     e = launch(s.tile_waves == 8 ? (hd == 128 ? fp4_tile_kernel<128, 8> : fp4_tile_kernel<64, 8>) : (hd == 128 ? fp4_tile_kernel<128, 4> : fp4_tile_kernel<64, 4>),
                dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * s.tile_waves), st, a);
   if (e == hipSuccess && s.decode && !s.whole) {
-    const int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
-    const uint32_t most = uint32_t(cache->pages.num_seqs) * most_new * num_q_heads;
+    int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
+    if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
+    const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;
     // states that a row has, about: many of them are read by many waves at a time (40 rows of 51 states: 8.8 us by four waves, 5.6 by sixteen; 1024 rows of
     // 32: calls of 43.6 us by one wave a row, 36.9 by four; 3072 of 16: 60.5 and 62), a few by one
-    const int parts = s.workers / (cache->pages.num_seqs * cache->num_kv_heads);
+    const int parts = int(s.workers / (s.active * cache->num_kv_heads));
     if (parts >= 16 && most <= 512)
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
     else if (parts >= 12 && most <= 3072)

@@ -110,12 +110,35 @@ __device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4L
 // Held to 128 registers, so that two of them run on a compute unit (1024 segments of 2048 tokens: 54.2 -> 47.4 us).
 constexpr int kWholeWaves = 8;
 
+// The number-th sequence that has queries for this kernel, or -1; for a workgroup of kWholeWaves waves, `lds`: kWholeWaves + 1 words.
+__device__ __forceinline__ int nth_active(const Fp4Attention& a, int number, int32_t* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int run = 0;
+  if (threadIdx.x == 0) lds[kWholeWaves] = -1;
+  for (int base = 0; base < a.batch.num_seqs && run <= number; base += 64 * kWholeWaves) {
+    const int b = base + int(threadIdx.x);
+    const bool active = b < a.batch.num_seqs && decode_seq(a, b).n > 0;
+    const uint64_t mask = __ballot(active);
+    __syncthreads();
+    if (lane == 0) lds[wave] = __builtin_popcountll(mask);
+    __syncthreads();
+    int before = run;
+    for (int w = 0; w < kWholeWaves; ++w) {
+      if (w < wave) before += lds[w];
+      run += lds[w];
+    }
+    if (active && before + __builtin_popcountll(mask & ((uint64_t(1) << lane) - 1)) == number) lds[kWholeWaves] = b;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(lds[kWholeWaves]);
+}
+
 template <int HD, int RT, bool WHOLE>
 __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 4 : RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
-  __shared__ int32_t scratch[kDecodeWaves + 1];
+  __shared__ int32_t lds_words[kWholeWaves + 1];
   // three or four operands of queries do not fit the registers next to their sums: every lane reads its own from LDS
   constexpr bool kKeepQ = RT <= 2;
   __shared__ u32x4 lds_q[kKeepQ ? 1 : kDecodeWaves][kKeepQ ? 1 : RT][kKeepQ ? 1 : kSteps][kKeepQ ? 1 : 64];
@@ -127,7 +150,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
   uint32_t u = 0, end = 1;
   bool stream = false;
   if constexpr (!WHOLE) {
-    line = make_line(a, pre, scratch);
+    line = make_line(a, pre, lds_words);
     const uint32_t share = cost_share(line.total, a.workers);
     w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
     u = w * share;
@@ -151,8 +174,11 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     Fp4Place place;
     int h, u0, u1;
     if constexpr (WHOLE) {
-      place.b = int(blockIdx.x) / bt.num_kv_heads;
-      h = int(blockIdx.x) - place.b * bt.num_kv_heads;
+      const int number = int(blockIdx.x) / bt.num_kv_heads;
+      h = int(blockIdx.x) - number * bt.num_kv_heads;
+      // more sequences than rows: the workgroups are for those that have any
+      place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
+      if (place.b < 0) return;
       const Fp4Seq s = decode_seq(a, place.b);
       place.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
       if (place.seq.n == 0) return;

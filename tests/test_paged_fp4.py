@@ -377,6 +377,24 @@ def test_attention_of_many_rows(lens, new, rep, d):
 
 
 @gpu
+@pytest.mark.parametrize("num_seqs", [70, 1500, 4096])
+def test_few_active_sequences_in_a_large_table(num_seqs):
+    """A table with room for many sequences, of which a few generate: one of them has no key, one many queries."""
+    rng = np.random.default_rng(num_seqs)
+    active = np.sort(rng.choice(num_seqs, 6, replace=False))
+    lens, new = np.zeros(num_seqs, int), np.zeros(num_seqs, int)
+    lens[active], new[active] = [300, 0, 77, 1000, 16, 130], [1, 1, 2, 1, 1, 1]
+    for most in (2, 60):
+        new[active[-1]] = most - 1
+        B = Batch(lens.tolist(), 2, 64, 16, torch.float16, seed=num_seqs)
+        B.store_all()
+        q = B.query(new.tolist(), 4)
+        for max_len in (1000, 0):
+            out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new.tolist()), max_new=most, max_len=max_len)
+            B.check(q, new.tolist(), out, lse)
+
+
+@gpu
 @pytest.mark.parametrize("new", [1, 3, 100])
 def test_attention_over_a_cache_beyond_the_last_cache(new):
     """285 MB of keys and values: read past the caches where a row's keys are read once.  Reference in binary64 on the device, from the cache's own
