@@ -561,7 +561,7 @@ int cocktail_pages_check(const cocktail_page_table* pages, void* stream);
  * Value of a code: exact in fp16 and bf16.  Beyond 49152 = 6 * 2^13 values saturate (infinities too); NaN is stored as 0.
  */
 typedef struct cocktail_fp4_cache {
-  cocktail_page_table pages; /* page_size a multiple of 16 up to 65536                                */
+  cocktail_page_table pages; /* page_size a multiple of 16 up to 65536, table_stride * page_size <= 2^31 - 256 */
   void* pool;                /* DEVICE num_pages pages of cocktail_fp4_page_bytes, 16-byte aligned    */
   int32_t num_kv_heads;
   int32_t head_dim;          /* 64 or 128                                                             */
@@ -602,8 +602,8 @@ int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32
  * starts[b] queries and len = seq_lens[b], query i of sequence b attends to tokens 0 .. len - n + i.  One query per sequence is a
  * decode step, some are the verification of drafts, many a prompt or a part of one; a batch may mix them.
  *     out[t,h] = softmax(sm_scale * q[t,h] . K^T) V,   kv head h / (num_q_heads / num_kv_heads)
- * Products and sums in binary32, K and V as stored, softmax weights rounded to fp16 (relative 2^-12) relative to a maximum that is
- * at most 2^8 too small.  bf16 queries are used as fp16 times a power of two of their own (exact, but for channels below 2^-14
+ * Products and sums in binary32, K and V as stored, softmax weights rounded to fp16 (relative 2^-11) relative to a maximum that may be
+ * too small by as much as fp16 can hold (2^14).  bf16 queries are used as fp16 times a power of two of their own (exact, but for channels below 2^-14
  * of the largest).
  *
  *   q         DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d, strides multiples of 8

@@ -157,7 +157,7 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
   s.row_tiles = (s.rows + 15) / 16;
   if (s.decode) {
-    // Two waves per SIMD of 256 compute units (128K, 40 heads: 1024, 2048, 3072 waves 116, 111, 113 us), one where a wave has more than one operand of
+    // Two waves per SIMD of 256 compute units (128K, 40 heads: 1024 waves 116 us, 2048 111, half as many again 113), one where a wave has more than one operand of
     // queries (8 x 16K, 32 rows: 2048 waves 53 us, 1024 48 us; their states are larger and the matrix cores have more to do); and four units at
     // least for a wave, at half a microsecond each: with fewer the states cost more than that (8 heads, 16K: 2, 4, 8 units 20.8, 15.4, 15.0 us;
     // 2K: 10.2, 10.9, 14.7).
@@ -284,11 +284,11 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
     const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;
     // states that a row has, about: many of them are read by many waves at a time (40 rows of 51 states: 8.8 us by four waves, 5.6 by sixteen; 1024 rows of
-    // 32: calls of 43.6 us by one wave a row, 36.9 by four; 3072 of 16: 60.5 and 62), a few by one
+    // 32: calls of 43.6 us by one wave a row, 36.9 by four; three times as many rows of 16: 60.5 and 62), a few by one
     const int parts = int(s.workers / (s.active * cache->num_kv_heads));
     if (parts >= 16 && most <= 512)
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
-    else if (parts >= 12 && most <= 3072)
+    else if (parts >= 12 && most <= 2048)
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 4> : fp4_merge_decode_kernel<64, 4>, dim3(most), dim3(256), st, a, most_new);
     else
       e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 1> : fp4_merge_decode_kernel<64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);

@@ -136,6 +136,21 @@ def test_refusals_of_attention():
     assert call(total=0, max_new=0) == 0
 
 
+def test_refusals_of_what_32_bits_do_not_number():
+    """Positions near 2^31, and launches of 2^32 threads."""
+    L = _lib.lib()
+    n = C.c_size_t(0)
+    far, near = _cache_desc(table_stride=(1 << 27) - 1), _cache_desc(num_seqs=1, table_stride=(1 << 27) - 16)
+    assert L.cocktail_fp4_store(C.byref(far), 4096, 4096, 0, 256, 128, 8, 4096, None) == _lib.EINVAL
+    assert L.cocktail_fp4_gather(C.byref(far), 4096, 4096, 0, 256, 128, 8, 4096, None) == _lib.EINVAL
+    assert L.cocktail_fp4_attention_workspace(C.byref(far), 4, 8, 8, 0, 0, C.byref(n)) == _lib.EINVAL
+    assert L.cocktail_fp4_attention_workspace(C.byref(near), 4, 8, 8, 0, 0, C.byref(n)) == 0
+    wide = _cache_desc(heads=512)
+    for fn in (L.cocktail_fp4_store, L.cocktail_fp4_gather):
+        assert fn(C.byref(wide), 4096, 4096, 0, 512 * 128, 128, 1 << 22, 4096, None) == _lib.EINVAL   # 2^20 quads of 2^14 threads
+        assert b"more than one launch" in L.cocktail_last_error()
+
+
 def test_the_binding_wants_device_tensors():
     with pytest.raises(TypeError):
         ck.PageTable(2, 64, 8, 16, torch.device("cpu"))
@@ -764,6 +779,53 @@ def test_calls_on_another_stream():
     ck.cocktail_pages_check(B.pages, stream=s)
     B.check(q, [1, 1], out, lse)
     assert np.array_equal(_f64(k), O.value(_f64(B.k)))
+
+
+@gpu
+def test_calls_and_graphs_on_two_streams_at_once():
+    """Two streams read one cache at the same time, eagerly and by graphs that are replayed side by side: nothing is shared but the cache."""
+    B = Batch([5000, 3000, 700, 40], 4, 128, 16, torch.float16, seed=33)
+    B.store_all()
+    new = [4, 1, 3, 2]
+    starts = B.starts(new)
+    queries = [B.query(new, 8), B.query(new, 8)]
+    call = lambda q: ck.cocktail_fp4_attention(B.cache, q, starts, max_new=4, max_len=5000)  # noqa: E731
+    want = [call(q)[0].clone() for q in queries]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = []
+        for s, q in zip(streams, queries):
+            with torch.cuda.stream(s):
+                got.append([call(q)[0] for _ in range(3)])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, want[i]) for i in range(2) for x in got[i])
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for g, s, q in zip(graphs, streams, queries):
+        with torch.cuda.graph(g, stream=s):
+            outs.append(call(q)[0])
+    for _ in range(10):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = call(queries[0])[0]
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[0]) and all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+@gpu
+def test_most_sequences_with_most_rows():
+    """4096 sequences, of which one needs four operands of queries of 128 channels: the most shared memory that a workgroup asks for."""
+    lens, new = [5] * 4096, [0] * 4096
+    lens[1234], new[1234], new[4000] = 700, 3, 1
+    B = Batch(lens, 1, 128, 16, torch.float16, seed=34)
+    B.store_all()
+    q = B.query(new, 20)
+    out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=3)
+    B.check(q, new, out, lse)
 
 
 @gpu
