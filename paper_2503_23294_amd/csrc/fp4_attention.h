@@ -13,6 +13,7 @@ constexpr float kMaxSlack = 8.0f;       // a reference maximum may be this much 
 constexpr int kUnit = 32;               // tokens that a wave of the decode kernel takes at a time
 constexpr int kDecodeRows = 64;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
 constexpr int kDecodeWaves = 4;         // waves per workgroup there
+constexpr int kComputeUnits = 256;
 constexpr int kTileKeys = 64;           // keys per step of the tile kernel
 constexpr uint64_t kCachedBytes = 256u << 20;   // the last cache before the memory
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

@@ -135,6 +135,31 @@ __device__ __forceinline__ int nth_active(const Fp4Attention& a, int number, int
   return __builtin_amdgcn_readfirstlane(lds[kWholeWaves]);
 }
 
+// The number-th longest of up to 64 sequences, for a workgroup of kWholeWaves waves: a lane has a sequence, a wave counts which of its share of them are
+// longer.  Those without queries come last.
+__device__ __forceinline__ int nth_longest(const Fp4Attention& a, int number, Fp4Seq* seq) {
+  constexpr int kShare = 64 / kWholeWaves;
+  __shared__ int counted[kWholeWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Fp4Seq s = {};
+  uint32_t key = 0;
+  if (lane < a.batch.num_seqs) {
+    s = decode_seq(a, lane);
+    const uint32_t units = s.n > 0 ? decode_units(s) + 1 : 0, most = (1u << 25) - 1;
+    key = (units < most ? units : most) << 6 | uint32_t(63 - lane);   // no two alike
+  }
+  int longer = 0, before = 0;
+#pragma unroll
+  for (int c = 0; c < kShare; ++c) longer += uint32_t(__builtin_amdgcn_readlane(int(key), wave * kShare + c)) > key ? 1 : 0;
+  counted[wave][lane] = longer;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWholeWaves; ++w) before += counted[w][lane];
+  const int b = __builtin_ctzll(__ballot(lane < a.batch.num_seqs && before == number));
+  *seq = {__builtin_amdgcn_readlane(s.first, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.len, b)};
+  return b;
+}
+
 template <int HD, int RT, bool WHOLE>
 __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 4 : RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
@@ -176,13 +201,25 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     Fp4Place place;
     int h, u0, u1;
     if constexpr (WHOLE) {
-      const int number = int(blockIdx.x) / bt.num_kv_heads;
-      h = int(blockIdx.x) - number * bt.num_kv_heads;
-      // more sequences than rows: the workgroups are for those that have any
-      place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
-      if (place.b < 0) return;
-      const Fp4Seq s = decode_seq(a, place.b);
-      place.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+      const int grid = gridDim.x;
+      int at = blockIdx.x;
+      if (bt.num_seqs <= 64 && grid > kComputeUnits) {
+        // two workgroups to a compute unit: the longest segments first, then beside them the shortest, then the others (64 sequences of 512 ..
+        // 4097 tokens, 8 heads: 41.7 -> 37.4 us; all of the same length 35.3 -> 35.6)
+        const int second = grid < 2 * kComputeUnits ? grid : 2 * kComputeUnits;
+        if (at >= kComputeUnits && at < second) at = kComputeUnits + second - 1 - at;
+        const int number = at / bt.num_kv_heads;
+        h = at - number * bt.num_kv_heads;
+        place.b = nth_longest(a, number, &place.seq);
+      } else {
+        const int number = at / bt.num_kv_heads;
+        h = at - number * bt.num_kv_heads;
+        // more sequences than rows: the workgroups are for those that have any
+        place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
+        if (place.b < 0) return;
+        const Fp4Seq s = decode_seq(a, place.b);
+        place.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+      }
       if (place.seq.n == 0) return;
       const uint32_t units = decode_units(place.seq);
       u0 = units * wave / kWholeWaves;

@@ -410,6 +410,21 @@ def test_few_active_sequences_in_a_large_table(num_seqs):
 
 
 @gpu
+@pytest.mark.parametrize("num_seqs,heads", [(40, 8), (64, 9), (33, 31), (64, 4), (65, 8)])
+def test_many_segments_of_unlike_lengths(num_seqs, heads):
+    """More short segments than compute units, in the order of their lengths: lengths that are alike or zero, sequences without queries."""
+    rng = np.random.default_rng(num_seqs)
+    lens = rng.choice([0, 1, 31, 32, 33, 64, 100, 257, 700], num_seqs)
+    new = (rng.random(num_seqs) < 0.8).astype(int)
+    new[lens == 0] = [1 - i % 2 for i in range(int((lens == 0).sum()))]
+    B = Batch(lens.tolist(), heads, 64, 32, torch.bfloat16, seed=heads)
+    B.store_all()
+    q = B.query(new.tolist(), 2)
+    out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new.tolist()), max_new=1, max_len=700)
+    B.check(q, new.tolist(), out, lse)
+
+
+@gpu
 @pytest.mark.parametrize("new", [1, 3, 100])
 def test_attention_over_a_cache_beyond_the_last_cache(new):
     """285 MB of keys and values: read past the caches where a row's keys are read once.  Reference in binary64 on the device, from the cache's own
