@@ -47,16 +47,18 @@ __device__ __forceinline__ Fp4Seq decode_seq(const Fp4Attention& a, int b) {
   return {s.first, s.count * a.rep <= a.decode_rows ? s.count : 0, fp4_len(a.batch, b)};
 }
 
-// Operands of 16 query rows that a sequence needs in the decode kernel, its units of keys, and what they cost: a unit takes about as long as it has
-// operands (8 x 16K: 0.7, 1.2, 1.9 and 2.4 us with one to four).
+// Operands of 16 query rows that a sequence needs in the decode kernel, its units of keys, and what they cost: the conversions of K and V
+// once, and products and weights per operand, each about as long (8 x 16K, 1 .. 6 tokens of 8 heads: 55.6 us by operands alone, 47.4 by operands + 1,
+// 49.4 by operands + 2).
 __device__ __forceinline__ int decode_operands(const Fp4Attention& a, const Fp4Seq& s) { return (s.n * a.rep + 15) >> 4; }
 __device__ __forceinline__ int decode_units(const Fp4Seq& s) { return s.n > 0 ? (s.len + kUnit - 1) / kUnit : 0; }
-__device__ __forceinline__ int decode_cost(const Fp4Attention& a, const Fp4Seq& s) { return decode_units(s) * decode_operands(a, s); }
+__device__ __forceinline__ int unit_cost(const Fp4Attention& a, const Fp4Seq& s) { return decode_operands(a, s) + 1; }
+__device__ __forceinline__ int decode_cost(const Fp4Attention& a, const Fp4Seq& s) { return decode_units(s) * unit_cost(a, s); }
 
-// A wave's share of the cost: not less than a unit's, so that a segment has units in every share that lies between its first and its last.
+// A wave's share of the cost: not less than the dearest unit's, so that a segment has units in every share that lies between its first and its last.
 __device__ __forceinline__ uint32_t cost_share(uint32_t cost, int workers) {
   const uint32_t n = (cost + uint32_t(workers) - 1) / uint32_t(workers);
-  return n < 4 ? 4 : n;
+  return n < 5 ? 5 : n;
 }
 
 __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode
   if (i < 0 || i >= s.n) return;
   const uint32_t h = hq / uint32_t(a.rep);
   const int64_t row = int64_t(s.first + i) * heads + hq;
-  const uint32_t units = decode_units(s), per_unit = decode_operands(a, s);
+  const uint32_t units = decode_units(s), per_unit = unit_cost(a, s);
   Merged<HD> r = {};
   if (units > 0) {
     // the waves that the segment's first and last unit belong to
@@ -157,14 +157,14 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
   s.row_tiles = (s.rows + 15) / 16;
   if (s.decode) {
-    // Two waves per SIMD of 256 compute units (128K, 40 heads: 1024 waves 116 us, 2048 111, half as many again 113), one where a wave has more than one operand of
-    // queries (8 x 16K, 32 rows: 2048 waves 53 us, 1024 48 us; their states are larger and the matrix cores have more to do); and four units at
+    // Two waves per SIMD of 256 compute units (128K, 40 heads: 1024 waves 116 us, 2048 111, half as many again 113; 8 x 16K, 32 rows: 1024 waves 47.5 us, 2048
+    // 44.4), one where a wave has three or four operands of queries and needs all registers; and four units at
     // least for a wave, at half a microsecond each: with fewer the states cost more than that (8 heads, 16K: 2, 4, 8 units 20.8, 15.4, 15.0 us;
     // 2K: 10.2, 10.9, 14.7).
     const int64_t seqs = s.active;
     const int64_t units = seqs * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
     int64_t workers = (units + 3) / 4;
-    const int64_t fill = s.row_tiles == 1 ? 2048 : 1024;
+    const int64_t fill = s.row_tiles <= 2 ? 2048 : 1024;
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
     // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 300, 1000, 2048 tokens 12.2, 12.2, 11.5 us in two launches,
@@ -210,7 +210,7 @@ int check_attention(const cocktail_fp4_cache* c, int32_t num_q_heads, int64_t to
   if (total < 0 || total * num_q_heads > (int64_t(1) << 30)) return fail(COCKTAIL_EINVAL, "total %lld is negative or too many for %d heads", (long long)total, num_q_heads);
   if (total && (max_new < 1 || max_new > total)) return fail(COCKTAIL_EINVAL, "max_new %d is not in 1 .. total (%lld)", max_new, (long long)total);
   const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
-  if (double(c->pages.num_seqs) * ((capacity + kUnit - 1) / kUnit) * c->num_kv_heads > 1.07e9)   // (costs, up to four times that, are 32 bits wide)
+  if (double(c->pages.num_seqs) * ((capacity + kUnit - 1) / kUnit) * c->num_kv_heads > 8.5e8)   // (costs, up to five times that, are 32 bits wide)
     return fail(COCKTAIL_EINVAL, "%d sequences of up to %lld tokens are too many for one call", c->pages.num_seqs, (long long)capacity);
   return COCKTAIL_OK;
 }

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     // read once and not again before hundreds of MB have passed: past the caches, which then read faster (128K, 40 heads: 130 -> 111 us); what
     // fits them is left to them (64 sequences of up to 4K, 8 heads, again and again: 38 us, and 42 past the caches).  With more than one
     // operand of queries the memory is not what is waited for.
-    stream = RT == 1 && uint64_t(line.total) * (kUnit * 17 / 16 * HD) > kCachedBytes;
+    stream = RT == 1 && uint64_t(line.total) / 2 * (kUnit * 17 / 16 * HD) > kCachedBytes;
   }
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
       place = find_place(a, line, pre, u);
     }
     const int b = place.b, n = place.seq.n, len = place.seq.len, rows = n * a.rep;
-    const uint32_t per_unit = decode_operands(a, place.seq);
+    const uint32_t operands = decode_operands(a, place.seq), per_unit = operands + 1;
     if constexpr (!WHOLE) {
       const uint32_t cost = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
       h = local / cost;
@@ -457,9 +457,9 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
       else walk(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
     } else {
       const std::integral_constant<int, 0> cached;
-      if (per_unit == 1) walk(cached, std::integral_constant<int, 1>{});
-      else if (RT == 2 || per_unit == 2) walk(cached, std::integral_constant<int, 2>{});
-      else if (RT == 3 || per_unit == 3) walk(cached, std::integral_constant<int, (RT < 3 ? RT : 3)>{});
+      if (operands == 1) walk(cached, std::integral_constant<int, 1>{});
+      else if (RT == 2 || operands == 2) walk(cached, std::integral_constant<int, 2>{});
+      else if (RT == 3 || operands == 3) walk(cached, std::integral_constant<int, (RT < 3 ? RT : 3)>{});
       else walk(cached, std::integral_constant<int, RT>{});
     }
 
