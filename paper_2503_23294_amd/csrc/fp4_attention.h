@@ -6,6 +6,7 @@
 
 namespace cocktail {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kNoMax = -3.0e38f;      // reference maximum of a row that has seen no key

@@ -168,7 +168,7 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
     // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 300, 1000, 2048 tokens 12.2, 12.2, 11.5 us in two launches,
-    // 5.7, 7.5, 10.8 in one; 4096: 12.0 and 17.9), and up to 6K where the segments fill the chip by themselves (128, 256, 512, 1024 of 4096 tokens:
+    // 4.5, 6.7, 9.4 in one; 4096: 11.9 and 15.3), and up to 6K where the segments fill the chip by themselves (128, 256, 512, 1024 of 4096 tokens:
     // 23.0, 32.6, 57.3, 104.7 and 19.6, 25.5, 46.7, 101.5; of 8192 the same within 3 %, but there one long sequence among short ones would be waited for).
     const int64_t segments = seqs * c->num_kv_heads;
     s.whole = s.row_tiles == 1 && max_len <= (segments >= 128 ? 6144 : 2048);
@@ -271,8 +271,14 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     typedef void (*Kernel)(Fp4Attention);
     static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1, false>, fp4_decode_kernel<64, 2, false>, fp4_decode_kernel<64, 3, false>, fp4_decode_kernel<64, 4, false>},
                                          {fp4_decode_kernel<128, 1, false>, fp4_decode_kernel<128, 2, false>, fp4_decode_kernel<128, 3, false>, fp4_decode_kernel<128, 4, false>}};
+    const int64_t segments = s.active * cache->num_kv_heads;
+    // Few segments leave most of the chip idle while their compute units convert and multiply: four workgroups to a segment, each for a quarter of the
+    // channels of V, all with the logits of their own (8 segments of 1000, 2048 tokens: 7.6, 10.9 -> 6.7, 9.4 us; 32: 7.7, 11.2 -> 6.9, 10.3; 64: 7.9, 11.4 ->
+    // 8.0, 14.8, for everything is read four times; halves of 64 channels: the same as whole ones)
+    const bool quarters = segments <= 32 && hd == 128;
     if (s.whole)
-      e = launch(hd == 128 ? fp4_decode_kernel<128, 1, true> : fp4_decode_kernel<64, 1, true>, dim3(uint32_t(s.active) * cache->num_kv_heads), dim3(64 * kWholeWaves), st, a);
+      e = launch(quarters ? fp4_decode_kernel<128, 1, true, 4> : hd == 128 ? fp4_decode_kernel<128, 1, true> : fp4_decode_kernel<64, 1, true>,
+                 dim3(uint32_t(segments) * (quarters ? 4 : 1)), dim3(64 * kWholeWaves), st, a);
     else
       e = launch_lds(kernels[hd == 128][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, a);
   }

@@ -109,7 +109,8 @@ __device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4L
 }
 
 // WHOLE: a workgroup of kWholeWaves waves has one segment and shares it out among them, their states are joined in LDS: one launch, for short contexts.
-// Held to 128 registers, so that two of them run on a compute unit (1024 segments of 2048 tokens: 54.2 -> 47.4 us).
+// Held to 128 registers, so that two of them run on a compute unit (1024 segments of 2048 tokens: 54.2 -> 47.4 us).  SPLIT: as many workgroups have a
+// segment, each for its part of the channels of V.
 constexpr int kWholeWaves = 8;
 
 // The number-th sequence that has queries for this kernel, or -1; for a workgroup of kWholeWaves waves, `lds`: kWholeWaves + 1 words.
@@ -160,10 +161,10 @@ __device__ __forceinline__ int nth_longest(const Fp4Attention& a, int number, Fp
   return b;
 }
 
-template <int HD, int RT, bool WHOLE>
+template <int HD, int RT, bool WHOLE, int SPLIT = 1>
 __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 4 : RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
-  constexpr int kChannelTiles = HD / 16;
+  constexpr int kChannelTiles = HD / 16 / SPLIT;   // of a wave's output
   extern __shared__ int32_t pre[];
   __shared__ int32_t lds_words[kWholeWaves + 1];
   // three or four operands of queries do not fit the registers next to their sums: every lane reads its own from LDS
@@ -189,6 +190,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     // operand of queries the memory is not what is waited for.
     stream = RT == 1 && uint64_t(line.total) / 2 * (kUnit * 17 / 16 * HD) > kCachedBytes;
   }
+  const int own_part = SPLIT > 1 ? int(blockIdx.x % SPLIT) : 0;
   const int P = bt.page_size;
   const int64_t run = fp4_run_bytes(HD, P);
   // byte offsets of a lane's pieces in 16 tokens
@@ -202,8 +204,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     Fp4Place place;
     int h, u0, u1;
     if constexpr (WHOLE) {
-      const int grid = gridDim.x;
-      int at = blockIdx.x;
+      const int grid = gridDim.x / SPLIT;
+      int at = blockIdx.x / SPLIT;
       if (bt.num_seqs <= 64 && grid > kComputeUnits) {
         // two workgroups to a compute unit: the longest segments first, then beside them the shortest, then the others (64 sequences of 512 ..
         // 4097 tokens, 8 heads: 41.7 -> 37.4 us; all of the same length 35.3 -> 35.6)
@@ -424,14 +426,14 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
         }
       };
       uint32_t a0 = ta.v[0], a1 = ta.v[1], a2 = ta.v[2], a3 = ta.v[3], b0 = tb.v[0], b1 = tb.v[1], b2 = tb.v[2], b3 = tb.v[3];
-      if constexpr (HD == 64) {
-        // a lane has half a piece: channels 4 c .. 4 c + 3
-        const int sh = (c16 & 1) * 16;
+      if constexpr (HD == 64 || SPLIT > 1) {
+        // 64 channels: a lane has half a piece, channels 4 c .. 4 c + 3; and the workgroup's own of those
+        const int sh = (HD == 64 ? (c16 & 1) * 16 : 0) + own_part * (4 * kChannelTiles);
         a0 >>= sh, a1 >>= sh, a2 >>= sh, a3 >>= sh, b0 >>= sh, b1 >>= sh, b2 >>= sh, b3 >>= sh;
       }
       pair_of_channels(std::integral_constant<int, 0>{}, a0, a1, a2, a3, b0, b1, b2, b3, 0);
-      pair_of_channels(std::integral_constant<int, 1>{}, a0, a1, a2, a3, b0, b1, b2, b3, 2);
-      if constexpr (HD == 128) {
+      if constexpr (kChannelTiles > 2) pair_of_channels(std::integral_constant<int, 1>{}, a0, a1, a2, a3, b0, b1, b2, b3, 2);
+      if constexpr (kChannelTiles > 4) {
         pair_of_channels(std::integral_constant<int, 2>{}, a0, a1, a2, a3, b0, b1, b2, b3, 4);
         pair_of_channels(std::integral_constant<int, 3>{}, a0, a1, a2, a3, b0, b1, b2, b3, 6);
       }
@@ -466,7 +468,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
     // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
     // each end, so two places per wave are enough
     if constexpr (WHOLE) {
-      __shared__ float states[kWholeWaves][16 * RT][HD + 4];   // sums, then (m, l, l unrounded)
+      constexpr int kWidth = HD / SPLIT;
+      __shared__ float states[kWholeWaves][16 * RT][kWidth + 4];   // sums, then (m, l, l unrounded)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float sum = lsum[rt];
@@ -476,30 +479,34 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int y = 0; y < kChannelTiles / 4; ++y)
-            *reinterpret_cast<f32x4*>(dst + j * (HD / 4) + x * kChannelTiles + 4 * y) =
-                f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
-        if (j == 0) dst[HD] = m[rt], dst[HD + 1] = l[rt][0], dst[HD + 2] = sum;
+          for (int y = 0; y < kChannelTiles / 2; ++y)
+            *reinterpret_cast<f32x2*>(dst + j * (kWidth / 4) + x * kChannelTiles + 2 * y) = f32x2{o[rt][2 * y][x], o[rt][2 * y + 1][x]};
+        if (j == 0) dst[kWidth] = m[rt], dst[kWidth + 1] = l[rt][0], dst[kWidth + 2] = sum;
       }
       __syncthreads();
-      // a wave joins every eighth row
+      // a wave joins every eighth row, a lane two neighbouring channels
       for (int r = wave; r < rows; r += kWholeWaves) {
         float top = kNoMax;
 #pragma unroll
-        for (int v = 0; v < kWholeWaves; ++v) top = fmaxf(top, states[v][r][HD]);
-        Merged<HD> x = {};
-        x.top = top;
+        for (int v = 0; v < kWholeWaves; ++v) top = fmaxf(top, states[v][r][kWidth]);
+        float own_l = 0.f, own_lsum = 0.f, o0 = 0.f, o1 = 0.f;
+        const int pair = lane < kWidth / 2 ? lane : 0;
 #pragma unroll
         for (int v = 0; v < kWholeWaves; ++v) {
           const float* src = states[v][r];
-          const float weight = __builtin_amdgcn_exp2f(src[HD] - top);
-          x.l += weight * src[HD + 1];
-          x.lsum += weight * src[HD + 2];
-#pragma unroll
-          for (int y = 0; y < HD / 64; ++y) x.o[y] += weight * src[lane * (HD / 64) + y];
+          const float weight = __builtin_amdgcn_exp2f(src[kWidth] - top);
+          own_l += weight * src[kWidth + 1];
+          own_lsum += weight * src[kWidth + 2];
+          const f32x2 v2 = *reinterpret_cast<const f32x2*>(src + 2 * pair);
+          o0 += weight * v2[0];
+          o1 += weight * v2[1];
         }
         const int i = r / a.rep;
-        write_merged<HD>(a, x, int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep, lane);
+        const int64_t row = int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
+        const float inv = own_l == 0.f ? 0.f : 1.f / own_l;
+        const int channel = 2 * pair / kChannelTiles * (HD / 16) + own_part * kChannelTiles + 2 * pair % kChannelTiles;
+        if (lane < kWidth / 2) reinterpret_cast<uint32_t*>(a.out)[(row * HD + channel) / 2] = pack_out(o0 * inv, o1 * inv, a.bf16);
+        if (a.lse && lane == 0 && own_part == 0) a.lse[row] = own_l == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(own_lsum)) * kLn2;
       }
       return;
     }
