@@ -13,20 +13,23 @@ import torch
 
 from . import _lib
 from ._lib import check, lib
-from .api import _stream_ptr
 
 _DTYPES = {torch.float16: _lib.FP16, torch.bfloat16: _lib.BF16}
 
 
+def _here(device: torch.device, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+    """Handle of the current stream, if the call is for it and the tensors' device is current; None if that has to be made so (_on)."""
+    index = device.index
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None and torch._C._cuda_getDevice() == index else None
+
+
 def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
-    """Makes the tensors' device current for the call, and the stream for what is allocated in it; None where both are already."""
-    if stream is not None:
-        if stream.device != device:
-            raise ValueError("the stream belongs to another device than the tensors")
-        return torch.cuda.stream(stream)
-    if device.index != torch.cuda.current_device():
+    """Makes the tensors' device current for the call, and the stream for what is allocated in it."""
+    if stream is None:
         return torch.cuda.device(device)
-    return None
+    if stream.device != device:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return torch.cuda.stream(stream)
 
 
 class _Workspaces:
@@ -136,46 +139,44 @@ def cocktail_pages_resize(pages: PageTable, delta: torch.Tensor, pools: Sequence
                           stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sequence b becomes delta[b] tokens longer or shorter (device int32 [num_seqs]).  A partly filled page that others hold is
     copied, in all `pools` (tensors [num_pages, ...]), before its sequence grows out of it."""
-    on = _on(pages.device, stream)
-    if on is not None:
-        with on:
+    handle = _here(pages.device, stream)
+    if handle is None:
+        with _on(pages.device, stream):
             return cocktail_pages_resize(pages, delta, pools)
     _int32("delta", delta, (pages.num_seqs,), pages.device)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    st = _stream_ptr(None)
     check(lib().cocktail_pages_resize(C.byref(pages.desc), delta.data_ptr(), array, n, bytes_per_page,
-                                      pages.workspaces.get(pages.workspace_bytes, st).data_ptr(), pages.workspace_bytes, st))
+                                      pages.workspaces.get(pages.workspace_bytes, handle).data_ptr(), pages.workspace_bytes, handle))
 
 
 def cocktail_pages_fork(pages: PageTable, source: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sequence b becomes what sequence source[b] was (device int32 [num_seqs]); source[b] == b leaves it, a negative one frees it."""
-    on = _on(pages.device, stream)
-    if on is not None:
-        with on:
+    handle = _here(pages.device, stream)
+    if handle is None:
+        with _on(pages.device, stream):
             return cocktail_pages_fork(pages, source)
     _int32("source", source, (pages.num_seqs,), pages.device)
-    check(lib().cocktail_pages_fork(C.byref(pages.desc), source.data_ptr(), _stream_ptr(None)))
+    check(lib().cocktail_pages_fork(C.byref(pages.desc), source.data_ptr(), handle))
 
 
 def cocktail_pages_compact(pages: PageTable, pools: Sequence[torch.Tensor] = (), stream: Optional[torch.cuda.Stream] = None) -> None:
     """Moves the pages in use to the front of the pools."""
-    on = _on(pages.device, stream)
-    if on is not None:
-        with on:
+    handle = _here(pages.device, stream)
+    if handle is None:
+        with _on(pages.device, stream):
             return cocktail_pages_compact(pages, pools)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    st = _stream_ptr(None)
     check(lib().cocktail_pages_compact(C.byref(pages.desc), array, n, bytes_per_page,
-                                       pages.workspaces.get(pages.workspace_bytes, st).data_ptr(), pages.workspace_bytes, st))
+                                       pages.workspaces.get(pages.workspace_bytes, handle).data_ptr(), pages.workspace_bytes, handle))
 
 
 def cocktail_pages_check(pages: PageTable, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Waits for the stream and raises CocktailError (code -6) if the last cocktail_pages_resize could not be done."""
-    on = _on(pages.device, stream)
-    if on is not None:
-        with on:
+    handle = _here(pages.device, stream)
+    if handle is None:
+        with _on(pages.device, stream):
             return cocktail_pages_check(pages)
-    check(lib().cocktail_pages_check(C.byref(pages.desc), _stream_ptr(None)))
+    check(lib().cocktail_pages_check(C.byref(pages.desc), handle))
 
 
 def _rows(name: str, t: torch.Tensor, heads: int, head_dim: int, device: torch.device) -> Tuple[int, int, int]:
@@ -204,24 +205,24 @@ def cocktail_fp4_store(cache: Fp4Cache, k: torch.Tensor, v: torch.Tensor, starts
     """Quantizes new tokens into the cache: rows starts[b] .. starts[b+1] of k and v ([tokens, Hkv, D]) become the last tokens of sequence
     b.  Without `starts` every sequence has the same number of rows.  Call cocktail_pages_resize first: it makes the room."""
     dev = cache.pages.device
-    on = _on(dev, stream)
-    if on is not None:
-        with on:
+    handle = _here(dev, stream)
+    if handle is None:
+        with _on(dev, stream):
             return cocktail_fp4_store(cache, k, v, starts)
     rows = _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
     if rows != _rows("v", v, cache.num_kv_heads, cache.head_dim, dev) or k.dtype != v.dtype:
         raise ValueError("k and v must have the same type, shape and strides")
     check(lib().cocktail_fp4_store(cache.desc_ref, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], rows[1], rows[2], rows[0],
-                                   _starts(cache, starts), _stream_ptr(None)))
+                                   _starts(cache, starts), handle))
 
 
 def cocktail_fp4_gather(cache: Fp4Cache, total: int, starts: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float16,
                         out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream: Optional[torch.cuda.Stream] = None):
     """Reads tokens back as the values they stand for: k, v [total, Hkv, D], rows as in cocktail_fp4_store."""
     dev = cache.pages.device
-    on = _on(dev, stream)
-    if on is not None:
-        with on:
+    handle = _here(dev, stream)
+    if handle is None:
+        with _on(dev, stream):
             return cocktail_fp4_gather(cache, total, starts, dtype, out)
     if out is None:
         shape = (int(total), cache.num_kv_heads, cache.head_dim)
@@ -231,7 +232,7 @@ def cocktail_fp4_gather(cache: Fp4Cache, total: int, starts: Optional[torch.Tens
     if rows != _rows("v", v, cache.num_kv_heads, cache.head_dim, dev) or k.dtype != v.dtype or rows[0] != total:
         raise ValueError("k and v must have the same type, shape and strides, and `total` rows")
     check(lib().cocktail_fp4_gather(cache.desc_ref, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], rows[1], rows[2], rows[0],
-                                    _starts(cache, starts), _stream_ptr(None)))
+                                    _starts(cache, starts), handle))
     return k, v
 
 
@@ -242,9 +243,9 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
     (out, lse).  max_new: no sequence has more queries (default: as many as there are rows); max_len: about the longest
     sequence, for the split of the work (default: what the table can hold)."""
     dev = cache.pages.device
-    on = _on(dev, stream)
-    if on is not None:
-        with on:
+    handle = _here(dev, stream)
+    if handle is None:
+        with _on(dev, stream):
             return cocktail_fp4_attention(cache, q, starts, max_new, max_len, sm_scale, out, lse)
     if q.dim() != 3:
         raise TypeError("q must be [tokens, Hq, D]")
@@ -253,11 +254,11 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
     if max_new is None:
         max_new = total // cache.pages.num_seqs if starts is None else total
     if out is None:
-        out = torch.empty((total, heads, cache.head_dim), dtype=q.dtype, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.dtype != q.dtype or out.shape != q.shape or out.device != dev or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's type, shape and device")
     if lse is None:
-        lse = torch.empty((total, heads), dtype=torch.float32, device=dev)
+        lse = q.new_empty((total, heads), dtype=torch.float32)
     elif lse.dtype != torch.float32 or tuple(lse.shape) != (total, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor [tokens, Hq]")
     first = _starts(cache, starts)
@@ -270,7 +271,6 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
         if len(cache.workspace_bytes) > 4096:
             cache.workspace_bytes.clear()
         need = cache.workspace_bytes[key] = int(size.value)
-    handle = _stream_ptr(None)
     check(lib().cocktail_fp4_attention(cache.desc_ref, heads, q.data_ptr(), _DTYPES[q.dtype], st, sh, total, first, int(max_new), int(max_len),
                                        float(sm_scale), out.data_ptr(), lse.data_ptr(), cache.workspaces.get(need, handle).data_ptr(), need,
                                        handle))
