@@ -167,8 +167,8 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
     const int64_t fill = s.row_tiles <= 2 ? 2048 : 1024;
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
-    // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 300, 1000, 2048 tokens 12.2, 12.2, 11.5 us in two launches,
-    // 4.5, 6.7, 9.4 in one; 4096: 11.9 and 15.3), and up to 6K where the segments fill the chip by themselves (128, 256, 512, 1024 of 4096 tokens:
+    // A workgroup per segment and no merge where contexts are short: up to 2K (8 heads: 1000, 2048 tokens 12.2, 11.5 us in two launches,
+    // 6.7, 9.4 in one; 4096: 11.9 and 15.3), and up to 6K where the segments fill the chip by themselves (128, 256, 512, 1024 of 4096 tokens:
     // 23.0, 32.6, 57.3, 104.7 and 19.6, 25.5, 46.7, 101.5; of 8192 the same within 3 %, but there one long sequence among short ones would be waited for).
     const int64_t segments = seqs * c->num_kv_heads;
     s.whole = s.row_tiles == 1 && max_len <= (segments >= 128 ? 6144 : 2048);
