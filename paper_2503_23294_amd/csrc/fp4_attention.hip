@@ -151,9 +151,11 @@ Split split_of(const cocktail_fp4_cache* c, int rep, int64_t total, int64_t max_
   if (max_len <= 0 || max_len > capacity) max_len = capacity;
   const int64_t most_rows = max_new * rep;
   s.active = c->pages.num_seqs < total ? c->pages.num_seqs : total;
-  // a batch may hold sequences for either kernel unless every sequence has the same number of queries
+  // A batch may hold sequences for either kernel, unless all have the same number of queries or the others cannot have so many that one is left with
+  // few: then the tile kernel has them all, whatever their numbers are, and two launches with nothing to do are saved (5 us each by themselves, 1 to 9 us of a call of 0.8 ms).
   s.tiles = most_rows > kDecodeRows;
-  s.decode = !s.tiles || (!uniform && rep <= kDecodeRows);
+  const int64_t least = total - (int64_t(c->pages.num_seqs) - 1) * max_new;
+  s.decode = !s.tiles || (!uniform && rep <= kDecodeRows && least * rep <= kDecodeRows);
   s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
   s.row_tiles = (s.rows + 15) / 16;
   if (s.decode) {

@@ -410,6 +410,24 @@ def test_few_active_sequences_in_a_large_table(num_seqs):
 
 
 @gpu
+def test_prompts_alone():
+    """No sequence can have few queries by the sizes of the call, so one kernel has them all: also a sequence that has few, next to one that has more than
+    it may and is left out."""
+    B = Batch([400, 390], 2, 128, 16, torch.float16, seed=41)
+    B.store_all()
+    for new in ([200, 100], [200, 200], [150, 130]):
+        q = B.query(new, 3)
+        out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=200, max_len=400)
+        B.check(q, new, out, lse)
+    new = [295, 5]
+    q = B.query(new, 3)
+    out, lse = torch.full_like(q, 7.0), torch.full((300, 6), 7.0, device=B.dev)
+    ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=200, max_len=400, out=out, lse=lse)
+    assert (out[:295] == 7.0).all() and (lse[:295] == 7.0).all()
+    B.check(q[295:], [0, 5], out[295:], lse[295:])
+
+
+@gpu
 @pytest.mark.parametrize("num_seqs,heads", [(40, 8), (64, 9), (33, 31), (64, 4), (65, 8)])
 def test_many_segments_of_unlike_lengths(num_seqs, heads):
     """More short segments than compute units, in the order of their lengths: lengths that are alike or zero, sequences without queries."""
