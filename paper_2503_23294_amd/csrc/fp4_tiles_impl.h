@@ -12,8 +12,8 @@
 
 namespace cocktail {
 
-// K in chunks of 32 keys, a ring of five: the two that are read in a step, the one before them that a slower wave may still read, and the
-// two that are written.  V of 64 keys, twice.
+// K in chunks of 32 keys, a ring of five: a step reads the two behind its first chunk (which was read before the barrier that it began with) and
+// writes the two behind those, the second of them into the place of that first chunk.  V of 64 keys, twice.
 constexpr int kChunk = 32, kRing = 5;
 constexpr float kSumLimit = 16384.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then
 template <int HD>
@@ -343,6 +343,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
       for (int x = 0; x < kSteps; ++x) s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(src + x * 16), q[x], s0, 0, 0, 0);
       mask(s0, k0 * kTileKeys, bad0 & 3);
     }
+    __syncthreads();                // the first step writes into the chunk that these products have read
     int chunk = 0;                  // slot of this step's first chunk
     for (int step = k0; step < k1; ++step) {
       const int buffer = (step - k0) & 1;
