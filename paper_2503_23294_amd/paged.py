@@ -2,11 +2,12 @@
 
 Same names as the C entry points.  torch supplies device memory and streams.  Workspaces: a cache keeps one per stream for the calls that are
 made on it, one after the other; what is captured into a graph has one of its own, from the graph's memory, so that graphs and eager calls never
-share one.
+share one.  Threads may call at the same time: a call with a workspace is launched as a whole before the next one begins.
 """
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -33,11 +34,13 @@ def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
 
 
 class _Workspaces:
-    """Workspaces by stream."""
+    """Workspaces by stream.  `lock` is held, and the workspace kept, from get() until the call that uses it has returned: a call is several
+    launches, and the interpreter lets other threads in between (launches of two calls mixed on one stream would work in the same memory)."""
 
     def __init__(self, device: torch.device):
         self.device = device
         self.kept = {}
+        self.lock = threading.RLock()
 
     def get(self, need: int, stream: int) -> torch.Tensor:
         """A workspace for a call that is about to be made on the current stream, whose handle is `stream`."""
@@ -145,8 +148,10 @@ def cocktail_pages_resize(pages: PageTable, delta: torch.Tensor, pools: Sequence
             return cocktail_pages_resize(pages, delta, pools)
     _int32("delta", delta, (pages.num_seqs,), pages.device)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    check(lib().cocktail_pages_resize(C.byref(pages.desc), delta.data_ptr(), array, n, bytes_per_page,
-                                      pages.workspaces.get(pages.workspace_bytes, handle).data_ptr(), pages.workspace_bytes, handle))
+    with pages.workspaces.lock:
+        workspace = pages.workspaces.get(pages.workspace_bytes, handle)
+        check(lib().cocktail_pages_resize(C.byref(pages.desc), delta.data_ptr(), array, n, bytes_per_page, workspace.data_ptr(),
+                                          pages.workspace_bytes, handle))
 
 
 def cocktail_pages_fork(pages: PageTable, source: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -166,8 +171,9 @@ def cocktail_pages_compact(pages: PageTable, pools: Sequence[torch.Tensor] = (),
         with _on(pages.device, stream):
             return cocktail_pages_compact(pages, pools)
     array, n, bytes_per_page = _pool_list(pages, pools)
-    check(lib().cocktail_pages_compact(C.byref(pages.desc), array, n, bytes_per_page,
-                                       pages.workspaces.get(pages.workspace_bytes, handle).data_ptr(), pages.workspace_bytes, handle))
+    with pages.workspaces.lock:
+        workspace = pages.workspaces.get(pages.workspace_bytes, handle)
+        check(lib().cocktail_pages_compact(C.byref(pages.desc), array, n, bytes_per_page, workspace.data_ptr(), pages.workspace_bytes, handle))
 
 
 def cocktail_pages_check(pages: PageTable, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -271,7 +277,8 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
         if len(cache.workspace_bytes) > 4096:
             cache.workspace_bytes.clear()
         need = cache.workspace_bytes[key] = int(size.value)
-    check(lib().cocktail_fp4_attention(cache.desc_ref, heads, q.data_ptr(), _DTYPES[q.dtype], st, sh, total, first, int(max_new), int(max_len),
-                                       float(sm_scale), out.data_ptr(), lse.data_ptr(), cache.workspaces.get(need, handle).data_ptr(), need,
-                                       handle))
+    with cache.workspaces.lock:
+        workspace = cache.workspaces.get(need, handle)
+        check(lib().cocktail_fp4_attention(cache.desc_ref, heads, q.data_ptr(), _DTYPES[q.dtype], st, sh, total, first, int(max_new), int(max_len),
+                                           float(sm_scale), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), need, handle))
     return out, lse

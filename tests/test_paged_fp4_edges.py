@@ -3,6 +3,8 @@ starts and lengths."""
 import re
 import shutil
 import subprocess
+import threading
+import time
 
 import numpy as np
 import pytest
@@ -10,7 +12,7 @@ import torch
 
 import paper_2503_23294_amd as ck
 from oracle import fp4_oracle as O
-from paper_2503_23294_amd import _lib
+from paper_2503_23294_amd import _lib, paged
 from test_device_code import _objdump
 from test_paged_fp4 import DTYPES, Batch, _f64
 
@@ -59,3 +61,94 @@ def test_last_tiles_with_idle_waves(lens, new, kv_heads, rep, d):
     for _ in range(10):
         again, lse2 = call()
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+# ---- threads -------------------------------------------------------------------------------------------------------------------
+
+
+class _SlowLib:
+    """The library, but for the calls that launch several kernels: those take their time and note which workspace they have, and for how long."""
+
+    def __init__(self):
+        self.real, self.inside, self.mixed, self.calls = _lib.lib(), [], [], 0
+
+    def __getattr__(self, name):
+        if name not in ("cocktail_fp4_attention", "cocktail_pages_resize", "cocktail_pages_compact"):
+            return getattr(self.real, name)
+        place = {"cocktail_fp4_attention": 14, "cocktail_pages_resize": 5, "cocktail_pages_compact": 4}[name]
+
+        def call(*args):
+            me = (args[place], args[place] + args[place + 1])
+            self.mixed += [(me, other) for other in self.inside if me[0] < other[1] and other[0] < me[1]]
+            self.inside.append(me)
+            self.calls += 1
+            time.sleep(2e-4)
+            self.inside.remove(me)
+            return 0
+        return call
+
+
+def test_threads_do_not_share_a_workspace_at_the_same_time(monkeypatch):
+    """Calls of several threads on one stream, of unlike sizes, so that the kept workspace is replaced by larger ones in between: no two calls
+    are ever inside the library with memory in common, nor with memory that has been given up."""
+    slow = _SlowLib()
+    monkeypatch.setattr(paged, "lib", lambda: slow)
+    monkeypatch.setattr(paged, "_here", lambda device, stream: 7)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    pages = ck.PageTable.of(i32(4, 2000), i32(4), i32(64), 16)
+    cache = ck.Fp4Cache(pages, 2, 128)
+    errors = []
+
+    def work(seed):
+        rng = np.random.default_rng(seed)
+        try:
+            for i in range(40):
+                kind = rng.integers(0, 4)
+                if kind == 0:
+                    ck.cocktail_pages_resize(pages, i32(4))
+                elif kind == 1:
+                    ck.cocktail_pages_compact(pages)
+                else:
+                    n = int(rng.integers(1, 9))
+                    ck.cocktail_fp4_attention(cache, torch.zeros(4 * n, 8, 128, dtype=torch.float16))
+        except Exception as e:   # a thread's failure is the test's
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(seed,)) for seed in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert slow.calls == 160 and not slow.mixed
+
+
+@gpu
+def test_two_threads_on_one_stream():
+    """Two threads attend to one cache on the default stream, each with queries of its own: what they get is what one alone gets."""
+    B = Batch([5000, 3000, 700, 40], 4, 128, 16, torch.float16, seed=51)
+    B.store_all()
+    new = [2, 1, 3, 1]
+    starts = B.starts(new)
+    queries = [B.query(new, 8) for _ in range(2)]
+    call = lambda q: ck.cocktail_fp4_attention(B.cache, q, starts, max_new=3, max_len=5000)  # noqa: E731
+    want = [[x.clone() for x in call(q)] for q in queries]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def work(i):
+        try:
+            got[i] = [call(queries[i]) for _ in range(300)]
+        except Exception as e:
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for i in range(2):
+        assert len(got[i]) == 300
+        assert all(torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1]) for out, lse in got[i])
