@@ -2,7 +2,8 @@
 
 Same names as the C entry points.  torch supplies device memory and streams.  Workspaces: a cache keeps one per stream for the calls that are
 made on it, one after the other; what is captured into a graph has one of its own, from the graph's memory, so that graphs and eager calls never
-share one.  Threads may call at the same time: a call with a workspace is launched as a whole before the next one begins.
+share one.  Threads may call at the same time: a call with a workspace is launched as a whole before the next one begins.  `stream`: another stream
+than the current one; it has to be behind what makes the arguments, which may be dropped as soon as the call returns.
 """
 from __future__ import annotations
 
@@ -31,6 +32,15 @@ def _on(device: torch.device, stream: Optional[torch.cuda.Stream]):
     if stream.device != device:
         raise ValueError("the stream belongs to another device than the tensors")
     return torch.cuda.stream(stream)
+
+
+def _used_on(stream: Optional[torch.cuda.Stream], pages: "PageTable", *tensors: Optional[torch.Tensor]) -> None:
+    """Behind a call on a stream that it was given: what it works on there may be dropped by the caller at once, and must not be handed out to others
+    on its own stream before the call has taken place."""
+    if stream is not None:
+        for t in (pages.table, pages.seq_lens, pages.refs, pages.status, *tensors):
+            if t is not None:
+                t.record_stream(stream)
 
 
 class _Workspaces:
@@ -145,7 +155,8 @@ def cocktail_pages_resize(pages: PageTable, delta: torch.Tensor, pools: Sequence
     handle = _here(pages.device, stream)
     if handle is None:
         with _on(pages.device, stream):
-            return cocktail_pages_resize(pages, delta, pools)
+            cocktail_pages_resize(pages, delta, pools)
+        return _used_on(stream, pages, delta, *pools)
     _int32("delta", delta, (pages.num_seqs,), pages.device)
     array, n, bytes_per_page = _pool_list(pages, pools)
     with pages.workspaces.lock:
@@ -159,7 +170,8 @@ def cocktail_pages_fork(pages: PageTable, source: torch.Tensor, stream: Optional
     handle = _here(pages.device, stream)
     if handle is None:
         with _on(pages.device, stream):
-            return cocktail_pages_fork(pages, source)
+            cocktail_pages_fork(pages, source)
+        return _used_on(stream, pages, source)
     _int32("source", source, (pages.num_seqs,), pages.device)
     check(lib().cocktail_pages_fork(C.byref(pages.desc), source.data_ptr(), handle))
 
@@ -169,7 +181,8 @@ def cocktail_pages_compact(pages: PageTable, pools: Sequence[torch.Tensor] = (),
     handle = _here(pages.device, stream)
     if handle is None:
         with _on(pages.device, stream):
-            return cocktail_pages_compact(pages, pools)
+            cocktail_pages_compact(pages, pools)
+        return _used_on(stream, pages, *pools)
     array, n, bytes_per_page = _pool_list(pages, pools)
     with pages.workspaces.lock:
         workspace = pages.workspaces.get(pages.workspace_bytes, handle)
@@ -214,7 +227,8 @@ def cocktail_fp4_store(cache: Fp4Cache, k: torch.Tensor, v: torch.Tensor, starts
     handle = _here(dev, stream)
     if handle is None:
         with _on(dev, stream):
-            return cocktail_fp4_store(cache, k, v, starts)
+            cocktail_fp4_store(cache, k, v, starts)
+        return _used_on(stream, cache.pages, cache.pool, k, v, starts)
     rows = _rows("k", k, cache.num_kv_heads, cache.head_dim, dev)
     if rows != _rows("v", v, cache.num_kv_heads, cache.head_dim, dev) or k.dtype != v.dtype:
         raise ValueError("k and v must have the same type, shape and strides")
@@ -229,7 +243,9 @@ def cocktail_fp4_gather(cache: Fp4Cache, total: int, starts: Optional[torch.Tens
     handle = _here(dev, stream)
     if handle is None:
         with _on(dev, stream):
-            return cocktail_fp4_gather(cache, total, starts, dtype, out)
+            result = cocktail_fp4_gather(cache, total, starts, dtype, out)
+        _used_on(stream, cache.pages, cache.pool, starts, *(out or ()))
+        return result
     if out is None:
         shape = (int(total), cache.num_kv_heads, cache.head_dim)
         out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
@@ -252,7 +268,9 @@ def cocktail_fp4_attention(cache: Fp4Cache, q: torch.Tensor, starts: Optional[to
     handle = _here(dev, stream)
     if handle is None:
         with _on(dev, stream):
-            return cocktail_fp4_attention(cache, q, starts, max_new, max_len, sm_scale, out, lse)
+            result = cocktail_fp4_attention(cache, q, starts, max_new, max_len, sm_scale, out, lse)
+        _used_on(stream, cache.pages, cache.pool, q, starts, out, lse)
+        return result
     if q.dim() != 3:
         raise TypeError("q must be [tokens, Hq, D]")
     heads = q.shape[1]

@@ -1,5 +1,6 @@
 """The paged 4-bit cache where it can go wrong besides what test_paged_fp4.py looks at: waits, threads, streams, far tails of a softmax, unusual queries,
 starts and lengths."""
+import contextlib
 import re
 import shutil
 import subprocess
@@ -152,3 +153,88 @@ def test_two_threads_on_one_stream():
     for i in range(2):
         assert len(got[i]) == 300
         assert all(torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1]) for out, lse in got[i])
+
+
+# ---- streams -------------------------------------------------------------------------------------------------------------------
+
+
+def test_what_is_used_on_another_stream_is_recorded_there(monkeypatch):
+    """Every tensor that a call on a given stream works on, those of the table and the cache among them; none where no stream is given."""
+    slow, seen = _SlowLib(), []
+    quiet = type("Quiet", (), {"__getattr__": lambda self, name: (lambda *a: 0) if name in launches else getattr(slow, name)})()
+    launches = ("cocktail_fp4_store", "cocktail_fp4_gather", "cocktail_pages_fork")
+    monkeypatch.setattr(paged, "lib", lambda: quiet)
+    monkeypatch.setattr(paged, "_here", lambda device, stream: None if stream is not None else 7)
+    monkeypatch.setattr(paged, "_on", lambda device, stream: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: seen.append((self.data_ptr(), stream)), raising=False)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    f16 = lambda *shape: torch.zeros(shape, dtype=torch.float16)  # noqa: E731
+    pages = ck.PageTable.of(i32(2, 5), i32(2), i32(8), 16)
+    cache = ck.Fp4Cache(pages, 1, 64)
+    table = [pages.table, pages.seq_lens, pages.refs, pages.status]
+    k, v, q, out, lse, starts, delta = f16(4, 1, 64), f16(4, 1, 64), f16(4, 2, 64), f16(4, 2, 64), torch.zeros(4, 2), i32(3), i32(2)
+    for call, used in ((lambda s: ck.cocktail_fp4_store(cache, k, v, starts, stream=s), [cache.pool, k, v, starts]),
+                       (lambda s: ck.cocktail_fp4_gather(cache, 4, starts, out=(k, v), stream=s), [cache.pool, k, v, starts]),
+                       (lambda s: ck.cocktail_fp4_gather(cache, 4, stream=s), [cache.pool]),
+                       (lambda s: ck.cocktail_fp4_attention(cache, q, starts, out=out, lse=lse, stream=s), [cache.pool, q, starts, out, lse]),
+                       (lambda s: ck.cocktail_fp4_attention(cache, q, stream=s), [cache.pool, q]),
+                       (lambda s: ck.cocktail_pages_resize(pages, delta, stream=s), [delta]),
+                       (lambda s: ck.cocktail_pages_fork(pages, delta, stream=s), [delta]),
+                       (lambda s: ck.cocktail_pages_compact(pages, stream=s), [])):
+        seen.clear()
+        call(None)
+        assert not seen
+        call("a stream")
+        assert {x for x, _ in seen} == {t.data_ptr() for t in table + used} and {s for _, s in seen} == {"a stream"}
+
+
+@gpu
+def test_tensors_that_are_dropped_behind_a_call_on_another_stream():
+    """A stream that is busy gets calls whose arguments are temporaries of the current stream; these are dropped, and tensors of their sizes made and
+    overwritten, before the calls take place."""
+    lens, new = [500, 64, 130], [3, 1, 2]
+    B = Batch(lens, 2, 128, 16, torch.bfloat16, seed=61)
+    q = B.query(new, 4)
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32), np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    B.store_all()
+    want = [x.clone() for x in ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=3)]
+    want += [x.clone() for x in ck.cocktail_fp4_gather(B.cache, sum(lens), B.starts(lens), dtype=B.dtype)]
+    pool = B.cache.pool.clone()
+    B.cache.pool.copy_(torch.from_numpy(B.junk))
+    free = sum(r == 0 for r in B.pages.refs.tolist())
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def dropped(*shape_of):
+        """Other tensors where the temporaries were."""
+        return [torch.zeros_like(x) for x in shape_of for _ in range(4)]
+
+    def there(*arrays):
+        """Temporaries that the other stream waits for."""
+        made = [(torch.from_numpy(a).to(B.dev) if isinstance(a, np.ndarray) else a.clone()) for a in arrays]
+        s.wait_stream(torch.cuda.current_stream())
+        return made
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    ck.cocktail_fp4_store(B.cache, *there(B.k, B.v, starts[0]), stream=s)
+    keep = dropped(B.k, B.v, torch.from_numpy(starts[0]).to(B.dev))
+    got = [*ck.cocktail_fp4_attention(B.cache, *there(q, starts[1]), max_new=3, stream=s)]
+    keep += dropped(q, torch.from_numpy(starts[1]).to(B.dev))
+    got += [*ck.cocktail_fp4_gather(B.cache, sum(lens), *there(starts[0]), dtype=B.dtype, stream=s)]
+    keep += dropped(torch.from_numpy(starts[0]).to(B.dev))
+    out, lse = torch.ones_like(q), torch.ones(sum(new), 8, device=B.dev)
+    ck.cocktail_fp4_attention(B.cache, *there(q, starts[1]), max_new=3, out=out, lse=lse, stream=s)
+    ck.cocktail_pages_fork(B.pages, *there(np.array([0, 1, 1], np.int32)), stream=s)
+    ck.cocktail_pages_resize(B.pages, *there(np.array([0, 0, -64], np.int32)), [B.cache.pool], stream=s)
+    keep += dropped(torch.zeros(3, dtype=torch.int32, device=B.dev))
+    assert not s.query()       # still asleep: none of the calls has taken place
+    ck.cocktail_pages_check(B.pages, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(B.cache.pool, pool)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert B.pages.seq_lens.tolist() == [500, 64, 0] and sum(r == 0 for r in B.pages.refs.tolist()) == free + 9
+    assert len(keep) > 0
