@@ -125,6 +125,26 @@ def test_threads_do_not_share_a_workspace_at_the_same_time(monkeypatch):
     assert slow.calls == 160 and not slow.mixed
 
 
+def test_the_caches_of_a_table_share_their_workspace(monkeypatch):
+    """Layers attend one after the other on a stream: one workspace is enough for all of them, and for the calls on the table."""
+    slow = _SlowLib()
+    monkeypatch.setattr(paged, "lib", lambda: slow)
+    monkeypatch.setattr(paged, "_here", lambda device, stream: 7)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    made, empty = [], torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: made.append(empty(*a, **k)) or made[-1])
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    pages = ck.PageTable.of(i32(4, 2000), i32(4), i32(64), 16)
+    layers = [ck.Fp4Cache(pages, 2, 128) for _ in range(5)]
+    q = torch.zeros(4, 8, 128, dtype=torch.float16)
+    made.clear()
+    for cache in layers:
+        ck.cocktail_fp4_attention(cache, q)
+    ck.cocktail_pages_resize(pages, i32(4))
+    assert slow.calls == 6 and sum(x.dtype == torch.uint8 for x in made) == 1
+
+
 @gpu
 def test_two_threads_on_one_stream():
     """Two threads attend to one cache on the default stream, each with queries of its own: what they get is what one alone gets."""
