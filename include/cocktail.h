@@ -602,9 +602,9 @@ int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32
  * starts[b] queries and len = seq_lens[b], query i of sequence b attends to tokens 0 .. len - n + i.  One query per sequence is a
  * decode step, some are the verification of drafts, many a prompt or a part of one; a batch may mix them.
  *     out[t,h] = softmax(sm_scale * q[t,h] . K^T) V,   kv head h / (num_q_heads / num_kv_heads)
- * Products and sums in binary32, K and V as stored, softmax weights rounded to fp16 (relative 2^-11) relative to a maximum that may be
- * too small by as much as fp16 can hold (2^14).  bf16 queries are used as fp16 times a power of two of their own (exact, but for channels below 2^-14
- * of the largest).
+ * Products and sums in binary32, K and V as stored, softmax weights rounded to fp16: by 2^-11 of themselves, or, where they are below 2^-25 of the
+ * largest, by 2^-36 of that at most (in calls with max_new * num_q_heads / num_kv_heads > 64: below 2^-21, by 2^-32).  bf16 queries are used as fp16
+ * times a power of two of their own (exact, but for channels below 2^-14 of the largest).
  *
  *   q         DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d, strides multiples of 8
  *   dtype     of q and out

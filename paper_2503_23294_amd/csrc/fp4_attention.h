@@ -9,8 +9,14 @@ namespace cocktail {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kNoMax = -3.0e38f;      // reference maximum of a row that has seen no key
-constexpr float kMaxSlack = 8.0f;       // a reference maximum may be this much too small (base 2) before it is raised: weights up to 2^8
+// Weights are 2^(logit - reference) and become fp16.  The reference of a row is kShift below the largest logit that it was made for, so that weights
+// lie in the upper part of fp16's range: from 2^-25 of that logit's weight on they are normal numbers, and what is smaller is off by 2^-36 of it at most, which
+// a million keys of a long tail together do not show in a 16-bit result (with the reference at the largest logit it were 2^-25: the tail of 128K keys
+// behind one that is 17 nats above them came out half as large again).  A reference that is kSlack too small is raised: weights up to 2^15.  The tile
+// kernel, whose waves have 32 rows that all wait while one is raised, has 2^-21 and 2^-32 (prompts of 8190 and 4095 tokens: 749 us without a shift, 748 with 7,
+// 760 with 8, 767 with 11).
+constexpr float kNoMax = -3.0e38f;      // reference of a row that has seen no key
+constexpr float kShift = 11.0f, kSlack = 4.0f, kTileShift = 7.0f;
 constexpr int kUnit = 32;               // tokens that a wave of the decode kernel takes at a time
 constexpr int kDecodeRows = 64;         // query rows (tokens x heads of a kv head) that the decode kernel serves at most
 constexpr int kDecodeWaves = 4;         // waves per workgroup there

@@ -12,8 +12,8 @@
 //    The result layout of S^T (lane: a query row, tokens 4 j + x) is the operand layout of P^T with tokens numbered accordingly: weights
 //    never leave their lane.
 //  * Codes become fp16 with one instruction per pair that applies the scale as well.
-//  * The reference maximum is only raised when a logit exceeds it by 2^8 (exact, the result does not depend on it), so that the common step has
-//    no exchange between lanes at all.  Sums of the rounded weights come from a product with ones (the matrix cores are idle otherwise).
+//  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4 (exact, the result does not depend on it), so that the
+//    common step has no exchange between lanes at all.  Sums of the rounded weights come from a product with ones (the matrix cores are idle otherwise).
 #pragma once
 #include "fp4_attention.h"
 
@@ -388,10 +388,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
       for (int rt = 0; rt < kLive; ++rt) {
         float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
                           fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3]))) * c[rt];
-        if (__any(top > m[rt] + kMaxSlack)) {
+        if (__any(top > m[rt] + (kShift + kSlack))) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float raised = fmaxf(m[rt], top), alpha = __builtin_amdgcn_exp2f(m[rt] - raised);
+          const float raised = fmaxf(m[rt], top - kShift), alpha = __builtin_amdgcn_exp2f(m[rt] - raised);
           m[rt] = raised;
           lsum[rt] *= alpha;
           l[rt] *= alpha;

@@ -15,7 +15,7 @@ namespace cocktail {
 // K in chunks of 32 keys, a ring of five: a step reads the two behind its first chunk (which was read before the barrier that it began with) and
 // writes the two behind those, the second of them into the place of that first chunk.  V of 64 keys, twice.
 constexpr int kChunk = 32, kRing = 5;
-constexpr float kSumLimit = 16384.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then
+constexpr float kSumLimit = 61440.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then (behind a new reference it is 16 * 2^7 at most)
 template <int HD>
 struct Fp4TileLds {
   static constexpr int kKeyStride = HD + 8;          // halves; rows shift by four banks
@@ -245,14 +245,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
       }
     }
   };
-  // The reference maximum of a row whose logits exceed it by too much becomes the largest of them.
+  // The reference of a row whose logits exceed it by too much is made for the largest of them.
   auto raise = [&](const f32x16& s) __attribute__((always_inline)) {
     float top = s[0];
 #pragma unroll
     for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
     top *= c;
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float raised = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - raised);
+    const float raised = fmaxf(m, top - kTileShift), alpha = __builtin_amdgcn_exp2f(m - raised);
     m = raised;
     lsum *= alpha;
 #pragma unroll

@@ -258,3 +258,42 @@ def test_tensors_that_are_dropped_behind_a_call_on_another_stream():
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     assert B.pages.seq_lens.tolist() == [500, 64, 0] and sum(r == 0 for r in B.pages.refs.tolist()) == free + 9
     assert len(keep) > 0
+
+
+# ---- softmax -------------------------------------------------------------------------------------------------------------------
+
+
+@gpu
+@pytest.mark.parametrize("spread", [0.0, 0.3])
+@pytest.mark.parametrize("tokens,new,max_len", [(131072, 1, 0), (131072, 1, 1), (131072, 6, 0), (131072, 10, 0), (131072, 16, 0), (32768, 40, 0)])
+def test_the_tail_behind_one_large_key(tokens, new, max_len, spread):
+    """One key with a logit that is 12 to 20 nats above those of all others (nearly alike), whose values are those that count: its own are zero, so
+    that the result is the tail's share.  In one launch and two, with one to four operands of queries, and in tiles."""
+    rep, d = 4, 64
+    B = Batch([tokens], 1, d, 64, torch.float16, seed=new)
+    gaps = (12.0, 15.0, 17.0, 17.5, 20.0)
+    B.k.normal_(0, 1).mul_(0.14 / 0.3 * spread)
+    B.v.normal_(0, 0.25).add_(1.0)
+    B.k[0], B.v[0] = 1.0, 0.0
+    B.store_all()
+    k, v = ck.cocktail_fp4_gather(B.cache, tokens)
+    k, v = k[:, 0].double(), v[:, 0].double()
+    q = torch.empty(new, rep, d, device=B.dev, dtype=torch.float16)
+    for i in range(new):
+        for h in range(rep):
+            q[i, h] = gaps[(i * rep + h) % 5] / d
+    out, lse = ck.cocktail_fp4_attention(B.cache, q, max_len=max_len, sm_scale=1.0)
+    s = q.double().view(-1, d) @ k.t()
+    last = torch.arange(tokens - new, tokens, device=B.dev).repeat_interleave(rep)
+    s.masked_fill_(torch.arange(tokens, device=B.dev)[None] > last[:, None], -float("inf"))
+    total = torch.exp(s - s[:, :1]).sum(1, keepdim=True)
+    w = torch.exp(s - s[:, :1]) / total
+    want = w @ v
+    # the result's rounding; the weights', in the sum over V and in the normaliser (2^-11 each); logits of up to 20, whose 64 products and sums in
+    # binary32 are off by 68 * 2^-24 * 20 = 8.2e-5, and whose difference to the reference, 29 * 1.45 at most, by 2^-19; two sums of one term per 16 keys, in eight
+    # parts at least where there are up to 64 rows; weights that are subnormals, results that are
+    adds = tokens // 16 // (8 if new * rep <= 64 else 1) + 64
+    bound = want.abs() * (3 * 2.0 ** -11 + 2 * (8.2e-5 + 2.0 ** -19) + 2 * adds * 2.0 ** -24) + tokens * 2.0 ** (-36 if new * rep <= 64 else -32) * v.abs().max() + 2.0 ** -25
+    far = (out.double().view(-1, d) - want).abs()
+    assert (far <= bound).all(), f"{(far / want.abs()).max()} of the result, {(far / bound).max()} of the bound"
+    assert ((lse.double().view(-1) - torch.logsumexp(s, 1)).abs() <= 8.2e-5 + 2.0 ** -18 + adds * 2.0 ** -24).all()
