@@ -77,6 +77,11 @@ __device__ __forceinline__ uint32_t pack_out(float lo, float hi, int bf16) {
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, b2{__bf16(lo), __bf16(hi)});
 }
+// Sum of two weights as they were rounded, and of what was there before.
+__device__ __forceinline__ float add_rounded(uint32_t w, float sum) {
+  const _Float16 one = _Float16(1.f);
+  return __builtin_amdgcn_fdot2(as_h2(w), h2{one, one}, sum, false);
+}
 // Two bf16 in a word as floats.
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }

@@ -13,7 +13,7 @@
 //    never leave their lane.
 //  * Codes become fp16 with one instruction per pair that applies the scale as well.
 //  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4 (exact, the result does not depend on it), so that the
-//    common step has no exchange between lanes at all.  Sums of the rounded weights come from a product with ones (the matrix cores are idle otherwise).
+//    common step has no exchange between lanes at all.
 #pragma once
 #include "fp4_attention.h"
 
@@ -169,6 +169,9 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
   __shared__ int32_t lds_words[kWholeWaves + 1];
   // three or four operands of queries do not fit the registers next to their sums: every lane reads its own from LDS
   constexpr bool kKeepQ = RT <= 2;
+  // the normaliser is the sum of the weights as they were rounded, so that a row whose values are all alike is that value: a product with ones, which
+  // adds up over the lanes too, or sums of a lane's own where four registers more per operand are not there
+  constexpr bool kOnes = RT <= 2;
   __shared__ float lds_state[WHOLE ? 1 : kDecodeWaves][WHOLE ? 1 : 16][WHOLE ? 1 : HD + 4];
   __shared__ u32x4 lds_q[kKeepQ ? 1 : kDecodeWaves][kKeepQ ? 1 : RT][kKeepQ ? 1 : kSteps][kKeepQ ? 1 : 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -310,7 +313,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
 
     h8 q[kKeepQ ? RT : 1][kSteps];
     float c[RT], m[RT], lsum[RT];
-    f32x4 l[RT], o[RT][kChannelTiles];
+    std::conditional_t<kOnes, f32x4, float> l[RT];
+    f32x4 o[RT][kChannelTiles];
     int lim[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
       lim[rt] = r < rows ? len - n + r / a.rep + 1 : 0;
       m[rt] = kNoMax;
       lsum[rt] = 0.f;
-      l[rt] = f32x4{};
+      l[rt] = {};
 #pragma unroll
       for (int ct = 0; ct < kChannelTiles; ++ct) o[rt][ct] = f32x4{};
     }
@@ -402,10 +406,13 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
 #pragma unroll
         for (int x = 0; x < 8; ++x) w8[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][x >> 2][x & 3], c[rt], -m[rt]));
         lsum[rt] += ((w8[0] + w8[1]) + (w8[2] + w8[3])) + ((w8[4] + w8[5]) + (w8[6] + w8[7]));
-        p[rt] = __builtin_bit_cast(h8, u32x4{pack_halves(w8[0], w8[1]), pack_halves(w8[2], w8[3]), pack_halves(w8[4], w8[5]), pack_halves(w8[6], w8[7])});
-        if constexpr (RT <= 2) {
+        const u32x4 words = {pack_halves(w8[0], w8[1]), pack_halves(w8[2], w8[3]), pack_halves(w8[4], w8[5]), pack_halves(w8[6], w8[7])};
+        p[rt] = __builtin_bit_cast(h8, words);
+        if constexpr (kOnes) {
           const _Float16 one = _Float16(1.f);
           l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h8{one, one, one, one, one, one, one, one}, p[rt], l[rt], 0, 0, 0);
+        } else {
+          l[rt] = add_rounded(words[3], add_rounded(words[2], add_rounded(words[1], add_rounded(words[0], l[rt]))));
         }
       }
       // weighted sums
@@ -518,7 +525,14 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       const int r = rt * 16 + c16;
-      const float lr = RT <= 2 ? l[rt][0] : sum;
+      float lr;
+      if constexpr (kOnes) {
+        lr = l[rt][0];
+      } else {
+        lr = l[rt];
+        lr += __shfl_xor(lr, 16);
+        lr += __shfl_xor(lr, 32);
+      }
       if (whole) {
         if (r >= rows) continue;
         const int i = r / a.rep;

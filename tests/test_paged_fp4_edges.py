@@ -297,3 +297,27 @@ def test_the_tail_behind_one_large_key(tokens, new, max_len, spread):
     far = (out.double().view(-1, d) - want).abs()
     assert (far <= bound).all(), f"{(far / want.abs()).max()} of the result, {(far / bound).max()} of the bound"
     assert ((lse.double().view(-1) - torch.logsumexp(s, 1)).abs() <= 8.2e-5 + 2.0 ** -18 + adds * 2.0 ** -24).all()
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,new,rep,max_len", [([1, 30, 400], [1, 1, 1], 3, 400), ([30, 400, 90], [1, 1, 1], 3, 0), ([400, 33, 2], [2, 2, 2], 16, 0),
+                                                  ([400, 390, 7] + [40 + 17 * i for i in range(20)], [3, 2, 3] + [3] * 20, 16, 0),
+                                                  ([400, 64, 5] + [50 + 17 * i for i in range(20)], [4, 3, 4] + [4] * 20, 16, 0)])
+def test_values_that_are_all_alike_come_out_as_they_are(lens, new, rep, max_len, d):
+    """Up to 64 rows every weight goes into the normaliser as it goes into the sum over V, rounded: where a head's values are one vector for all keys the result
+    is that vector, whatever the weights are.  Two sums of up to 400 terms in binary32, each off by 400 * 2^-23 = 4.8e-5 at most, are nearer to it
+    than half the distance to the next fp16 below a power of two, 2^-13."""
+    B = Batch(lens, 2, d, 16, torch.float16, seed=d + new[0])
+    B.v[:] = torch.from_numpy(O.value(_f64(B.v[:1]))).to(B.dev, B.dtype)
+    B.store_all()
+    want = B.v[0].repeat_interleave(rep, 0)[None].expand(sum(new), -1, -1).clone()
+    at = 0
+    for t, n in zip(lens, new):
+        want[at:at + max(0, n - t)] = 0
+        at += n
+    for scale in (1.0, 2.0, 4.0, 6.0, 8.0, 12.0):
+        q = B.query(new, rep, scale)
+        out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=max(new), max_len=max_len)
+        B.check(q, new, out, lse)
+        assert torch.equal(out, want), scale
