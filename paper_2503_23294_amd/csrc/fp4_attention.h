@@ -86,11 +86,11 @@ __device__ __forceinline__ float add_rounded(uint32_t w, float sum) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 
-// Power of two that brings a row of bf16 values, the largest of which is `top`, below 2; 1 for rows of zeros.  Not far from the ends of
-// the range, where its reciprocal would be lost.
+// Power of two that brings a row of bf16 values, the largest of which is `top`, below 2 (the largest of all below 4, so that the reciprocal is a
+// normal number); 1 for rows of zeros.
 __device__ __forceinline__ float row_factor(float top) {
   const uint32_t e = __builtin_bit_cast(uint32_t, top) >> 23;
-  return top == 0.f ? 1.f : __builtin_bit_cast(float, (e < 20u ? 20u : e > 230u ? 230u : e) << 23);
+  return top == 0.f ? 1.f : __builtin_bit_cast(float, (e < 1u ? 1u : e > 253u ? 253u : e) << 23);
 }
 
 // A word of the page table through the scalar data path: the table is written by other launches only, and the address is wave-uniform.

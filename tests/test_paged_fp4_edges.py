@@ -321,3 +321,17 @@ def test_values_that_are_all_alike_come_out_as_they_are(lens, new, rep, max_len,
         out, lse = ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=max(new), max_len=max_len)
         B.check(q, new, out, lse)
         assert torch.equal(out, want), scale
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 5, 40])
+@pytest.mark.parametrize("power", [120, 125, 103, -105, -112, -120])
+def test_bf16_queries_of_any_size(power, new):
+    """Queries near the ends of bf16's range, and a scale that brings their logits back: results as for queries of ordinary size."""
+    B = Batch([400, 77], 2, 128, 16, torch.bfloat16, seed=71)
+    B.store_all()
+    q = B.query([new, new], 4) * 2.0 ** power
+    assert torch.isfinite(q).all()
+    sm_scale = 2.0 ** -power / 128 ** 0.5
+    out, lse = ck.cocktail_fp4_attention(B.cache, q, sm_scale=sm_scale)
+    B.check(q, [new, new], out, lse, sm_scale)
