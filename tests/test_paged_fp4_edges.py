@@ -335,3 +335,40 @@ def test_bf16_queries_of_any_size(power, new):
     sm_scale = 2.0 ** -power / 128 ** 0.5
     out, lse = ck.cocktail_fp4_attention(B.cache, q, sm_scale=sm_scale)
     B.check(q, [new, new], out, lse, sm_scale)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("lens,new,rep", [([300, 120], [1, 1], 4), ([5000, 120], [3, 2], 16), ([5000, 120], [2, 4], 16), ([400, 399], [40, 70], 4),
+                                          ([4000], [70], 4)])
+def test_queries_that_are_not_finite(lens, new, rep, dtype):
+    """A query with a NaN has a result and a logarithm of NaN, also where sums are held against limits; one with an infinity whose logits are none or infinite
+    as well; all other queries have what they have without them.  Queries without keys have zeros, whatever they are."""
+    B = Batch(lens, 2, 128, 16, DTYPES[dtype], seed=81)
+    B.k[:, :, 7] = 1.5 * torch.sign(B.k[:, :, 7].float()).to(B.dtype) + 0.25       # channel 7 is stored as zero nowhere
+    B.store_all()
+    q = B.query(new, rep)
+    call = lambda q: ck.cocktail_fp4_attention(B.cache, q, B.starts(new), max_new=max(new))  # noqa: E731
+    out, lse = call(q)
+    B.check(q, new, out, lse)
+    heads, n = 2 * rep, sum(new)
+    bad = [(0, 0), (0, heads - 1), (n - 1, 1), (n // 2, heads // 2)]
+    for value in (float("nan"), float("inf"), -float("inf")):
+        x = q.clone()
+        for i, h in bad:
+            x[i, h, 7] = value
+        got, gl = call(x)
+        same = torch.ones(n, heads, dtype=torch.bool, device=B.dev)
+        for i, h in bad:
+            same[i, h] = False
+            assert torch.isnan(got[i, h]).all() and torch.isnan(gl[i, h]), (value, i, h)
+        assert torch.equal(got[same], out[same]) and torch.equal(gl[same], lse[same])
+    many = [t + 2 for t in lens] if max(lens) < 1000 else None
+    if many:
+        x = torch.full((sum(many), heads, 128), float("nan"), device=B.dev, dtype=B.dtype)
+        got, gl = ck.cocktail_fp4_attention(B.cache, x, B.starts(many), max_new=max(many))
+        at = 0
+        for t, m in zip(lens, many):
+            assert (got[at:at + 2] == 0).all() and torch.isneginf(gl[at:at + 2]).all()
+            assert torch.isnan(got[at + 2:at + m]).all() and torch.isnan(gl[at + 2:at + m]).all()
+            at += m
