@@ -618,7 +618,7 @@ int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32
  *   workspace DEVICE, at least cocktail_fp4_attention_workspace bytes for the same sizes, 16-byte aligned, not initialised; calls
  *             that share one must not overlap in time
  *
- * Keys on a page that is no page of the pool are left out.  Calls on the same inputs agree bit for bit.
+ * Keys on a page that is no page of the pool, or behind what the table row can hold, are left out.  Calls on the same inputs agree bit for bit.
  * num_q_heads / num_kv_heads from 1 to COCKTAIL_MAX_Q_PER_KV.  Up to four launches.  Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
  */
 int cocktail_fp4_attention_workspace(const cocktail_fp4_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,

@@ -44,15 +44,18 @@ struct Fp4Attention {
   float* tile_o;
 };
 
-// A sequence as one kernel sees it: its rows (none if they are the other kernel's), tokens.
+// A sequence as one kernel sees it: its rows (none if they are the other kernel's), tokens that the table holds, tokens before the new ones.  Query i
+// sees tokens 0 .. past + i, as far as there are any.
 struct Fp4Seq {
-  int first, n, len;
+  int first, n, len, past;
 };
 
 __device__ __forceinline__ Fp4Seq decode_seq(const Fp4Attention& a, int b) {
   const Fp4Span s = fp4_span(a.batch, b);
-  return {s.first, s.count * a.rep <= a.decode_rows ? s.count : 0, fp4_len(a.batch, b)};
+  const int len = fp4_len(a.batch, b);
+  return {s.first, s.count * a.rep <= a.decode_rows ? s.count : 0, fp4_held(a.batch, len), len - s.count};
 }
+__device__ __forceinline__ int seen_by(const Fp4Seq& s, int i) { return min(s.past + i + 1, s.len); }
 
 // Operands of 16 query rows that a sequence needs in the decode kernel, its units of keys, and what they cost: the conversions of K and V
 // once, and products and weights per operand, each about as long (8 x 16K, 1 .. 6 tokens of 8 heads: 55.6 us by operands alone, 47.4 by operands + 1,

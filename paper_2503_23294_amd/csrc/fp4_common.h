@@ -38,9 +38,14 @@ __device__ __forceinline__ Fp4Span fp4_span(const Fp4Batch& a, int b) {
   const bool ok = s0 >= 0 && s1 >= s0 && s1 <= a.total && s1 - s0 <= a.max_new;
   return {int32_t(s0), ok ? int32_t(s1 - s0) : 0};
 }
+// Tokens of a sequence, and those of them that its row of the table can hold (resize makes no more, but lengths may come from elsewhere).
 __device__ __forceinline__ int fp4_len(const Fp4Batch& a, int b) {
-  const int n = a.seq_lens[b], most = a.table_stride * a.page_size;
-  return n < 0 ? 0 : n > most ? most : n;
+  const int n = a.seq_lens[b];
+  return n < 0 ? 0 : n;
+}
+__device__ __forceinline__ int fp4_held(const Fp4Batch& a, int len) {
+  const int most = a.table_stride * a.page_size;
+  return len > most ? most : len;
 }
 
 // Inclusive prefix sum over the lanes of a wave, without a trip through shared memory: shifts inside rows of 16, then the last lane of a row

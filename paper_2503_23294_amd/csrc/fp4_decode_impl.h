@@ -77,6 +77,11 @@ __device__ __forceinline__ Fp4Line make_line(const Fp4Attention& a, int32_t* pre
   return r;
 }
 
+__device__ __forceinline__ Fp4Seq of_lane(const Fp4Seq& s, int lane) {
+  return {__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.len, lane),
+          __builtin_amdgcn_readlane(s.past, lane)};
+}
+
 // The sequence at place u of the line: the last one that costs anything and has no more than u before it.
 struct Fp4Place {
   int b, before, cost;   // cost of a kv head
@@ -90,7 +95,7 @@ __device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4L
     p.b = 63 - __builtin_clzll(candidates);
     p.before = __builtin_amdgcn_readlane(line.before, p.b);
     p.cost = __builtin_amdgcn_readlane(line.cost, p.b);
-    p.seq = {__builtin_amdgcn_readlane(line.seq.first, p.b), __builtin_amdgcn_readlane(line.seq.n, p.b), __builtin_amdgcn_readlane(line.seq.len, p.b)};
+    p.seq = of_lane(line.seq, p.b);
   } else {
     int b = 0, e = a.batch.num_seqs;
     while (e - b > 1) {
@@ -102,8 +107,7 @@ __device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4L
     p.b = __builtin_amdgcn_readfirstlane(b);
     p.before = __builtin_amdgcn_readfirstlane(pre[p.b]);
     p.cost = __builtin_amdgcn_readfirstlane(pre[p.b + 1]) - p.before;
-    const Fp4Seq s = decode_seq(a, p.b);
-    p.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+    p.seq = of_lane(decode_seq(a, p.b), 0);
   }
   return p;
 }
@@ -157,7 +161,7 @@ __device__ __forceinline__ int nth_longest(const Fp4Attention& a, int number, Fp
 #pragma unroll
   for (int w = 0; w < kWholeWaves; ++w) before += counted[w][lane];
   const int b = __builtin_ctzll(__ballot(lane < a.batch.num_seqs && before == number));
-  *seq = {__builtin_amdgcn_readlane(s.first, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.len, b)};
+  *seq = of_lane(s, b);
   return b;
 }
 
@@ -223,8 +227,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
         // more sequences than rows: the workgroups are for those that have any
         place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
         if (place.b < 0) return;
-        const Fp4Seq s = decode_seq(a, place.b);
-        place.seq = {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len)};
+        place.seq = of_lane(decode_seq(a, place.b), 0);
       }
       if (place.seq.n == 0) return;
       const uint32_t units = decode_units(place.seq);
@@ -341,14 +344,14 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
         else lds_q[wave][rt][s][lane] = raw[rt][s];
       }
       const int r = rt * 16 + c16;
-      lim[rt] = r < rows ? len - n + r / a.rep + 1 : 0;
+      lim[rt] = r < rows ? seen_by(place.seq, r / a.rep) : 0;
       m[rt] = kNoMax;
       lsum[rt] = 0.f;
       l[rt] = {};
 #pragma unroll
       for (int ct = 0; ct < kChannelTiles; ++ct) o[rt][ct] = f32x4{};
     }
-    const int free_below = len - n + 1;   // tokens that every query sees
+    const int free_below = seen_by(place.seq, 0);   // tokens that every query sees
 
     auto compute = [&](auto operands, Fp4Tile<HD>& ta, Fp4Tile<HD>& tb, int tok0) __attribute__((always_inline)) {
       constexpr int kLive = decltype(operands)::value;   // of the RT operands of queries

@@ -47,15 +47,16 @@ __device__ __forceinline__ Fp4Item find_item(const Fp4Batch& a, const int32_t* l
   }
   it.seq = b;
   const Fp4Span s = fp4_span(a, b);
-  const int p0 = fp4_len(a, b) - s.count;                            // position of the range's first token
+  const int p0 = fp4_len(a, b) - s.count;                            // position of the range's first token (the last one's is below 2^31)
   const int q0 = p0 >> 2;                                            // its quad (rounded down: p0 may be negative)
   const int k = quad - quad_number(lds_starts[b], b);
+  it.active = k >= 0 && s.count > 0 && q0 + k <= (p0 + s.count - 1) >> 2;
+  if (!it.active) return it;
   it.pos = (q0 + k) * 4;
-  it.row = s.first + it.pos - p0;
+  it.row = s.first + (it.pos - p0);
   it.lo = p0 > it.pos ? p0 - it.pos : 0;
   const int left = p0 + s.count - it.pos;
   it.hi = left < 4 ? left : 4;
-  it.active = k >= 0 && s.count > 0 && it.lo < it.hi;
   return it;
 }
 

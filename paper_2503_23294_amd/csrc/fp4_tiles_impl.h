@@ -78,10 +78,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   const int tile = __builtin_amdgcn_readfirstlane(found[1]);
   const Fp4Span span = fp4_span(bt, b);
   const int first = __builtin_amdgcn_readfirstlane(span.first), n = __builtin_amdgcn_readfirstlane(span.count);
-  const int rows = n * a.rep, len = __builtin_amdgcn_readfirstlane(fp4_len(bt, b));
+  const int rows = n * a.rep, all = __builtin_amdgcn_readfirstlane(fp4_len(bt, b)), len = fp4_held(bt, all);
+  const Fp4Seq seq = {first, n, len, all - n};
   const int r0 = tile * kTileRows;
   const int last_row = (r0 + kTileRows < rows ? r0 + kTileRows : rows) - 1;
-  int most = len - n + last_row / a.rep + 1;          // keys that the last row sees
+  int most = seen_by(seq, last_row / a.rep);          // keys that the last row sees
   most = most < 0 ? 0 : most;
   const uint32_t steps = (most + kTileKeys - 1) / kTileKeys;
   const int k0 = steps * uint32_t(split) / splits, k1 = steps * uint32_t(split + 1) / splits;   // (steps < 2^25, splits up to 64)
@@ -90,9 +91,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   const int row_lane = lane & 31, half = lane >> 5;
   const int r = r0 + wave * 32 + row_lane, i = r / a.rep;
   const bool live = r < rows;
-  const int lim = live ? len - n + i + 1 : 0;
+  const int lim = live ? seen_by(seq, i) : 0;
   const int wave_first = r0 + wave * 32;
-  const int wave_free = wave_first + 31 < rows ? len - n + wave_first / a.rep + 1 : 0;   // below: no masking
+  const int wave_free = wave_first + 31 < rows ? seen_by(seq, wave_first / a.rep) : 0;   // below: no masking
 
   // A thread's pieces of every 64 keys: kPieces words (of eight channels) of a key of K, and as many pairs of channels of a quad of tokens of V.
   constexpr int kPieces = HD * 8 / kThreads;

@@ -372,3 +372,63 @@ def test_queries_that_are_not_finite(lens, new, rep, dtype):
             assert (got[at:at + 2] == 0).all() and torch.isneginf(gl[at:at + 2]).all()
             assert torch.isnan(got[at + 2:at + m]).all() and torch.isnan(gl[at + 2:at + m]).all()
             at += m
+
+
+# ---- lengths and starts ----------------------------------------------------------------------------------------------------------
+
+
+@gpu
+@pytest.mark.parametrize("num_seqs", [2, 70])
+@pytest.mark.parametrize("d,page,new", [(128, 16, [1, 1]), (64, 32, [10, 7]), (128, 16, [40, 3]), (64, 16, [9, 70])])
+def test_lengths_beyond_the_table(d, page, new, num_seqs):
+    """Lengths that the rows of the table cannot hold (they come from elsewhere: cocktail_pages_resize makes none): tokens behind the last column are
+    not stored, read as zeros and are no keys; all others are what they are."""
+    dev, room = torch.device("cuda:0"), 64
+    rng = np.random.default_rng(d + num_seqs)
+    for lens in ([70, 66], [64, 65], [2 ** 31 - 1, 100], [room + 2 * new[0] + 1, 2 ** 31 - 3]):
+        columns = room // page
+        table = rng.permutation(num_seqs * columns).astype(np.int32).reshape(num_seqs, columns)
+        all_lens = np.zeros(num_seqs, np.int64)
+        at = (0, num_seqs - 1)
+        all_lens[list(at)] = lens
+        counts = np.zeros(num_seqs, np.int64)
+        counts[list(at)] = new
+        t = lambda a: torch.from_numpy(a.astype(np.int32)).to(dev)  # noqa: E731
+        pages = ck.PageTable.of(t(table), t(all_lens), t(np.ones(num_seqs * columns)), page)
+        cache = ck.Fp4Cache(pages, 2, d)
+        total = sum(new)
+        starts = t(np.concatenate([[0], np.cumsum(counts)]))
+        # what is there before: 64 tokens of every sequence
+        k0, v0 = (torch.randn(num_seqs * room, 2, d, device=dev, dtype=torch.float16) for _ in range(2))
+        pages.seq_lens.fill_(room)
+        ck.cocktail_fp4_store(cache, k0, v0)
+        want = [O.value(_f64(x)).reshape(num_seqs, room, 2, d) for x in (k0, v0)]
+        pages.seq_lens.copy_(t(all_lens))
+        k, v, q = (torch.randn(total, h, d, device=dev, dtype=torch.float16) for h in (2, 2, 4))
+        ck.cocktail_fp4_store(cache, k, v, starts)
+        gk, gv = ck.cocktail_fp4_gather(cache, total, starts)
+        out, lse = ck.cocktail_fp4_attention(cache, q, starts, max_new=max(new))
+        row = 0
+        for b, length, n in zip(at, lens, new):
+            read = np.zeros((2, n, 2, d))
+            for i in range(n):
+                pos = length - n + i
+                if 0 <= pos < room:
+                    for x, given in enumerate((k, v)):
+                        want[x][b, pos] = read[x, i] = O.value(_f64(given[row + i]))
+            rows = slice(row, row + n)
+            assert np.array_equal(_f64(gk[rows]), read[0]) and np.array_equal(_f64(gv[rows]), read[1])
+            # queries see at most what there is
+            for i in range(n):
+                seen = max(0, min(length - n + i + 1, room))
+                w, wl, mean_v, _ = O.attention(_f64(q[row + i:row + i + 1]), want[0][b, :seen], want[1][b, :seen])
+                # the result's rounding, the weights' twice; logits of unit normals add less than the slack of 2^-12
+                assert (np.abs(_f64(out[row + i:row + i + 1]) - w) <= 2.0 ** -11 * np.abs(w) + 2.5 * 2.0 ** -11 * mean_v).all(), (b, i)
+                if seen == 0:
+                    assert torch.isneginf(lse[row + i]).all()
+                else:
+                    assert (np.abs(_f64(lse[row + i:row + i + 1]) - wl) <= 2.0 ** -12).all(), (b, i)
+            row += n
+        pages.seq_lens.fill_(room)
+        gk, gv = ck.cocktail_fp4_gather(cache, num_seqs * room)
+        assert np.array_equal(_f64(gk).reshape(want[0].shape), want[0]) and np.array_equal(_f64(gv).reshape(want[1].shape), want[1])
