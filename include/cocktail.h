@@ -489,7 +489,7 @@ typedef struct cocktail_page_table {
   int32_t* refs;        /* DEVICE [num_pages]                                                         */
   int32_t* status;      /* DEVICE [4]                                                                 */
   int32_t num_seqs;     /* 1 .. COCKTAIL_MAX_SEQS                                                     */
-  int32_t table_stride; /* pages a sequence can have; table_stride * page_size < 2^31                 */
+  int32_t table_stride; /* pages a sequence can have; table_stride * page_size and num_seqs * table_stride < 2^31 */
   int32_t page_size;    /* tokens per page                                                            */
   int32_t num_pages;    /* pages of every pool                                                        */
 } cocktail_page_table;

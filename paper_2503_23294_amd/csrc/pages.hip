@@ -329,6 +329,9 @@ int check_page_table(const cocktail_page_table* p) {
     return fail(COCKTAIL_EINVAL, "table_stride, page_size and num_pages must be positive (pages up to 2^30)");
   if (int64_t(p->table_stride) * p->page_size >= (int64_t(1) << 31))
     return fail(COCKTAIL_EINVAL, "table_stride * page_size = %lld tokens: must be below 2^31", (long long)(int64_t(p->table_stride) * p->page_size));
+  // (a resize adds up in 32 bits how many pages all sequences take)
+  if (int64_t(p->num_seqs) * p->table_stride >= (int64_t(1) << 31))
+    return fail(COCKTAIL_EINVAL, "num_seqs * table_stride = %lld entries: must be below 2^31", (long long)(int64_t(p->num_seqs) * p->table_stride));
   if ((reinterpret_cast<uintptr_t>(p->table) | reinterpret_cast<uintptr_t>(p->seq_lens) | reinterpret_cast<uintptr_t>(p->refs) |
        reinterpret_cast<uintptr_t>(p->status)) & 3)
     return fail(COCKTAIL_EALIGN, "table, seq_lens, refs and status must be 4-byte aligned");

@@ -1,6 +1,7 @@
 """The paged 4-bit cache where it can go wrong besides what test_paged_fp4.py looks at: waits, threads, streams, far tails of a softmax, unusual queries,
 starts and lengths."""
 import contextlib
+import ctypes as C
 import re
 import shutil
 import subprocess
@@ -432,3 +433,16 @@ def test_lengths_beyond_the_table(d, page, new, num_seqs):
         pages.seq_lens.fill_(room)
         gk, gv = ck.cocktail_fp4_gather(cache, num_seqs * room)
         assert np.array_equal(_f64(gk).reshape(want[0].shape), want[0]) and np.array_equal(_f64(gv).reshape(want[1].shape), want[1])
+
+
+def test_tables_of_more_entries_than_32_bits_count_are_refused():
+    """A resize adds up the pages that all sequences take; 2048 sequences of 2^20 pages are 2^31, whose sum would come out negative."""
+    L = _lib.lib()
+    n = C.c_size_t(0)
+    for num_seqs, stride, page, code in ((2048, 1 << 20, 16, _lib.EINVAL), (4096, 1 << 20, 1, _lib.EINVAL), (2, 1 << 30, 1, _lib.EINVAL),
+                                         (2047, 1 << 20, 16, 0), (4096, (1 << 19) - 1, 16, 0)):
+        d = _lib.PageTableDesc(4096, 4096, 4096, 4096, num_seqs, stride, page, 64)
+        assert L.cocktail_pages_workspace(C.byref(d), C.byref(n)) == code, (num_seqs, stride)
+        if code:
+            assert L.cocktail_pages_resize(C.byref(d), 4096, None, 0, 0, 4096, 1 << 20, None) == code
+            assert b"2^31" in L.cocktail_last_error()
