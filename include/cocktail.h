@@ -504,7 +504,8 @@ int cocktail_pages_workspace(const cocktail_page_table* pages, size_t* bytes);
  * other sequences hold takes a copy of it first (before its further pages), so that what it stores there is its own; where a page
  * is held by growing sequences only, the last of them keeps it.  The copies are made in all `num_pools` pools.
  * All or nothing: if pages are lacking, or the table has too few columns, nothing changes and status[0] says so; the
- * cocktail_fp4_store calls that follow then store nothing, until a resize succeeds.
+ * cocktail_fp4_store calls that follow then store nothing, until a resize succeeds; all other calls go by the lengths as they are (cocktail_pages_check
+ * tells).
  *
  *   delta       DEVICE int32 [num_seqs]
  *   pools       HOST array of DEVICE pointers to pools of num_pages pages of page_bytes bytes each; 16-byte aligned
@@ -582,7 +583,8 @@ int cocktail_fp4_page_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t page
  *   dtype     COCKTAIL_FP16 or COCKTAIL_BF16
  *   total     rows; 0 is fine
  *   starts    DEVICE int32 [num_seqs + 1], ascending from 0 to total, or NULL: total / num_seqs rows for every sequence
- *             (total a multiple of num_seqs).  A sequence whose range is not within [0, total] is left out.
+ *             (total a multiple of num_seqs).  A sequence whose range is not within [0, total] is left out.  (Where starts descend, the
+ *             rows of sequences that begin below an earlier start have no defined result.)
  *
  * One launch.  Errors: EINVAL, EUNSUPPORTED (head_dim), EALIGN, EHIP.
  */

@@ -12,8 +12,8 @@
 
 namespace cocktail {
 
-// K in chunks of 32 keys, a ring of five: a step reads the two behind its first chunk (which was read before the barrier that it began with) and
-// writes the two behind those, the second of them into the place of that first chunk.  V of 64 keys, twice.
+// K in chunks of 32 keys, a ring of five.  A step begins with the logits of its first chunk, reads the next two and writes the fourth and the fifth behind
+// it: the fifth takes the place of the first, which was read before the barrier that the step began with.  V of 64 keys, twice.
 constexpr int kChunk = 32, kRing = 5;
 constexpr float kSumLimit = 61440.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then (behind a new reference it is 16 * 2^7 at most)
 template <int HD>

@@ -446,3 +446,70 @@ def test_tables_of_more_entries_than_32_bits_count_are_refused():
         if code:
             assert L.cocktail_pages_resize(C.byref(d), 4096, None, 0, 0, 4096, 1 << 20, None) == code
             assert b"2^31" in L.cocktail_last_error()
+
+
+@gpu
+@pytest.mark.parametrize("starts,valid", [([0, 40, 30, 30], [0]), ([0, 40, 65, 99], [0, 1]), ([-3, 40, 65, 98], [1, 2]), ([0, 40, 120, 98], [0]),
+                                          ([5, 40, 65, 98], [0, 1, 2]), ([0, 40, -1, 98], [0]), ([0, 40, 65, 2 ** 31 - 1], [0, 1])])
+@pytest.mark.parametrize("rep", [1, 4])
+def test_ranges_that_are_none_next_to_good_ones(starts, valid, rep):
+    """Sequences whose range is within the batch are stored, read back and attended to as ever; nothing is written for the others."""
+    B = Batch([40, 30, 33], 2, 128, 16, torch.float16, seed=5)
+    B.store_all()
+    x, y = (torch.randn(98, 2, 128, device=B.dev).half() for _ in range(2))
+    q = torch.randn(98, 2 * rep, 128, device=B.dev).half()
+    dev_starts = torch.tensor(starts, dtype=torch.int32, device=B.dev)
+    ck.cocktail_fp4_store(B.cache, x, y, dev_starts)
+    gk, gv = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    ck.cocktail_fp4_gather(B.cache, 98, dev_starts, out=(gk, gv))
+    out, lse = torch.full_like(q, 7.0), torch.full((98, 2 * rep), 7.0, device=B.dev)
+    ck.cocktail_fp4_attention(B.cache, q, dev_starts, out=out, lse=lse)
+    others = torch.ones(98, dtype=torch.bool)
+    for b in valid:
+        n = starts[b + 1] - starts[b]
+        rows = slice(starts[b], starts[b + 1])
+        others[rows] = False
+        mine = B.rows(b)
+        last = slice(mine.stop - n, mine.stop)
+        B.k[last], B.v[last] = x[rows], y[rows]
+        assert np.array_equal(_f64(gk[rows]), O.value(_f64(x[rows]))) and np.array_equal(_f64(gv[rows]), O.value(_f64(y[rows])))
+        B.check(q[rows], [n if i == b else 0 for i in range(3)], out[rows], lse[rows])
+    for t in (gk, gv, out, lse):
+        assert (t.cpu()[others] == 7.0).all()
+    # the pool: what has been stored, and nothing else
+    k, v = ck.cocktail_fp4_gather(B.cache, 103, B.starts(B.lens))
+    assert np.array_equal(_f64(k), O.value(_f64(B.k))) and np.array_equal(_f64(v), O.value(_f64(B.v)))
+
+
+@gpu
+def test_workspaces_that_grow_while_graphs_live():
+    """Eager calls of unlike sizes on one stream, each larger one with a new workspace, between replays of graphs that were captured when the
+    workspaces were smaller; resizes and compactions use the same ones."""
+    B = Batch([3000, 900, 40], 2, 128, 16, torch.float16, seed=91)
+    B.store_all()
+    sizes = [[1, 1, 1], [4, 1, 2], [8, 8, 8], [70, 3, 20], [16, 16, 16]]
+    queries = [B.query(new, 4) for new in sizes]
+    call = lambda i: ck.cocktail_fp4_attention(B.cache, queries[i], B_starts[i], max_new=max(sizes[i]), max_len=3000)  # noqa: E731
+    B_starts = [B.starts(new) for new in sizes]
+    want, graphs, outs = [], [], []
+    side = torch.cuda.Stream()
+    for i in range(len(sizes)):
+        out, lse = call(i)
+        B.check(queries[i], sizes[i], out, lse)
+        want.append((out.clone(), lse.clone()))
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            outs.append(call(i))
+        graphs.append(graph)
+    nothing = torch.zeros(3, dtype=torch.int32, device=B.dev)
+    for turn in range(6):
+        for i in (turn % 5, (turn + 2) % 5, 4 - turn % 5):
+            outs[i][0].zero_()
+            outs[i][1].zero_()
+            graphs[i].replay()
+            got = call((i + turn) % 5)
+            ck.cocktail_pages_resize(B.pages, nothing, [B.cache.pool])
+            assert torch.equal(got[0], want[(i + turn) % 5][0]) and torch.equal(got[1], want[(i + turn) % 5][1])
+            assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
+        ck.cocktail_pages_compact(B.pages, [B.cache.pool])
