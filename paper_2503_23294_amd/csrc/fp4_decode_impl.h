@@ -1,8 +1,8 @@
 // Decode kernel of cocktail_fp4_attention: up to 64 query rows (new tokens x query heads of a kv head) per (sequence, kv head).
 //
-// Bound by memory up to 16 rows: a key costs 2 * 17/32 D bytes and 4 D * rows operations.  Measured: 128K tokens, 40 heads (713 MB) 108 us, 6.6 TB/s;
-// eight sequences of 1 .. 128K, 8 kv heads, 4 query heads each (698 MB) 109 us; with more rows by the conversions, exponentials and
-// products: eight sequences of 9 .. 16K, 8 kv heads, 8 .. 48 rows (102 MB) 32 us.  What it takes to read at the rate of the memory:
+// Bound by memory up to 16 rows: a key costs 2 * 17/32 D bytes and 4 D * rows operations.  Measured (averages): 128K tokens, 40 heads (713 MB) 114 us, 6.3 TB/s;
+// eight sequences of 1 .. 128K, 8 kv heads, 4 query heads each (698 MB) 113 .. 119 us; with more rows by the conversions, exponentials and
+// products: eight sequences of 9 .. 16K, 8 kv heads, 8 .. 48 rows (102 MB) 34 us.  What it takes to read at the rate of the memory:
 //  * Work is cut by tokens, not by sequences: the units of 32 tokens of all (sequence, kv head) segments lie one behind the other, each as long as it
 //    costs, and every wave takes those that begin in its share of that line, whatever the lengths are.  The numbering is made on the device from seq_lens, so that lengths can change
 //    under a captured graph.  A segment inside one share is finished by its wave, the others leave a partial state per wave.

@@ -10,7 +10,7 @@ namespace cocktail {
 // side, and no two threads write the same byte): sixteen bytes of each of four rows, so that neighbouring threads read and write
 // neighbouring memory on both sides.  The four threads of a group of 32 channels find its scale together.  (A whole group per
 // thread, 64 bytes of a row, was 4 times slower on the way back, whose stores then leave lines half written, and a third slower on
-// the way in.)  Measured: 32K tokens of 32 heads of 128, 0.68 GB each way, stored in 125 us (5.4 TB/s) and read back in 95 (7.2); a step
+// the way in.)  Measured: 32K tokens of 32 heads of 128, 0.68 GB each way, stored in 133 us (5.1 TB/s) and read back in 97 (7.0); a step
 // of 8 sequences 4 us each way.
 // Numbering: per quad (K or V, head, eight channels), channels fastest.  Quads are numbered over the batch with room for one that
 // starts and one that ends inside a sequence's range: those of sequence b are first[b] / 4 + 2 b and following.

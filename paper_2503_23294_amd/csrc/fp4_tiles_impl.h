@@ -3,8 +3,8 @@
 // Bound by the matrix cores and, close behind, by the exponentials of the softmax.  A workgroup takes 128 or 256 rows of one (sequence, kv head), 32
 // per wave, and walks over the keys 64 at a time: codes are loaded a step or two ahead of their use, become fp16 once per workgroup on
 // their way to LDS (K as rows of channels, V transposed, both as the operands of 32x32x16 products want them), and serve all waves.
-// Measured: 2048 tokens of 4 x 8 heads of 128 behind 30K 1.08 .. 1.12 ms (950 .. 990 TFLOP/s; a large library product of fp16 matrices reaches 1132), two whole prompts of 8190 and
-// 4095 tokens, 32 heads, 0.75 .. 0.77 ms (890 .. 915, of the products that are not masked).
+// Measured: 2048 tokens of 4 x 8 heads of 128 behind 30K 1.08 .. 1.13 ms (940 .. 990 TFLOP/s; a large library product of fp16 matrices reaches 1132), two whole prompts of 8190 and
+// 4095 tokens, 32 heads, 0.75 .. 0.77 ms (890 .. 920, of the products that are not masked).
 // S^T = K Q^T leaves a lane with one query row and half the keys of a step, in the order in which O^T = V^T P^T takes them (the
 // tokens of V lie in LDS in that order), so weights stay in their lanes.
 #pragma once
