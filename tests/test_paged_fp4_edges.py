@@ -513,3 +513,30 @@ def test_workspaces_that_grow_while_graphs_live():
             assert torch.equal(got[0], want[(i + turn) % 5][0]) and torch.equal(got[1], want[(i + turn) % 5][1])
             assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
         ck.cocktail_pages_compact(B.pages, [B.cache.pool])
+
+
+@gpu
+def test_calls_on_a_given_stream_while_it_is_captured():
+    """stream= names the stream that is captured, or one that joins the capture: tensors are recorded there as outside of a capture, and replays give what
+    eager calls give, also after temporaries of the capture have been dropped."""
+    B = Batch([2500, 64, 130], 2, 64, 16, torch.float16, seed=101)
+    B.store_all()
+    new = [2, 1, 1]
+    q, starts = B.query(new, 6), B.starts(new)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        first = ck.cocktail_fp4_attention(B.cache, q * 1.0, starts, max_new=2, stream=side)
+        other.wait_stream(side)
+        second = ck.cocktail_fp4_attention(B.cache, q, starts, max_new=2, sm_scale=0.01, stream=other)
+        side.wait_stream(other)
+    for _ in range(5):
+        q.copy_(B.query(new, 6))
+        graph.replay()
+        for got, scale in ((first, 0.0), (second, 0.01)):
+            out, lse = ck.cocktail_fp4_attention(B.cache, q, starts, max_new=2, sm_scale=scale)
+            assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+        junk = [torch.randn_like(q) for _ in range(8)]
+        torch.cuda.synchronize()
+        del junk
