@@ -512,7 +512,8 @@ int cocktail_pages_workspace(const cocktail_page_table* pages, size_t* bytes);
  *   num_pools   0 .. COCKTAIL_MAX_POOLS; with 0 nothing can be copied: for callers whose sequences share no partly filled pages
  *               (where one has to be, nothing is done and status[0] is -2)
  *   page_bytes  a multiple of 16
- *   workspace   DEVICE, cocktail_pages_workspace bytes, 16-byte aligned, not initialised
+ *   workspace   DEVICE, cocktail_pages_workspace bytes, 16-byte aligned, not initialised; shared between calls as that of
+ *               cocktail_fp4_attention
  *
  * One launch, and one for the copies if there are pools.  Errors: EINVAL, EALIGN, ENOSPACE, EHIP.
  */
@@ -618,7 +619,7 @@ int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32
  *   out       DEVICE [total][num_q_heads][D], 16-byte aligned; zeros for a query without keys
  *   lse       DEVICE fp32 [total][num_q_heads] natural log-sum-exp (-inf without keys), or NULL
  *   workspace DEVICE, at least cocktail_fp4_attention_workspace bytes for the same sizes, 16-byte aligned, not initialised; calls
- *             that share one must not overlap in time
+ *             that share one must not overlap in time, nor be made by two threads at once (a call is several launches)
  *
  * Keys on a page that is no page of the pool, or behind what the table row can hold, are left out.  Calls on the same inputs agree bit for bit.
  * num_q_heads / num_kv_heads from 1 to COCKTAIL_MAX_Q_PER_KV.  Up to four launches.  Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
