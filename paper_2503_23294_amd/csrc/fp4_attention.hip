@@ -1,4 +1,4 @@
-// cocktail_fp4_attention: which kernel serves which sequences, the merge of partial states, the C entry.
+// cocktail_fp4_attention: which kernel serves which sequences, the C entry.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -6,132 +6,6 @@
 
 #include "fp4_decode_impl.h"
 #include "fp4_tiles_impl.h"
-
-namespace cocktail {
-
-// The sequence of new token t: the last one that does not start behind it (those before it with the same start are empty).
-__device__ __forceinline__ int seq_of_row(const Fp4Batch& bt, int t) {
-  if (!bt.starts) return t / bt.uniform;
-  int b = 0, e = bt.num_seqs;
-  while (e - b > 1) {
-    const int mid = (b + e) >> 1;
-    if (bt.starts[mid] <= t) b = mid;
-    else e = mid;
-  }
-  return b;
-}
-
-// Sum of a row's partial states: `parts` of them, the first at row `first_slot` of the arrays and the others at second_slot, second_slot + step ...
-// Wave `wave` of `waves` takes every waves-th; o: the lane's channels, l and lsum: whole sums (in every wave).
-template <int HD>
-__device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* po, int64_t first_slot, int64_t second_slot, int64_t step, int parts,
-                                                  int wave, int waves, int lane) {
-  constexpr int kPer = HD / 64;
-  auto slot = [&](int k) -> int64_t { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
-  Merged<HD> r = {};
-  r.top = kNoMax;
-  for (int k = lane; k < parts; k += 64) r.top = fmaxf(r.top, ml[slot(k) * 3]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) r.top = fmaxf(r.top, __shfl_xor(r.top, d));
-  for (int base = 0; base < parts; base += 64) {
-    float w = 0.f;
-    if (base + lane < parts) {
-      const float* x = ml + slot(base + lane) * 3;
-      w = __builtin_amdgcn_exp2f(x[0] - r.top);
-      r.l += w * x[1];
-      r.lsum += w * x[2];
-    }
-    const int n = parts - base < 64 ? parts - base : 64;
-    // eight states at a time on their way; behind the last one it is the last one again, with no weight
-    for (int k = wave; k < n; k += 8 * waves) {
-      float x[8][kPer];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float* src = po + slot(base + min(k + i * waves, n - 1)) * HD + lane * kPer;
-#pragma unroll
-        for (int y = 0; y < kPer; ++y) x[i][y] = src[y];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int at = k + i * waves;
-        const float wk = at < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(at, n - 1))) : 0.f;
-#pragma unroll
-        for (int y = 0; y < kPer; ++y) r.o[y] += at < n ? wk * x[i][y] : 0.f;
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    r.l += __shfl_xor(r.l, d);
-    r.lsum += __shfl_xor(r.lsum, d);
-  }
-  return r;
-}
-
-// Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves of its segment left, if there were several, and
-// writes rows without keys.  WAVES waves for a row, at least four to a workgroup.  Numbered by sequence, most_new tokens each, or, where most of those
-// would have no token, by new token (most_new 0), which is looked for among the sequences.
-template <int HD, int WAVES>
-__global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void fp4_merge_decode_kernel(Fp4Attention a, int most_new) {
-  constexpr int kPer = HD / 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
-  __shared__ float o[WAVES][HD];
-  const Fp4Batch& bt = a.batch;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
-  const uint32_t heads = bt.num_kv_heads * a.rep;
-  const uint32_t number = blockIdx.x * kRows + (WAVES < 4 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0);
-  const uint32_t hq = number % heads, bi = number / heads;
-  if (bi >= uint32_t(most_new ? bt.num_seqs * most_new : bt.total)) return;   // (kRows > 1 only, where nobody waits for anybody)
-  const int b = most_new ? bi / uint32_t(most_new) : seq_of_row(bt, bi);
-  const uint32_t before = a.prefix[b], total = a.prefix[bt.num_seqs];
-  const Fp4Seq s = decode_seq(a, b);
-  const int i = most_new ? bi % uint32_t(most_new) : int(bi) - s.first;
-  if (i < 0 || i >= s.n) return;
-  const uint32_t h = hq / uint32_t(a.rep);
-  const int64_t row = int64_t(s.first + i) * heads + hq;
-  const uint32_t units = decode_units(s), per_unit = unit_cost(a, s);
-  Merged<HD> r = {};
-  if (units > 0) {
-    // the waves that the segment's first and last unit belong to
-    const uint32_t share = cost_share(total * uint32_t(bt.num_kv_heads), a.workers);
-    const uint32_t u0 = before * uint32_t(bt.num_kv_heads) + h * units * per_unit, u1 = u0 + (units - 1) * per_unit;
-    const uint32_t w0 = u0 / share, w1 = u1 / share;
-    if (w0 == w1) return;   // its wave has finished it
-    const int in_state = i * a.rep + int(hq - h * a.rep);
-    r = merge_parts<HD>(a.part_ml, a.part_o, (2 * int64_t(w0) + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state, 2 * (int64_t(w0) + 1) * a.rows + in_state,
-                        2 * int64_t(a.rows), int(w1 - w0) + 1, wave, WAVES, lane);
-  }
-  if constexpr (WAVES > 1) {
-    if (wave) {
-#pragma unroll
-      for (int x = 0; x < kPer; ++x) o[wave][lane * kPer + x] = r.o[x];
-    }
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int v = 1; v < WAVES; ++v)
-#pragma unroll
-      for (int x = 0; x < kPer; ++x) r.o[x] += o[v][lane * kPer + x];
-  }
-  write_merged<HD>(a, r, row, lane);
-}
-
-// Rows of the tile kernel whose keys were cut: a wave per (new token, query head).
-template <int HD>
-__global__ __launch_bounds__(256) void fp4_merge_tiles_kernel(Fp4Attention a) {
-  const Fp4Batch& bt = a.batch;
-  const int lane = threadIdx.x & 63;
-  const int heads = bt.num_kv_heads * a.rep;
-  const int row = __builtin_amdgcn_readfirstlane(int(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (row >= bt.total * heads) return;
-  const int t = row / heads, b = seq_of_row(bt, t);
-  const Fp4Span s = fp4_span(bt, b);
-  // not the rows of a sequence with a bad range, or of the decode kernel
-  if (t < s.first || t >= s.first + s.count || s.count * a.rep <= a.decode_rows) return;
-  const int64_t step = int64_t(bt.total) * heads;
-  write_merged<HD>(a, merge_parts<HD>(a.tile_ml, a.tile_o, row, row + step, step, a.splits, 0, 1, lane), row, lane);
-}
-
-}  // namespace cocktail
 
 using namespace cocktail;
 
@@ -230,7 +104,7 @@ extern "C" int cocktail_fp4_attention_workspace(const cocktail_fp4_cache* cache,
 extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t num_q_heads, const void* q, int32_t dtype, int64_t stride_t,
                                       int64_t stride_h, int64_t total, const int32_t* starts, int32_t max_new, int32_t max_len,
                                       float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-  Fp4Attention a = {};
+  PagedAttention a = {};
   if (int rc = check_attention(cache, num_q_heads, total, max_new)) return rc;
   if (int rc = check_fp4_rows(cache, q, out, dtype, stride_t, stride_h, total, starts, num_q_heads, &a.batch)) return rc;
   if (!total) return COCKTAIL_OK;
@@ -270,7 +144,7 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (s.decode) {
-    typedef void (*Kernel)(Fp4Attention);
+    typedef void (*Kernel)(PagedAttention);
     static const Kernel kernels[2][4] = {{fp4_decode_kernel<64, 1, false>, fp4_decode_kernel<64, 2, false>, fp4_decode_kernel<64, 3, false>, fp4_decode_kernel<64, 4, false>},
                                          {fp4_decode_kernel<128, 1, false>, fp4_decode_kernel<128, 2, false>, fp4_decode_kernel<128, 3, false>, fp4_decode_kernel<128, 4, false>}};
     const int64_t segments = s.active * cache->num_kv_heads;
@@ -295,14 +169,14 @@ extern "C" int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t n
     // 32: calls of 43.6 us by one wave a row, 36.9 by four; three times as many rows of 16: 60.5 and 62), a few by one
     const int parts = int(s.workers / (s.active * cache->num_kv_heads));
     if (parts >= 16 && most <= 512)
-      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 16> : fp4_merge_decode_kernel<64, 16>, dim3(most), dim3(1024), st, a, most_new);
+      e = launch(hd == 128 ? merge_decode_kernel<Fp4Cost, 128, 16> : merge_decode_kernel<Fp4Cost, 64, 16>, dim3(most), dim3(1024), st, a, most_new);
     else if (parts >= 12 && most <= 2048)
-      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 4> : fp4_merge_decode_kernel<64, 4>, dim3(most), dim3(256), st, a, most_new);
+      e = launch(hd == 128 ? merge_decode_kernel<Fp4Cost, 128, 4> : merge_decode_kernel<Fp4Cost, 64, 4>, dim3(most), dim3(256), st, a, most_new);
     else
-      e = launch(hd == 128 ? fp4_merge_decode_kernel<128, 1> : fp4_merge_decode_kernel<64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
+      e = launch(hd == 128 ? merge_decode_kernel<Fp4Cost, 128, 1> : merge_decode_kernel<Fp4Cost, 64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
   }
   if (e == hipSuccess && s.splits > 1)
-    e = launch(hd == 128 ? fp4_merge_tiles_kernel<128> : fp4_merge_tiles_kernel<64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);
+    e = launch(hd == 128 ? merge_tiles_kernel<Fp4Cost, 128> : merge_tiles_kernel<Fp4Cost, 64>, dim3(uint32_t((total * num_q_heads + 3) / 4)), dim3(256), st, a);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return COCKTAIL_OK;
 }

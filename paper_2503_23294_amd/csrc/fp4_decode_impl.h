@@ -15,9 +15,17 @@
 //  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4 (exact, the result does not depend on it), so that the
 //    common step has no exchange between lanes at all.
 #pragma once
-#include "fp4_attention.h"
+#include "fp4_common.h"
+#include "paged_attention.h"
 
 namespace cocktail {
+
+// What a unit costs: the conversions of K and V once, and products and weights per operand, each about as long (8 x 16K, 1 .. 6 tokens of 8 heads:
+// 55.6 us by operands alone, 47.4 by operands + 1, 49.4 by operands + 2).
+struct Fp4Cost {
+  static constexpr uint32_t kMost = 5;
+  __device__ static int unit(const PagedAttention& a, const PagedSeq& s) { return decode_operands(a, s) + 1; }
+};
 
 // 16 tokens of one (sequence, kv head) as a lane holds them.
 template <int HD>
@@ -29,144 +37,12 @@ struct Fp4Tile {
   int ok;           // wave-uniform: the page is one
 };
 
-// What lies where on the line of costs: with up to 64 sequences every wave has them in its lanes, otherwise the workgroup has what is before every
-// sequence in LDS (pre[0 .. num_seqs]), for one kv head.
-struct Fp4Line {
-  Fp4Seq seq;        // of sequence `lane`
-  int cost, before;
-  uint32_t total;    // of all sequences and kv heads
-};
-
-__device__ __forceinline__ Fp4Line make_line(const Fp4Attention& a, int32_t* pre, int32_t* scratch) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Fp4Line r = {};
-  int run = 0;
-  if (a.batch.num_seqs <= 64) {
-    if (lane < a.batch.num_seqs) {
-      r.seq = decode_seq(a, lane);
-      r.cost = decode_cost(a, r.seq);
-    }
-    const int upto = wave_prefix(r.cost);
-    r.before = upto - r.cost;
-    run = __builtin_amdgcn_readlane(upto, 63);
-    if (blockIdx.x == 0 && wave == 0) {
-      if (lane < a.batch.num_seqs) a.prefix[lane] = r.before;
-      if (lane == 0) a.prefix[a.batch.num_seqs] = run;
-    }
-  } else {
-    for (int base = 0; base < a.batch.num_seqs; base += 64 * kDecodeWaves) {
-      const int b = base + threadIdx.x;
-      const int v = b < a.batch.num_seqs ? decode_cost(a, decode_seq(a, b)) : 0;
-      const int x = wave_prefix(v);
-      __syncthreads();
-      if (lane == 63) scratch[wave] = x;
-      __syncthreads();
-      int before = run;
-      for (int w = 0; w < kDecodeWaves; ++w) {
-        if (w < wave) before += scratch[w];
-        run += scratch[w];
-      }
-      if (b < a.batch.num_seqs) pre[b] = before + x - v;
-    }
-    if (threadIdx.x == 0) pre[a.batch.num_seqs] = run;
-    __syncthreads();
-    if (blockIdx.x == 0)
-      for (int b = threadIdx.x; b <= a.batch.num_seqs; b += 64 * kDecodeWaves) a.prefix[b] = pre[b];
-  }
-  r.total = uint32_t(run) * uint32_t(a.batch.num_kv_heads);
-  return r;
-}
-
-__device__ __forceinline__ Fp4Seq of_lane(const Fp4Seq& s, int lane) {
-  return {__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.len, lane),
-          __builtin_amdgcn_readlane(s.past, lane)};
-}
-
-// The sequence at place u of the line: the last one that costs anything and has no more than u before it.
-struct Fp4Place {
-  int b, before, cost;   // cost of a kv head
-  Fp4Seq seq;
-};
-__device__ __forceinline__ Fp4Place find_place(const Fp4Attention& a, const Fp4Line& line, const int32_t* pre, uint32_t u) {
-  Fp4Place p;
-  const uint32_t heads = a.batch.num_kv_heads;
-  if (a.batch.num_seqs <= 64) {
-    const uint64_t candidates = __ballot(line.cost > 0 && uint32_t(line.before) * heads <= u);
-    p.b = 63 - __builtin_clzll(candidates);
-    p.before = __builtin_amdgcn_readlane(line.before, p.b);
-    p.cost = __builtin_amdgcn_readlane(line.cost, p.b);
-    p.seq = of_lane(line.seq, p.b);
-  } else {
-    int b = 0, e = a.batch.num_seqs;
-    while (e - b > 1) {
-      const int m = (b + e) >> 1;
-      if (uint32_t(pre[m]) * heads <= u) b = m;
-      else e = m;
-    }
-    // (of sequences with the same before them the search ends at the last, which is the one that costs something)
-    p.b = __builtin_amdgcn_readfirstlane(b);
-    p.before = __builtin_amdgcn_readfirstlane(pre[p.b]);
-    p.cost = __builtin_amdgcn_readfirstlane(pre[p.b + 1]) - p.before;
-    p.seq = of_lane(decode_seq(a, p.b), 0);
-  }
-  return p;
-}
-
 // WHOLE: a workgroup of kWholeWaves waves has one segment and shares it out among them, their states are joined in LDS: one launch, for short contexts.
 // Held to 128 registers, so that two of them run on a compute unit (1024 segments of 2048 tokens: 54.2 -> 47.4 us).  SPLIT: as many workgroups have a
 // segment, each for its part of the channels of V.
-constexpr int kWholeWaves = 8;
-
-// The number-th sequence that has queries for this kernel, or -1; for a workgroup of kWholeWaves waves, `lds`: kWholeWaves + 1 words.
-__device__ __forceinline__ int nth_active(const Fp4Attention& a, int number, int32_t* lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int run = 0;
-  if (threadIdx.x == 0) lds[kWholeWaves] = -1;
-  for (int base = 0; base < a.batch.num_seqs && run <= number; base += 64 * kWholeWaves) {
-    const int b = base + int(threadIdx.x);
-    const bool active = b < a.batch.num_seqs && decode_seq(a, b).n > 0;
-    const uint64_t mask = __ballot(active);
-    __syncthreads();
-    if (lane == 0) lds[wave] = __builtin_popcountll(mask);
-    __syncthreads();
-    int before = run;
-    for (int w = 0; w < kWholeWaves; ++w) {
-      if (w < wave) before += lds[w];
-      run += lds[w];
-    }
-    if (active && before + __builtin_popcountll(mask & ((uint64_t(1) << lane) - 1)) == number) lds[kWholeWaves] = b;
-  }
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(lds[kWholeWaves]);
-}
-
-// The number-th longest of up to 64 sequences, for a workgroup of kWholeWaves waves: a lane has a sequence, a wave counts which of its share of them are
-// longer.  Those without queries come last.
-__device__ __forceinline__ int nth_longest(const Fp4Attention& a, int number, Fp4Seq* seq) {
-  constexpr int kShare = 64 / kWholeWaves;
-  __shared__ int counted[kWholeWaves][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Fp4Seq s = {};
-  uint32_t key = 0;
-  if (lane < a.batch.num_seqs) {
-    s = decode_seq(a, lane);
-    const uint32_t units = s.n > 0 ? decode_units(s) + 1 : 0, most = (1u << 25) - 1;
-    key = (units < most ? units : most) << 6 | uint32_t(63 - lane);   // no two alike
-  }
-  int longer = 0, before = 0;
-#pragma unroll
-  for (int c = 0; c < kShare; ++c) longer += uint32_t(__builtin_amdgcn_readlane(int(key), wave * kShare + c)) > key ? 1 : 0;
-  counted[wave][lane] = longer;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWholeWaves; ++w) before += counted[w][lane];
-  const int b = __builtin_ctzll(__ballot(lane < a.batch.num_seqs && before == number));
-  *seq = of_lane(s, b);
-  return b;
-}
 
 template <int HD, int RT, bool WHOLE, int SPLIT = 1>
-__global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 4 : RT <= 2 ? 2 : 1) void fp4_decode_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 4 : RT <= 2 ? 2 : 1) void fp4_decode_kernel(PagedAttention a) {
   constexpr int kSteps = HD / 32;        // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16 / SPLIT;   // of a wave's output
   extern __shared__ int32_t pre[];
@@ -180,14 +56,14 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
   __shared__ u32x4 lds_q[kKeepQ ? 1 : kDecodeWaves][kKeepQ ? 1 : RT][kKeepQ ? 1 : kSteps][kKeepQ ? 1 : 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j = lane >> 4;
-  const Fp4Batch& bt = a.batch;
-  Fp4Line line = {};
+  const PagedBatch& bt = a.batch;
+  CostLine line = {};
   int w = 0;
   uint32_t u = 0, end = 1;
   bool stream = false;
   if constexpr (!WHOLE) {
-    line = make_line(a, pre, lds_words);
-    const uint32_t share = cost_share(line.total, a.workers);
+    line = make_line<Fp4Cost>(a, pre, lds_words);
+    const uint32_t share = cost_share<Fp4Cost>(line.total, a.workers);
     w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
     u = w * share;
     end = u + share < line.total ? u + share : line.total;
@@ -208,7 +84,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), WHOLE ? 
 
   bool first_segment = true;
   while (u < end) {
-    Fp4Place place;
+    CostPlace place;
     int h, u0, u1;
     if constexpr (WHOLE) {
       const int grid = gridDim.x / SPLIT;

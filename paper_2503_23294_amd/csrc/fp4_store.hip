@@ -24,7 +24,7 @@ __device__ __forceinline__ int quad_number(int first, int b) { return (first >> 
 
 // starts[0 .. num_seqs] in LDS; the thread's item from its number in the grid.
 template <int HD>
-__device__ __forceinline__ Fp4Item find_item(const Fp4Batch& a, const int32_t* lds_starts) {
+__device__ __forceinline__ Fp4Item find_item(const PagedBatch& a, const int32_t* lds_starts) {
   constexpr int kParts = HD / 8;
   Fp4Item it;
   const uint32_t per_quad = 2u * kParts * a.num_kv_heads;
@@ -46,8 +46,8 @@ __device__ __forceinline__ Fp4Item find_item(const Fp4Batch& a, const int32_t* l
     else e = m;
   }
   it.seq = b;
-  const Fp4Span s = fp4_span(a, b);
-  const int p0 = fp4_len(a, b) - s.count;                            // position of the range's first token (the last one's is below 2^31)
+  const PagedSpan s = paged_span(a, b);
+  const int p0 = paged_len(a, b) - s.count;                            // position of the range's first token (the last one's is below 2^31)
   const int q0 = p0 >> 2;                                            // its quad (rounded down: p0 may be negative)
   const int k = quad - quad_number(lds_starts[b], b);
   it.active = k >= 0 && s.count > 0 && q0 + k <= (p0 + s.count - 1) >> 2;
@@ -60,8 +60,8 @@ __device__ __forceinline__ Fp4Item find_item(const Fp4Batch& a, const int32_t* l
   return it;
 }
 
-__device__ __forceinline__ void load_starts(const Fp4Batch& a, int32_t* lds) {
-  // a range that is no range is cut to the batch, so that the numbers ascend as far as they can; fp4_span leaves it out
+__device__ __forceinline__ void load_starts(const PagedBatch& a, int32_t* lds) {
+  // a range that is no range is cut to the batch, so that the numbers ascend as far as they can; paged_span leaves it out
   for (int b = threadIdx.x; b <= a.num_seqs; b += 256) {
     const int v = a.starts ? a.starts[b] : b * a.uniform;
     lds[b] = v < 0 ? 0 : v > a.total ? a.total : v;
@@ -70,7 +70,7 @@ __device__ __forceinline__ void load_starts(const Fp4Batch& a, int32_t* lds) {
 }
 
 // The page's bytes for the item's head, or NULL.
-__device__ __forceinline__ char* page_run(const Fp4Batch& a, const Fp4Item& it, int64_t run) {
+__device__ __forceinline__ char* page_run(const PagedBatch& a, const Fp4Item& it, int64_t run) {
   if (it.pos < 0) return nullptr;
   const int col = it.pos / a.page_size;
   if (col >= a.table_stride) return nullptr;
@@ -162,7 +162,7 @@ struct Fp4Rows {
 };
 
 template <int HD, bool BF16>
-__global__ __launch_bounds__(256) void fp4_store_kernel(Fp4Batch a, Fp4Rows r) {
+__global__ __launch_bounds__(256) void fp4_store_kernel(PagedBatch a, Fp4Rows r) {
   extern __shared__ int32_t lds_starts[];
   load_starts(a, lds_starts);
   if (r.status[0] != 0) return;   // there was no room for these tokens
@@ -226,7 +226,7 @@ __device__ __forceinline__ u32x4 load_codes(const char* p) {
 }
 
 template <int HD, bool BF16, bool LINES>
-__global__ __launch_bounds__(256) void fp4_gather_kernel(Fp4Batch a, Fp4Rows r) {
+__global__ __launch_bounds__(256) void fp4_gather_kernel(PagedBatch a, Fp4Rows r) {
   extern __shared__ int32_t lds_starts[];
   load_starts(a, lds_starts);
   const Fp4Item it = find_item<HD>(a, lds_starts);
@@ -264,8 +264,8 @@ int check_fp4_cache(const cocktail_fp4_cache* c) {
   if (c->num_kv_heads < 1 || c->num_kv_heads > 1024) return fail(COCKTAIL_EINVAL, "num_kv_heads %d is not in 1 .. 1024", c->num_kv_heads);
   if (c->head_dim != 64 && c->head_dim != 128)
     return fail(COCKTAIL_EUNSUPPORTED, "kernels are built for head_dim 64 and 128, got %d", c->head_dim);
-  if (c->pages.page_size % 16 || c->pages.page_size > kFp4MostPage)
-    return fail(COCKTAIL_EINVAL, "page_size %d is not a multiple of 16 up to %d", c->pages.page_size, kFp4MostPage);
+  if (c->pages.page_size % 16 || c->pages.page_size > kMostPageSize)
+    return fail(COCKTAIL_EINVAL, "page_size %d is not a multiple of 16 up to %d", c->pages.page_size, kMostPageSize);
   // (positions and the numbers of keys a little behind the last one are ints)
   if (int64_t(c->pages.table_stride) * c->pages.page_size > (int64_t(1) << 31) - 256)
     return fail(COCKTAIL_EINVAL, "table_stride * page_size must be at most 2^31 - 256 for the cache");
@@ -275,7 +275,7 @@ int check_fp4_cache(const cocktail_fp4_cache* c) {
 }
 
 int check_fp4_rows(const cocktail_fp4_cache* c, const void* x, const void* y, int32_t dtype, int64_t stride_t, int64_t stride_h,
-                   int64_t total, const int32_t* starts, int heads, Fp4Batch* a) {
+                   int64_t total, const int32_t* starts, int heads, PagedBatch* a) {
   if (int rc = check_fp4_cache(c)) return rc;
   if (dtype != COCKTAIL_FP16 && dtype != COCKTAIL_BF16) return fail(COCKTAIL_EINVAL, "dtype %d is neither COCKTAIL_FP16 nor COCKTAIL_BF16", dtype);
   if (total < 0 || total > (int64_t(1) << 30)) return fail(COCKTAIL_EINVAL, "total %lld is not in 0 .. 2^30", (long long)total);
@@ -301,7 +301,7 @@ using namespace cocktail;
 namespace {
 
 template <class Kernel>
-int launch_rows(Kernel kernel, const Fp4Batch& a, const Fp4Rows& r, int head_dim, void* stream, const char* what) {
+int launch_rows(Kernel kernel, const PagedBatch& a, const Fp4Rows& r, int head_dim, void* stream, const char* what) {
   if (!a.total) return COCKTAIL_OK;
   const uint64_t quads = uint64_t(a.total) / 4 + 2 * uint64_t(a.num_seqs) + 1;
   const uint64_t blocks = (quads * (2 * a.num_kv_heads * (head_dim / 8)) + 255) / 256;
@@ -317,15 +317,15 @@ extern "C" int cocktail_fp4_page_bytes(int32_t num_kv_heads, int32_t head_dim, i
   if (!bytes) return fail(COCKTAIL_EINVAL, "bytes is NULL");
   if (num_kv_heads < 1 || num_kv_heads > 1024) return fail(COCKTAIL_EINVAL, "num_kv_heads %d is not in 1 .. 1024", num_kv_heads);
   if (head_dim != 64 && head_dim != 128) return fail(COCKTAIL_EUNSUPPORTED, "kernels are built for head_dim 64 and 128, got %d", head_dim);
-  if (page_size < 16 || page_size % 16 || page_size > kFp4MostPage)
-    return fail(COCKTAIL_EINVAL, "page_size %d is not a multiple of 16 up to %d", page_size, kFp4MostPage);
+  if (page_size < 16 || page_size % 16 || page_size > kMostPageSize)
+    return fail(COCKTAIL_EINVAL, "page_size %d is not a multiple of 16 up to %d", page_size, kMostPageSize);
   *bytes = num_kv_heads * fp4_run_bytes(head_dim, page_size);
   return COCKTAIL_OK;
 }
 
 extern "C" int cocktail_fp4_store(const cocktail_fp4_cache* cache, const void* k, const void* v, int32_t dtype, int64_t stride_t,
                                   int64_t stride_h, int64_t total, const int32_t* starts, void* stream) {
-  Fp4Batch a;
+  PagedBatch a;
   if (int rc = check_fp4_rows(cache, k, v, dtype, stride_t, stride_h, total, starts, cache ? cache->num_kv_heads : 0, &a)) return rc;
   const Fp4Rows r = {static_cast<char*>(const_cast<void*>(k)), static_cast<char*>(const_cast<void*>(v)), 2 * stride_t, 2 * stride_h, cache->pages.status};
   const bool d128 = cache->head_dim == 128;
@@ -336,10 +336,10 @@ extern "C" int cocktail_fp4_store(const cocktail_fp4_cache* cache, const void* k
 
 extern "C" int cocktail_fp4_gather(const cocktail_fp4_cache* cache, void* k, void* v, int32_t dtype, int64_t stride_t, int64_t stride_h,
                                    int64_t total, const int32_t* starts, void* stream) {
-  Fp4Batch a;
+  PagedBatch a;
   if (int rc = check_fp4_rows(cache, k, v, dtype, stride_t, stride_h, total, starts, cache ? cache->num_kv_heads : 0, &a)) return rc;
   const Fp4Rows r = {static_cast<char*>(k), static_cast<char*>(v), 2 * stride_t, 2 * stride_h, nullptr};
-  typedef void (*Kernel)(Fp4Batch, Fp4Rows);
+  typedef void (*Kernel)(PagedBatch, Fp4Rows);
   static const Kernel kernels[2][2][2] = {   // head_dim, dtype, whole lines
       {{fp4_gather_kernel<64, false, false>, fp4_gather_kernel<64, false, true>}, {fp4_gather_kernel<64, true, false>, fp4_gather_kernel<64, true, true>}},
       {{fp4_gather_kernel<128, false, false>, fp4_gather_kernel<128, false, true>}, {fp4_gather_kernel<128, true, false>, fp4_gather_kernel<128, true, true>}}};

@@ -8,7 +8,8 @@
 // S^T = K Q^T leaves a lane with one query row and half the keys of a step, in the order in which O^T = V^T P^T takes them (the
 // tokens of V lie in LDS in that order), so weights stay in their lanes.
 #pragma once
-#include "fp4_attention.h"
+#include "fp4_common.h"
+#include "paged_attention.h"
 
 namespace cocktail {
 
@@ -25,7 +26,7 @@ struct Fp4TileLds {
 };
 
 template <int WAVES>
-__device__ __forceinline__ int tile_count(const Fp4Attention& a, const Fp4Span& s) {
+__device__ __forceinline__ int tile_count(const PagedAttention& a, const PagedSpan& s) {
   return s.count * a.rep > a.decode_rows ? (s.count * a.rep + 32 * WAVES - 1) / (32 * WAVES) : 0;
 }
 
@@ -38,12 +39,12 @@ __device__ __forceinline__ const char* pick(int k, const char* a, const char* b,
 }
 
 template <int HD, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(PagedAttention a) {
   constexpr int kThreads = 64 * WAVES, kTileRows = 32 * WAVES;
   constexpr int kSteps = HD / 16, kChannelTiles = HD / 32;
   __shared__ Fp4TileLds<HD> lds;
   __shared__ int32_t found[4], scratch[WAVES];
-  const Fp4Batch& bt = a.batch;
+  const PagedBatch& bt = a.batch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // which rows: heads first, so that the heaviest tiles of all heads come first and the tiles of a head, which read the same keys, run on the same XCD
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   if (tid == 0) found[0] = -1;
   for (int base = 0; base < bt.num_seqs; base += kThreads) {
     const int b = base + tid;
-    const Fp4Span s = b < bt.num_seqs ? fp4_span(bt, b) : Fp4Span{0, 0};
+    const PagedSpan s = b < bt.num_seqs ? paged_span(bt, b) : PagedSpan{0, 0};
     const int v = tile_count<WAVES>(a, s);
     const int x = wave_prefix(v);
     __syncthreads();
@@ -76,10 +77,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fp4_tile_kernel(Fp4Attention a)
   const int b = __builtin_amdgcn_readfirstlane(found[0]);
   if (b < 0) return;
   const int tile = __builtin_amdgcn_readfirstlane(found[1]);
-  const Fp4Span span = fp4_span(bt, b);
+  const PagedSpan span = paged_span(bt, b);
   const int first = __builtin_amdgcn_readfirstlane(span.first), n = __builtin_amdgcn_readfirstlane(span.count);
-  const int rows = n * a.rep, all = __builtin_amdgcn_readfirstlane(fp4_len(bt, b)), len = fp4_held(bt, all);
-  const Fp4Seq seq = {first, n, len, all - n};
+  const int rows = n * a.rep, all = __builtin_amdgcn_readfirstlane(paged_len(bt, b)), len = paged_held(bt, all);
+  const PagedSeq seq = {first, n, len, all - n};
   const int r0 = tile * kTileRows;
   const int last_row = (r0 + kTileRows < rows ? r0 + kTileRows : rows) - 1;
   int most = seen_by(seq, last_row / a.rep);          // keys that the last row sees
