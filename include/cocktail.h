@@ -630,6 +630,130 @@ int cocktail_fp4_attention(const cocktail_fp4_cache* cache, int32_t num_q_heads,
                            int64_t stride_h, int64_t total, const int32_t* starts, int32_t max_new, int32_t max_len,
                            float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ======================================= A paged cache in 16 bits ======================================= */
+
+/*
+ * A paged cache that holds K and V as they are, in fp16 or bf16, on the same page tables: for a prefill whose context is quantized later
+ * (cocktail_reorder_quantize_paged reads these pages: stride_t = D, stride_h = page_size * D, stride_page = num_kv_heads * page_size * D), and
+ * for layers that stay in 16 bits.  A pool for K and one for V per layer; both are pools of cocktail_pages_resize and
+ * cocktail_pages_compact, pages of num_kv_heads * page_size * D * 2 bytes.
+ *
+ * Page: [num_kv_heads][page_size][D].
+ */
+typedef struct cocktail_kv16_cache {
+  cocktail_page_table pages; /* page_size a multiple of 16 up to 65536, table_stride * page_size <= 2^31 - 256 */
+  void* k;                   /* DEVICE num_pages pages, 16-byte aligned                               */
+  void* v;                   /* DEVICE num_pages pages, 16-byte aligned                               */
+  int32_t num_kv_heads;      /* 1 .. 1024                                                             */
+  int32_t head_dim;          /* 64 or 128                                                             */
+  int32_t dtype;             /* COCKTAIL_FP16 or COCKTAIL_BF16                                        */
+  int32_t reserved;          /* 0                                                                     */
+} cocktail_kv16_cache;
+
+/*
+ * Rotation of channels by the position: pair i of the first rotary_dim channels of a head, (x, y) = channels (i, i + rotary_dim / 2), or
+ * (2 i, 2 i + 1) if interleaved, becomes factor * (x cos a - y sin a, y cos a + x sin a) with a = position * inv_freq[i].  The angle is taken
+ * in binary64 and brought into one turn there, so that it is as good at position 2^31 as at 1; the rest is binary32, rounded
+ * once to the type of the rows.  The other channels stay as they are.
+ */
+typedef struct cocktail_rotation {
+  const double* inv_freq; /* DEVICE [rotary_dim / 2], 8-byte aligned                                  */
+  int32_t rotary_dim;     /* a multiple of 16 up to head_dim                                          */
+  int32_t interleaved;    /* 0 or 1                                                                   */
+  float factor;           /* finite; 1 for a plain rotation                                           */
+  int32_t reserved;       /* 0                                                                        */
+} cocktail_rotation;
+
+/*
+ * Appends new tokens: row t of k and v, starts[b] <= t < starts[b+1], becomes one of the last n = starts[b+1] - starts[b] tokens of
+ * sequence b (token seq_lens[b] - n + t - starts[b]), k rotated on the way; the queries of the same tokens are rotated into q_out.
+ * Call cocktail_pages_resize first, as for cocktail_fp4_store: where it found no room nothing is stored (the queries are rotated all
+ * the same), and rows for tokens before the first, or behind what the table row can hold, or on a page that is no page of the
+ * pool, are left out.  Nothing else in the pools is written.
+ *
+ *   k, v       DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d; strides in elements, multiples of 8; of the
+ *              cache's dtype, as q and q_out are
+ *   total, starts   as cocktail_fp4_store
+ *   rotation   HOST, or NULL: K is stored as it is, q must be NULL
+ *   positions  DEVICE int32 [total]: positions of the rows for the rotation, or NULL: the tokens' numbers in their sequences
+ *   q          DEVICE, 16-byte aligned, strides as k's, or NULL
+ *   q_out      DEVICE [total][num_q_heads][D], 16-byte aligned; may be q itself where that is laid out the same; otherwise they must
+ *              not overlap.  Rows of a sequence with a bad range are not written.
+ *   num_q_heads  1 .. 65536 with q, else 0
+ *
+ * One launch.  Errors: EINVAL, EUNSUPPORTED (head_dim, rotary_dim), EALIGN, EHIP.
+ */
+int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void* k, const void* v, int64_t stride_t, int64_t stride_h,
+                         int64_t total, const int32_t* starts, const cocktail_rotation* rotation, const int32_t* positions,
+                         const void* q, int32_t num_q_heads, int64_t q_stride_t, int64_t q_stride_h, void* q_out, void* stream);
+
+/*
+ * Attention of the newest tokens of every sequence over its cached keys, themselves included (causal): rows, arguments, workspace and
+ * what is left out as cocktail_fp4_attention; q and out are of the cache's dtype.
+ * Products and sums in binary32; softmax weights rounded to the cache's dtype (fp16: as there; bf16: by 2^-8 of themselves), and
+ * divided by the sum of the rounded ones.  A value of V that is not finite spoils its channel for all queries of its sequence and kv head in the
+ * call, also for those that do not see its token.  Calls on the same inputs agree bit for bit.  Up to four launches.
+ * Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
+ */
+int cocktail_kv16_attention_workspace(const cocktail_kv16_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,
+                                      int32_t max_len, int32_t uniform, size_t* bytes);
+int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t num_q_heads, const void* q, int64_t stride_t, int64_t stride_h,
+                            int64_t total, const int32_t* starts, int32_t max_new, int32_t max_len, float sm_scale, void* out,
+                            float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ============================================ Beam search ============================================ */
+
+/*
+ * Selection of a step of beam search: `groups` requests with `beams` hypotheses each, rows r = group * beams + beam of logits.
+ *     logp[r, v] = logits[r, v] - log sum_u exp(logits[r, u])
+ * Candidate (r, v) has the value scores[r] + logp[r, v]; a hypothesis that has ended (finished[r] != 0) has the one candidate (r, eos) of value
+ * scores[r].  The `keep` candidates of a group with the largest values are selected, in descending order, ties by the lowest
+ * (row, token); those of a row are in the order of their logits, also where binary64 cannot tell their values apart.  What has no probability is no candidate: logits that are -inf or NaN, rows whose score is -inf or NaN, rows without a
+ * finite logit.  An infinite logit counts as the largest finite number.  Where a group has fewer than `keep` candidates the other places are
+ * source -1, token -1, score -inf, finished 0.
+ * With keep == beams `source` is what cocktail_pages_fork and cocktail_beam_reorder take (places without a candidate free their pages).
+ *
+ *   logits    DEVICE, aligned to its elements; element (r, v) at r * stride_row + v (stride_row >= vocab, in elements)
+ *   dtype     COCKTAIL_FP16, COCKTAIL_BF16 or COCKTAIL_FP32
+ *   groups, beams, vocab, keep   groups * beams <= 2^20, beams 1 .. 64, vocab 1 .. 2^24, keep 1 .. 64
+ *   scores    DEVICE fp32 [groups * beams]
+ *   finished  DEVICE uint8 [groups * beams], or NULL: none
+ *   eos       token that ends a hypothesis, or -1: none (then finished must be NULL)
+ *   source    DEVICE int32 [groups * keep] out: rows of logits
+ *   token     DEVICE int32 [groups * keep] out
+ *   score     DEVICE fp32 [groups * keep] out: the candidates' values
+ *   finished_out  DEVICE uint8 [groups * keep] out, or NULL: finished[source] or token == eos
+ *   workspace DEVICE, cocktail_beam_select_workspace bytes, 16-byte aligned, not initialised; shared between calls as that of
+ *             cocktail_fp4_attention
+ *
+ * Exponentials and sums of up to eight of them in binary32, longer sums and the candidates' values in binary64.  The results may not overlap
+ * with each other or the inputs, but for score over scores and finished_out over finished where keep == beams.
+ * Calls on the same inputs agree bit for bit.  Two launches.  Errors: EINVAL, EALIGN, ENOSPACE, EHIP.
+ */
+#define COCKTAIL_FP32 2
+#define COCKTAIL_MAX_KEEP 64
+int cocktail_beam_select_workspace(int32_t groups, int32_t beams, int32_t vocab, int32_t keep, size_t* bytes);
+int cocktail_beam_select(const void* logits, int32_t dtype, int64_t stride_row, int32_t groups, int32_t beams, int32_t vocab,
+                         int32_t keep, const float* scores, const uint8_t* finished, int32_t eos, int32_t* source, int32_t* token,
+                         float* score, uint8_t* finished_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Reorders what hypotheses carry: row r of every state becomes what row source[r] was before the call; rows whose source is negative,
+ * or no row, stay as they are.  The counterpart of cocktail_pages_fork for tensors (token histories, recurrent states).
+ *
+ *   source     DEVICE int32 [rows]
+ *   rows       1 .. COCKTAIL_MAX_SEQS
+ *   from, to   HOST arrays of num_states DEVICE pointers to contiguous rows; to[i] == from[i] reorders in place, otherwise they must not
+ *              overlap; no memory may be written twice in a call
+ *   row_bytes  HOST int64 [num_states], bytes of a row of each state; any number up to 2^40 (whole pieces of 16 bytes are fastest, then of 4)
+ *   num_states 0 .. COCKTAIL_MAX_STATES
+ *
+ * Up to two launches (states in place, others).  Errors: EINVAL, EALIGN, EHIP.
+ */
+#define COCKTAIL_MAX_STATES 64
+int cocktail_beam_reorder(const int32_t* source, int32_t rows, const void* const* from, void* const* to, const int64_t* row_bytes,
+                          int32_t num_states, void* stream);
+
 /* Message of the last failure on the calling thread ("" if none).  Static storage. */
 const char* cocktail_last_error(void);
 

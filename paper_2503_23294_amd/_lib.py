@@ -21,8 +21,8 @@ STATIC_WORKSPACE_BYTES = 16 << 20
 
 OK, EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP, ESTATE = 0, -1, -2, -3, -4, -5, -6
 SRC_STRIDED, SRC_RAGGED = 0, 1
-FP16, BF16 = 0, 1
-MAX_SEQS, MAX_POOLS = 4096, 256
+FP16, BF16, FP32 = 0, 1, 2
+MAX_SEQS, MAX_POOLS, MAX_KEEP, MAX_STATES = 4096, 256, 64, 64
 
 
 class Shape(C.Structure):
@@ -62,6 +62,15 @@ class PageTableDesc(C.Structure):
 
 class Fp4CacheDesc(C.Structure):
     _fields_ = [("pages", PageTableDesc), ("pool", C.c_void_p), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Kv16CacheDesc(C.Structure):
+    _fields_ = [("pages", PageTableDesc), ("k", C.c_void_p), ("v", C.c_void_p), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class RotationDesc(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float), ("reserved", C.c_int32)]
 
 
 EXPORTS = {
@@ -108,6 +117,16 @@ EXPORTS = {
                                                    C.POINTER(C.c_size_t)]),
     "cocktail_fp4_attention": (C.c_int, [C.POINTER(Fp4CacheDesc), C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
                                          C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cocktail_kv16_append": (C.c_int, [C.POINTER(Kv16CacheDesc), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                       C.POINTER(RotationDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p]),
+    "cocktail_kv16_attention_workspace": (C.c_int, [C.POINTER(Kv16CacheDesc), C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                                    C.POINTER(C.c_size_t)]),
+    "cocktail_kv16_attention": (C.c_int, [C.POINTER(Kv16CacheDesc), C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                                          C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cocktail_beam_select_workspace": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]),
+    "cocktail_beam_select": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cocktail_beam_reorder": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "cocktail_last_error": (C.c_char_p, []),
     "cocktail_version": (C.c_int, []),
 }

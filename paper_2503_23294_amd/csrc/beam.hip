@@ -1,0 +1,519 @@
+// cocktail_beam_select / cocktail_beam_reorder: a step of beam search over the logits, and the reordering of what its hypotheses carry.
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+#include <cmath>
+
+#include "common.h"
+
+namespace cocktail {
+
+// The selection is two launches.  The first reads the logits once: a workgroup has a piece of a row, keeps its largest value and the sum of exponentials
+// against it, and the `keep` largest logits of the piece; a logit is compared with the smallest of those that are wanted so far, and only what
+// is larger goes into a buffer, which is sorted 64 at a time.  The second has a workgroup per request: it joins the pieces of
+// every row to log sum exp, turns the pieces' candidates into values and selects among them.  All keys differ (a value, then the lower
+// place first), so that the order in which candidates are met does not matter.
+constexpr int kSelectWaves = 4;
+constexpr int kMostKeep = COCKTAIL_MAX_KEEP;
+constexpr int kPerLane = 8;              // logits that a lane takes at a time
+static_assert(kMostKeep == 64, "a wave has a list of the best in its lanes");
+
+// A float as an integer of the same order; 0 is below all numbers.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ __forceinline__ uint64_t ordered(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return u >> 63 ? ~u : u | uint64_t(1) << 63;
+}
+__device__ __forceinline__ double from_ordered(uint64_t u) { return __builtin_bit_cast(double, u >> 63 ? u & ~(uint64_t(1) << 63) : ~u); }
+
+// Keys of the two launches: the larger one comes first; {} is none.
+struct LogitKey {
+  uint64_t x;   // ordered logit, then the complement of the token
+};
+struct ValueKey {
+  uint64_t value;   // ordered value
+  uint64_t place;   // complement of the row in the group, ordered logit (values of a row that binary64 cannot tell apart), complement of the token
+};
+__device__ __forceinline__ uint64_t value_place(int j, uint32_t logit, uint32_t token) {
+  return uint64_t(63 - j) << 56 | uint64_t(logit) << 24 | (0xffffffu - token);
+}
+__device__ __forceinline__ bool before(const LogitKey& a, const LogitKey& b) { return a.x > b.x; }
+__device__ __forceinline__ bool before(const ValueKey& a, const ValueKey& b) { return a.value > b.value || (a.value == b.value && a.place > b.place); }
+__device__ __forceinline__ LogitKey of_lane(const LogitKey& k, int lane) { return {uint64_t(__shfl(static_cast<unsigned long long>(k.x), lane))}; }
+__device__ __forceinline__ ValueKey of_lane(const ValueKey& k, int lane) {
+  return {uint64_t(__shfl(static_cast<unsigned long long>(k.value), lane)), uint64_t(__shfl(static_cast<unsigned long long>(k.place), lane))};
+}
+
+// One step of a bitonic network: the lane keeps the earlier or the later of its key and its partner's.
+template <class Key>
+__device__ __forceinline__ void exchange(Key& k, int partner, bool keep_first) {
+  const Key other = of_lane(k, partner);
+  if (before(other, k) == keep_first) k = other;
+}
+// The keys of a wave in order, the first one in lane 0.
+template <class Key>
+__device__ __forceinline__ Key sorted(Key k, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+    for (int step = size >> 1; step; step >>= 1) exchange(k, lane ^ step, ((lane & step) == 0) == ((lane & size) == 0 || size == 64));
+  return k;
+}
+// The first 64 of two sorted lists.
+template <class Key>
+__device__ __forceinline__ Key merged(Key a, const Key& b, int lane) {
+  const Key other = of_lane(b, 63 - lane);
+  if (before(other, a)) a = other;
+#pragma unroll
+  for (int step = 32; step; step >>= 1) exchange(a, lane ^ step, (lane & step) == 0);
+  return a;
+}
+
+// A wave's list of the best keys that it has met, and a buffer in LDS of those that may join it.
+constexpr int kBuffer = 64 * (kPerLane + 1);
+template <class Key>
+struct Best {
+  Key list, border;   // sorted over the lanes; the keep-th of them (only what comes before it can join)
+  int count;          // in the buffer
+  Key* buffer;
+  int keep, lane;
+  __device__ Best(Key* lds, int keep_, int lane_) : list{}, border{}, count(0), buffer(lds), keep(keep_), lane(lane_) {}
+  // Offers a key per lane where `there`.  Room for 64 more is the caller's to see to (join_full).
+  __device__ __forceinline__ void offer(const Key& k, bool there) {
+    const uint64_t mask = __ballot(there);
+    if (!mask) return;
+    if (there) buffer[count + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0))] = k;
+    count += __builtin_popcountll(mask);
+  }
+  __device__ __forceinline__ void join(int n) {   // the last n of the buffer
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    Key k = {};
+    if (lane < n) k = buffer[count - n + lane];
+    count -= n;
+    list = merged(list, sorted(k, lane), lane);
+    border = of_lane(list, keep - 1);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  __device__ __forceinline__ void join_full() {
+    while (count >= 64) join(64);
+  }
+  __device__ __forceinline__ void join_all() {
+    join_full();
+    if (count) join(count);
+  }
+};
+
+struct BeamSelect {
+  const void* logits;
+  int64_t stride_row;   // elements
+  int32_t groups, beams, vocab, keep, pieces;
+  const float* scores;
+  const uint8_t* finished;
+  int32_t eos;
+  int32_t *source, *token;
+  float* score;
+  uint8_t* finished_out;
+  double* sums;         // workspace: [rows][pieces] sum of exponentials
+  LogitKey* keys;       // [rows][pieces][keep]
+  float* tops;          // [rows][pieces] what the sum is against
+};
+
+// Whether a row has candidates that its logits say.
+__device__ __forceinline__ bool reads_logits(const BeamSelect& a, int row) { return a.scores[row] > -__builtin_inff() && !(a.finished && a.finished[row]); }
+
+template <class T>
+__device__ __forceinline__ float as_logit(T x) {
+  const float f = float(x);
+  // no number: none; an infinite one counts as the largest; -0 as 0
+  return f != f ? -__builtin_inff() : fminf(f, FLT_MAX) + 0.f;
+}
+
+// Eight logits from a multiple of eight (counted from the first aligned address at or before the row), those outside of the row as none.
+template <class T>
+__device__ __forceinline__ void load_logits(const T* row, int skip, int vocab, int64_t piece, float* x) {
+  const int64_t at = piece * kPerLane - skip;
+  if (at >= 0 && at + kPerLane <= vocab) {
+    constexpr int kWords = sizeof(T) * kPerLane / 16;
+    u32x4 w[kWords];
+    const u32x4* src = reinterpret_cast<const u32x4*>(row + at);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = __builtin_nontemporal_load(src + i);
+    T t[kPerLane];
+    __builtin_memcpy(t, w, sizeof t);
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) x[i] = as_logit(t[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) x[i] = at + i >= 0 && at + i < vocab ? as_logit(row[at + i]) : -__builtin_inff();
+  }
+}
+
+constexpr float kLog2eBeam = 1.4426950408889634f;
+
+template <class T>
+__global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSelect a) {
+  __shared__ LogitKey buffers[kSelectWaves][kBuffer];
+  __shared__ double lds_sum[kSelectWaves];
+  __shared__ float lds_top[kSelectWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
+  if (!reads_logits(a, row)) return;
+  const T* src = static_cast<const T*>(a.logits) + int64_t(row) * a.stride_row;
+  // sixteen-byte words lie at aligned addresses
+  const int skip = int(reinterpret_cast<uintptr_t>(src) % (sizeof(T) * kPerLane) / sizeof(T));
+  const int64_t words = (int64_t(skip) + a.vocab + kPerLane - 1) / kPerLane;
+  // of 64 words each; the piece's, then the wave's
+  const int64_t tiles = (words + 63) / 64;
+  const int64_t tile0 = tiles * piece / a.pieces, tile1 = tiles * (piece + 1) / a.pieces;
+
+  Best<LogitKey> best(buffers[wave], a.keep, lane);
+  float top = -FLT_MAX;
+  double sum = 0.0;
+  uint32_t border = 0;   // ordered value of the border
+  float next[kPerLane];
+  int64_t tile = tile0 + wave;
+  if (tile < tile1) load_logits(src, skip, a.vocab, tile * 64 + lane, next);
+  for (bool first = true; tile < tile1; tile += kSelectWaves, first = false) {
+    float x[kPerLane];
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) x[i] = next[i];
+    if (tile + kSelectWaves < tile1) load_logits(src, skip, a.vocab, (tile + kSelectWaves) * 64 + lane, next);
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < kPerLane; ++i) most = fmaxf(most, x[i]);
+    if (most > top) {
+      sum *= __builtin_amdgcn_exp2f((top - most) * kLog2eBeam);
+      top = most;
+    }
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) part += __builtin_amdgcn_exp2f((x[i] - top) * kLog2eBeam);
+    sum += part;
+    const uint32_t mine = most == -__builtin_inff() ? 0 : ordered(most);
+    if (first) {
+      // as many logits as are wanted are not below the keep-th of the lanes' largest
+      const LogitKey k = sorted(LogitKey{uint64_t(mine)}, lane);
+      border = uint32_t(of_lane(k, a.keep - 1).x);
+    }
+    if (__any(mine && mine >= border)) {
+      const int64_t at = (tile * 64 + lane) * kPerLane - skip;
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) {
+        const LogitKey k = {uint64_t(ordered(x[i])) << 32 | uint32_t(~uint32_t(at + i))};
+        best.offer(k, x[i] > -__builtin_inff() && uint32_t(k.x >> 32) >= border && before(k, best.border));
+      }
+      best.join_full();
+      const uint32_t now = uint32_t(best.border.x >> 32);
+      border = now > border ? now : border;
+    }
+  }
+  best.join_all();
+  // the waves' states together
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const float other = __shfl_xor(top, d), raised = fmaxf(top, other);
+    const double s = __shfl_xor(sum, d);
+    sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + s * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
+    top = raised;
+  }
+  if (lane == 0) lds_sum[wave] = sum, lds_top[wave] = top;
+  buffers[wave][lane] = best.list;
+  __syncthreads();
+  if (wave) return;
+  LogitKey list = best.list;
+  for (int w = 1; w < kSelectWaves; ++w) {
+    list = merged(list, buffers[w][lane], lane);
+    const float other = lds_top[w], raised = fmaxf(top, other);
+    sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + lds_sum[w] * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
+    top = raised;
+  }
+  const int64_t slot = int64_t(row) * a.pieces + piece;
+  if (lane < a.keep) a.keys[slot * a.keep + lane] = list;
+  if (lane == 0) a.sums[slot] = sum, a.tops[slot] = top;
+}
+
+__global__ __launch_bounds__(64 * kSelectWaves) void beam_join_kernel(BeamSelect a) {
+  __shared__ ValueKey buffers[kSelectWaves][kBuffer];
+  __shared__ double log_sum[64];
+  __shared__ float row_top[64];
+  __shared__ uint8_t over[64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = blockIdx.x, row0 = group * a.beams;
+  // a wave takes every fourth row: its pieces together
+  for (int j = wave; j < a.beams; j += kSelectWaves) {
+    const int row = row0 + j;
+    float top = -FLT_MAX;
+    double sum = 0.0;
+    if (reads_logits(a, row)) {
+      for (int p = lane; p < a.pieces; p += 64) {
+        const int64_t slot = int64_t(row) * a.pieces + p;
+        const float other = a.tops[slot], raised = fmaxf(top, other);
+        sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + a.sums[slot] * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
+        top = raised;
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const float other = __shfl_xor(top, d), raised = fmaxf(top, other);
+        const double s = __shfl_xor(sum, d);
+        sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + s * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
+        top = raised;
+      }
+    }
+    if (lane == 0) {
+      log_sum[j] = log(sum);
+      row_top[j] = top;
+      over[j] = a.finished && a.finished[row] ? 1 : 0;
+    }
+  }
+  __syncthreads();
+  Best<ValueKey> best(buffers[wave], a.keep, lane);
+  const int per_row = a.pieces * a.keep, all = a.beams * per_row;
+  for (int base = wave * 64; base < all; base += 64 * kSelectWaves) {
+    const int i = base + lane, j = i < all ? i / per_row : 0, row = row0 + j;
+    const double score = a.scores[row];
+    ValueKey k = {};
+    bool there = false;
+    if (i < all && score > -__builtin_inf()) {
+      if (over[j]) {
+        // one candidate
+        there = i == j * per_row;
+        k = {ordered(score), value_place(j, 0, uint32_t(a.eos))};
+      } else {
+        const LogitKey x = a.keys[int64_t(row) * per_row + (i - j * per_row)];
+        there = x.x != 0;
+        const uint32_t logit = uint32_t(x.x >> 32);
+        if (there) k = {ordered(score + ((double(from_ordered(logit)) - row_top[j]) - log_sum[j])), value_place(j, logit, ~uint32_t(x.x))};
+      }
+    }
+    best.offer(k, there && before(k, best.border));
+    best.join_full();
+  }
+  best.join_all();
+  buffers[wave][lane] = best.list;
+  __syncthreads();
+  if (wave) return;
+  ValueKey list = best.list;
+  for (int w = 1; w < kSelectWaves; ++w) list = merged(list, buffers[w][lane], lane);
+  if (lane >= a.keep) return;
+  const bool there = list.value != 0;
+  const int j = there ? 63 - int(list.place >> 56) : 0;
+  const int v = 0xffffff - int(list.place & 0xffffffu);
+  const int64_t at = int64_t(group) * a.keep + lane;
+  a.source[at] = there ? row0 + j : -1;
+  a.token[at] = there ? v : -1;
+  a.score[at] = there ? float(from_ordered(list.value)) : -__builtin_inff();
+  if (a.finished_out) a.finished_out[at] = there && (over[j] || v == a.eos) ? 1 : 0;
+}
+
+// ---- reordering ----------------------------------------------------------------------------------------------------------------
+
+struct BeamStates {
+  const char* from[COCKTAIL_MAX_STATES];
+  char* to[COCKTAIL_MAX_STATES];
+  int64_t row_bytes[COCKTAIL_MAX_STATES];
+  int32_t num_states, rows;
+};
+
+__device__ __forceinline__ int beam_source(const int32_t* source, int row, int rows) {
+  const int s = source[row];
+  return s >= 0 && s < rows ? s : row;
+}
+
+// Rows into other memory: a workgroup has 4096 bytes of a row of a state.
+constexpr int kCopyBytes = 4096;
+template <class Word>
+__device__ __forceinline__ void copy_words(char* to, const char* from, int bytes) {
+  for (int i = threadIdx.x * int(sizeof(Word)); i < bytes; i += 256 * int(sizeof(Word))) *reinterpret_cast<Word*>(to + i) = *reinterpret_cast<const Word*>(from + i);
+}
+__device__ __forceinline__ int alignment(uint64_t bits) { return bits & 3 ? 1 : bits & 15 ? 4 : 16; }
+
+__global__ __launch_bounds__(256) void beam_copy_kernel(const int32_t* source, BeamStates s) {
+  const int row = blockIdx.y, of = source[row];
+  if (of < 0 || of >= s.rows) return;
+  int64_t chunk = blockIdx.x;
+  for (int i = 0; i < s.num_states; ++i) {
+    if (s.from[i] == s.to[i]) continue;
+    const int64_t bytes = s.row_bytes[i], chunks = (bytes + kCopyBytes - 1) / kCopyBytes;
+    if (chunk >= chunks) {
+      chunk -= chunks;
+      continue;
+    }
+    const int64_t at = chunk * kCopyBytes;
+    const int n = int(bytes - at < kCopyBytes ? bytes - at : kCopyBytes);
+    char* to = s.to[i] + row * bytes + at;
+    const char* from = s.from[i] + of * bytes + at;
+    const int align = alignment(reinterpret_cast<uintptr_t>(s.to[i]) | reinterpret_cast<uintptr_t>(s.from[i]) | uint64_t(bytes));
+    if (align == 16) copy_words<u32x4>(to, from, n);
+    else if (align == 4) copy_words<uint32_t>(to, from, n);
+    else copy_words<uint8_t>(to, from, n);
+    return;
+  }
+}
+
+// Rows in place: a workgroup has a column of a state, all rows of it, which are read before any is written.
+constexpr int kPlaceBytes = 65536;   // of a column, in LDS
+template <class Word>
+__device__ __forceinline__ void permute_words(const int32_t* source, char* state, int rows, int64_t row_bytes, int64_t at, int width, char* lds) {
+  const int words = width / int(sizeof(Word)), all = rows * words;
+  Word* held = reinterpret_cast<Word*>(lds);
+  for (int i = threadIdx.x; i < all; i += 256) {
+    const int row = i / words, w = i - row * words, of = beam_source(source, row, rows);
+    if (of != row) held[i] = *reinterpret_cast<const Word*>(state + of * row_bytes + at + w * int(sizeof(Word)));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < all; i += 256) {
+    const int row = i / words, w = i - row * words;
+    if (beam_source(source, row, rows) != row) *reinterpret_cast<Word*>(state + row * row_bytes + at + w * int(sizeof(Word))) = held[i];
+  }
+}
+
+__host__ __device__ inline int column_bytes(int rows) {
+  const int n = kPlaceBytes / rows / 16 * 16;   // 16 at least: 4096 rows
+  return n < kCopyBytes ? n : kCopyBytes;
+}
+
+__global__ __launch_bounds__(256) void beam_place_kernel(const int32_t* source, BeamStates s) {
+  extern __shared__ u32x4 lds[];
+  const int width = column_bytes(s.rows);
+  int64_t chunk = blockIdx.x;
+  for (int i = 0; i < s.num_states; ++i) {
+    if (s.from[i] != s.to[i]) continue;
+    const int64_t bytes = s.row_bytes[i], chunks = (bytes + width - 1) / width;
+    if (chunk >= chunks) {
+      chunk -= chunks;
+      continue;
+    }
+    const int64_t at = chunk * width;
+    const int n = int(bytes - at < width ? bytes - at : width);
+    const int align = alignment(reinterpret_cast<uintptr_t>(s.to[i]) | uint64_t(bytes));
+    char* held = reinterpret_cast<char*>(lds);
+    if (align == 16) permute_words<u32x4>(source, s.to[i], s.rows, bytes, at, n, held);
+    else if (align == 4) permute_words<uint32_t>(source, s.to[i], s.rows, bytes, at, n, held);
+    else permute_words<uint8_t>(source, s.to[i], s.rows, bytes, at, n, held);
+    return;
+  }
+}
+
+}  // namespace cocktail
+
+using namespace cocktail;
+
+namespace {
+
+struct SelectPlan {
+  int pieces;
+  size_t sums, keys, tops, bytes;
+};
+
+int plan_select(int32_t groups, int32_t beams, int32_t vocab, int32_t keep, SelectPlan* s) {
+  if (groups < 1 || beams < 1 || beams > 64 || int64_t(groups) * beams > (1 << 20))
+    return fail(COCKTAIL_EINVAL, "%d groups of %d beams: beams must be in 1 .. 64, groups * beams in 1 .. 2^20", groups, beams);
+  if (vocab < 1 || vocab > (1 << 24)) return fail(COCKTAIL_EINVAL, "vocab %d is not in 1 .. 2^24", vocab);
+  if (keep < 1 || keep > kMostKeep) return fail(COCKTAIL_EINVAL, "keep %d is not in 1 .. %d", keep, kMostKeep);
+  const int64_t rows = int64_t(groups) * beams;
+  int64_t pieces = (1024 + rows - 1) / rows;
+  const int64_t most = (int64_t(vocab) + 4095) / 4096;
+  pieces = pieces < most ? pieces : most;
+  s->pieces = int(pieces);
+  s->sums = size_t(rows * pieces) * sizeof(double);
+  s->keys = size_t(rows * pieces) * size_t(keep) * sizeof(LogitKey);
+  s->tops = size_t(rows * pieces) * sizeof(float);
+  s->bytes = s->sums + s->keys + s->tops + 16;
+  return COCKTAIL_OK;
+}
+
+}  // namespace
+
+extern "C" int cocktail_beam_select_workspace(int32_t groups, int32_t beams, int32_t vocab, int32_t keep, size_t* bytes) {
+  if (!bytes) return fail(COCKTAIL_EINVAL, "bytes is NULL");
+  SelectPlan s;
+  if (int rc = plan_select(groups, beams, vocab, keep, &s)) return rc;
+  *bytes = s.bytes;
+  return COCKTAIL_OK;
+}
+
+extern "C" int cocktail_beam_select(const void* logits, int32_t dtype, int64_t stride_row, int32_t groups, int32_t beams, int32_t vocab,
+                                    int32_t keep, const float* scores, const uint8_t* finished, int32_t eos, int32_t* source, int32_t* token,
+                                    float* score, uint8_t* finished_out, void* workspace, size_t workspace_bytes, void* stream) {
+  SelectPlan s;
+  if (int rc = plan_select(groups, beams, vocab, keep, &s)) return rc;
+  if (dtype != COCKTAIL_FP16 && dtype != COCKTAIL_BF16 && dtype != COCKTAIL_FP32)
+    return fail(COCKTAIL_EINVAL, "dtype %d is none of COCKTAIL_FP16, COCKTAIL_BF16, COCKTAIL_FP32", dtype);
+  if (!logits || !scores || !source || !token || !score) return fail(COCKTAIL_EINVAL, "logits, scores, source, token and score must not be NULL");
+  if (stride_row < vocab || stride_row > (int64_t(1) << 40)) return fail(COCKTAIL_EINVAL, "stride_row %lld is not in vocab .. 2^40", (long long)stride_row);
+  if (eos < -1 || eos >= vocab) return fail(COCKTAIL_EINVAL, "eos %d is not in -1 .. vocab - 1", eos);
+  if (finished && eos < 0) return fail(COCKTAIL_EINVAL, "finished hypotheses need an eos");
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == COCKTAIL_FP32 ? 4 : 2)) return fail(COCKTAIL_EALIGN, "logits must be aligned to their elements");
+  if ((reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(source) | reinterpret_cast<uintptr_t>(token) | reinterpret_cast<uintptr_t>(score)) & 3)
+    return fail(COCKTAIL_EALIGN, "scores, source, token and score must be 4-byte aligned");
+  if ((score == scores || (finished_out && finished_out == finished)) && keep != beams)
+    return fail(COCKTAIL_EINVAL, "results can replace the scores only where keep == beams");
+  if (!workspace) return fail(COCKTAIL_EINVAL, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(COCKTAIL_EALIGN, "workspace must be 16-byte aligned");
+  if (workspace_bytes < s.bytes) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, s.bytes);
+  BeamSelect a = {};
+  a.logits = logits;
+  a.stride_row = stride_row;
+  a.groups = groups;
+  a.beams = beams;
+  a.vocab = vocab;
+  a.keep = keep;
+  a.pieces = s.pieces;
+  a.scores = scores;
+  a.finished = finished;
+  a.eos = eos;
+  a.source = source;
+  a.token = token;
+  a.score = score;
+  a.finished_out = finished_out;
+  char* w = static_cast<char*>(workspace);
+  a.sums = reinterpret_cast<double*>(w);
+  a.keys = reinterpret_cast<LogitKey*>(w + s.sums);
+  a.tops = reinterpret_cast<float*>(w + s.sums + s.keys);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const uint32_t blocks = uint32_t(groups) * uint32_t(beams) * uint32_t(s.pieces);
+  hipError_t e = launch(dtype == COCKTAIL_FP32 ? beam_pieces_kernel<float> : dtype == COCKTAIL_BF16 ? beam_pieces_kernel<__bf16> : beam_pieces_kernel<_Float16>,
+                        dim3(blocks), dim3(64 * kSelectWaves), st, a);
+  if (e == hipSuccess) e = launch(beam_join_kernel, dim3(uint32_t(groups)), dim3(64 * kSelectWaves), st, a);
+  if (e != hipSuccess) return fail(COCKTAIL_EHIP, "beam selection launch failed: %s", hipGetErrorString(e));
+  return COCKTAIL_OK;
+}
+
+extern "C" int cocktail_beam_reorder(const int32_t* source, int32_t rows, const void* const* from, void* const* to, const int64_t* row_bytes,
+                                     int32_t num_states, void* stream) {
+  if (!source) return fail(COCKTAIL_EINVAL, "source is NULL");
+  if (reinterpret_cast<uintptr_t>(source) & 3) return fail(COCKTAIL_EALIGN, "source must be 4-byte aligned");
+  if (rows < 1 || rows > COCKTAIL_MAX_SEQS) return fail(COCKTAIL_EINVAL, "rows %d is not in 1 .. %d", rows, COCKTAIL_MAX_SEQS);
+  if (num_states < 0 || num_states > COCKTAIL_MAX_STATES) return fail(COCKTAIL_EINVAL, "num_states %d is not in 0 .. %d", num_states, COCKTAIL_MAX_STATES);
+  if (num_states && (!from || !to || !row_bytes)) return fail(COCKTAIL_EINVAL, "from, to and row_bytes must not be NULL");
+  BeamStates s = {};
+  s.num_states = num_states;
+  s.rows = rows;
+  int64_t copies = 0, columns = 0;
+  const int width = column_bytes(rows);
+  for (int i = 0; i < num_states; ++i) {
+    if (row_bytes[i] < 0 || row_bytes[i] > (int64_t(1) << 40)) return fail(COCKTAIL_EINVAL, "row_bytes of state %d is not in 0 .. 2^40", i);
+    if (row_bytes[i] && (!from[i] || !to[i])) return fail(COCKTAIL_EINVAL, "state %d is NULL", i);
+    s.from[i] = static_cast<const char*>(from[i]);
+    s.to[i] = static_cast<char*>(to[i]);
+    s.row_bytes[i] = row_bytes[i];
+    if (from[i] == to[i]) columns += (row_bytes[i] + width - 1) / width;
+    else copies += (row_bytes[i] + kCopyBytes - 1) / kCopyBytes;
+  }
+  if (copies * rows >= (int64_t(1) << 24) || copies >= (int64_t(1) << 24) || columns >= (int64_t(1) << 24))
+    return fail(COCKTAIL_EINVAL, "the states are more than one launch takes");
+  hipError_t e = hipSuccess;
+  if (copies) e = launch(beam_copy_kernel, dim3(uint32_t(copies), uint32_t(rows)), dim3(256), static_cast<hipStream_t>(stream), source, s);
+  if (e == hipSuccess && columns)
+    e = launch_lds(beam_place_kernel, dim3(uint32_t(columns)), dim3(256), size_t(width) * rows, static_cast<hipStream_t>(stream), source, s);
+  if (e != hipSuccess) return fail(COCKTAIL_EHIP, "beam reordering launch failed: %s", hipGetErrorString(e));
+  return COCKTAIL_OK;
+}

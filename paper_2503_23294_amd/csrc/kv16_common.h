@@ -1,0 +1,13 @@
+// The paged 16-bit cache (cocktail_kv16_*): pages of [num_kv_heads][page_size][head_dim] in fp16 or bf16, a pool for K and one for V.
+#pragma once
+#include "paged_batch.h"
+
+namespace cocktail {
+
+int check_kv16_cache(const cocktail_kv16_cache* c);
+// Rows [total][heads] of the cache's dtype.
+int check_kv16_rows(const cocktail_kv16_cache* c, const void* x, const void* y, int64_t stride_t, int64_t stride_h, int64_t total, int heads);
+// The batch of a call, with K's pool; checks `total` against `starts`.
+int check_kv16_batch(const cocktail_kv16_cache* c, int64_t total, const int32_t* starts, PagedBatch* a);
+
+}  // namespace cocktail

@@ -459,7 +459,7 @@ static inline int64_t align16(int64_t x) { return (x + 15) & ~int64_t(15); }
 using namespace cocktail;
 
 extern "C" const char* cocktail_last_error(void) { return g_err; }
-extern "C" int cocktail_version(void) { return (0 << 16) | 5; }
+extern "C" int cocktail_version(void) { return (0 << 16) | 6; }
 
 // Reads one field of the plan header by name, so that tools and tests that look inside a plan follow the
 // header's real layout instead of a copy of it.

@@ -1,0 +1,232 @@
+"""Beam search: selection over hypotheses and vocabulary, and the reordering of states, against the oracle in binary64."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_23294_amd as ck
+from oracle import kv16_oracle as O
+from paper_2503_23294_amd import _lib
+
+gpu = pytest.mark.gpu
+DTYPES = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def test_selection_of_the_oracle():
+    # two hypotheses, three tokens: probabilities 1/2, 1/4, 1/4 and 1/8, 7/8, 0
+    logits = np.log(np.array([[0.5, 0.25, 0.25], [0.125, 0.875, 1e-300]]))
+    logits[1, 2] = -np.inf
+    source, token, score, over = O.select(logits + 3.0, [0.0, np.log(0.5)], 2, 6, eos=1)
+    assert source.tolist() == [[0, 1, 0, 0, 1, -1]] and token.tolist() == [[0, 1, 1, 2, 0, -1]] and over.tolist() == [[False, True, True, False, False, False]]
+    assert np.allclose(np.exp(score[0]), [0.5, 0.4375, 0.25, 0.25, 0.0625, 0.0])
+    source, token, score, over = O.select(logits, [0.0, -0.1], 2, 3, eos=2, finished=[False, True])
+    assert source.tolist() == [[1, 0, 0]] and token.tolist() == [[2, 0, 1]] and over.tolist() == [[True, False, False]] and score[0, 0] == -0.1
+    assert O.select(np.full((1, 4), -np.inf), [0.0], 1, 2)[0].tolist() == [[-1, -1]]
+    assert np.allclose(O.log_probabilities(np.array([np.inf, 1.0, np.inf, np.nan])), [-np.log(2), -3.4028234663852886e38, -np.log(2), -np.inf])
+    assert np.array_equal(O.reorder(np.arange(4) * 10, [3, 3, -1, 9]), [30, 30, 20, 30])
+
+
+def test_refusals_of_selection():
+    L = _lib.lib()
+    n = C.c_size_t(0)
+    need = lambda g=2, b=4, v=100, k=4: L.cocktail_beam_select_workspace(g, b, v, k, C.byref(n))  # noqa: E731
+    bad_sizes = (dict(g=0), dict(b=0), dict(b=65), dict(g=1 << 18, b=5), dict(v=0), dict(v=(1 << 24) + 1), dict(k=0), dict(k=65))
+    for bad in bad_sizes:
+        assert need(**bad) == _lib.EINVAL, bad
+    assert L.cocktail_beam_select_workspace(2, 4, 100, 4, None) == _lib.EINVAL
+    assert need() == 0 and n.value > 0
+
+    def call(logits=4096, dtype=2, stride=100, g=2, b=4, v=100, k=4, scores=4096, finished=None, eos=-1, source=4096, token=8192, score=12288, out=None, ws=4096, wb=1 << 40):
+        return L.cocktail_beam_select(logits, dtype, stride, g, b, v, k, scores, finished, eos, source, token, score, out, ws, wb, None)
+    for bad in bad_sizes:
+        assert call(**bad, stride=1 << 24) == _lib.EINVAL, bad
+    for bad, code in ((dict(wb=n.value - 1), _lib.ENOSPACE), (dict(ws=None), _lib.EINVAL), (dict(ws=8), _lib.EALIGN), (dict(dtype=3), _lib.EINVAL), (dict(dtype=-1), _lib.EINVAL),
+                      (dict(logits=None), _lib.EINVAL), (dict(scores=None), _lib.EINVAL), (dict(source=None), _lib.EINVAL), (dict(token=None), _lib.EINVAL),
+                      (dict(score=None), _lib.EINVAL), (dict(logits=4098), _lib.EALIGN), (dict(logits=4097, dtype=0), _lib.EALIGN), (dict(scores=4098), _lib.EALIGN),
+                      (dict(token=8193), _lib.EALIGN), (dict(stride=99), _lib.EINVAL), (dict(eos=100), _lib.EINVAL), (dict(eos=-2), _lib.EINVAL),
+                      (dict(finished=4096), _lib.EINVAL), (dict(k=3, score=4096), _lib.EINVAL), (dict(k=8, finished=4096, out=4096, eos=1), _lib.EINVAL)):
+        assert call(**bad) == code, bad
+        assert L.cocktail_last_error()
+
+
+def test_refusals_of_reordering():
+    L = _lib.lib()
+
+    def call(source=4096, rows=4, of=(4096,), to=(8192,), size=(64,), n=None):
+        k = len(of)
+        return L.cocktail_beam_reorder(source, rows, (C.c_void_p * k)(*of), (C.c_void_p * k)(*to), (C.c_int64 * k)(*size), k if n is None else n, None)
+    for bad, code in ((dict(source=None), _lib.EINVAL), (dict(source=2), _lib.EALIGN), (dict(rows=0), _lib.EINVAL), (dict(rows=4097), _lib.EINVAL),
+                      (dict(n=-1), _lib.EINVAL), (dict(n=65), _lib.EINVAL), (dict(of=(None,)), _lib.EINVAL), (dict(to=(None,)), _lib.EINVAL),
+                      (dict(size=(-1,)), _lib.EINVAL), (dict(size=((1 << 40) + 1,)), _lib.EINVAL), (dict(size=(1 << 36,)), _lib.EINVAL),
+                      (dict(to=(4096,), size=(1 << 40,)), _lib.EINVAL)):
+        assert call(**bad) == code, bad
+        assert L.cocktail_last_error()
+    assert L.cocktail_beam_reorder(4096, 4, None, None, None, 1, None) == _lib.EINVAL
+    assert L.cocktail_beam_reorder(4096, 4, None, None, None, 0, None) == 0 and call(size=(0,)) == 0       # nothing to do
+
+
+def test_the_binding_wants_device_tensors():
+    with pytest.raises(TypeError):
+        ck.cocktail_beam_select(torch.zeros(4, 10), torch.zeros(4), 2)
+    with pytest.raises(TypeError):
+        ck.cocktail_beam_reorder(torch.zeros(4, dtype=torch.int32), [torch.zeros(4, 2)])
+
+
+# ---- on the GPU ------------------------------------------------------------------------------------------------------------
+
+
+def _check(logits, scores, beams, keep, eos, finished, got):
+    """Selected places are the oracle's, but where two candidates' values are nearer than what they may be off by: those of one row differ by their
+    logits exactly; the sum of exponentials in binary32 has terms within 2^-20 (the argument's rounding, at most 40 * 2^-24 of them where they count, and the
+    function's), so values of different rows are within 2^-20 + one rounding to binary32."""
+    source, token, score, over = [x.cpu().numpy() for x in got]
+    ws, wt, wv, wo = O.select(logits.double().cpu().numpy(), scores.tolist(), beams, keep, eos, None if finished is None else finished.tolist())
+    assert np.array_equal(np.isneginf(score), ws < 0) and np.array_equal(source < 0, ws < 0)
+    live = ws >= 0
+    tol = 2.0 ** -20 + 2.0 ** -24 * np.abs(np.where(live, wv, 0))
+    assert (np.abs(np.where(live, score, 0) - np.where(live, wv, 0)) <= tol).all()
+    for g in range(len(ws)):
+        for i in range(keep):
+            if source[g, i] == ws[g, i] and token[g, i] == wt[g, i]:
+                continue
+            # the same place elsewhere, or beyond the end, at a value as good
+            near = [k for k in range(keep) if abs(wv[g, k] - wv[g, i]) <= 2 * tol[g, i] and ws[g, k] != ws[g, i]]
+            assert near or i == keep - 1, (g, i, source[g], ws[g], token[g], wt[g])
+    assert (over == wo).all() or not np.array_equal(source, ws)
+    return np.array_equal(source, ws) and np.array_equal(token, wt)
+
+
+def _logits(rng, rows, vocab, dtype, spread=3.0):
+    return torch.from_numpy(rng.standard_normal((rows, vocab)) * spread).to("cuda:0", dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("groups,beams,vocab,keep", [(1, 1, 1, 1), (1, 4, 1, 4), (2, 3, 7, 5), (1, 4, 32000, 4), (3, 8, 5003, 8), (2, 64, 999, 64), (5, 5, 4096, 10),
+                                                     (1, 64, 20011, 64), (40, 2, 513, 2), (300, 4, 2049, 4), (2, 1, 300001, 64), (1, 16, 8191, 32)])
+def test_selection(groups, beams, vocab, keep, dtype):
+    rng = np.random.default_rng(vocab + keep)
+    rows = groups * beams
+    logits = _logits(rng, rows, vocab, DTYPES[dtype])
+    scores = torch.from_numpy(rng.standard_normal(rows).astype(np.float32) - 20).cuda()
+    eos = vocab // 2
+    finished = torch.from_numpy(rng.random(rows) < 0.3).cuda()
+    for f in (None, finished):
+        got = ck.cocktail_beam_select(logits, scores, beams, keep=keep, eos=eos, finished=f)
+        assert [x.shape for x in got] == [(groups, keep)] * 4
+        _check(logits, scores, beams, keep, eos, f, got)
+        again = ck.cocktail_beam_select(logits, scores, beams, keep=keep, eos=eos, finished=f)
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_ties_go_to_the_lowest_place(dtype):
+    dt = DTYPES[dtype]
+    # all alike, over many pieces
+    got = ck.cocktail_beam_select(torch.full((4, 50001), -1.5, dtype=dt, device="cuda:0"), torch.zeros(4, device="cuda:0"), 2, keep=5)
+    assert got[0].tolist() == [[0] * 5, [2] * 5] and got[1].tolist() == [[0, 1, 2, 3, 4]] * 2
+    # a few values, zeros of both signs among them, in falling, rising and any order
+    rng = np.random.default_rng(3)
+    x = rng.integers(-3, 1, (3, 9001)) * 0.5
+    x[0].sort()
+    x[1] = -np.sort(-x[1])
+    x = np.where((x == 0) & (rng.random(x.shape) < 0.5), -0.0, x)
+    logits = torch.from_numpy(x).to("cuda:0", dt)
+    got = ck.cocktail_beam_select(logits, torch.zeros(3, device="cuda:0"), 1, keep=64)
+    want = O.select(x, [0.0] * 3, 1, 64)
+    assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+    # rising rows without ties: every logit joins the list of its wave
+    rise = torch.arange(60000, device="cuda:0", dtype=torch.float32)[None] * 2.0 ** -10
+    got = ck.cocktail_beam_select(rise.repeat(2, 1), torch.tensor([0.0, -50.0], device="cuda:0"), 2, keep=64)
+    assert got[0].tolist() == [[0] * 64] and got[1].tolist() == [list(range(59999, 59935, -1))]
+    # equal rows at equal scores: a value's tokens of the first row, then of the second
+    two = _logits(rng, 1, 1000, dt).repeat(2, 1)
+    got = ck.cocktail_beam_select(two, torch.tensor([-1.0, -1.0], device="cuda:0"), 2, keep=6)
+    want = O.select(two.double().cpu().numpy(), [-1.0, -1.0], 2, 6)
+    assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_what_has_no_probability_is_no_candidate(dtype):
+    dt, inf = DTYPES[dtype], float("inf")
+    rng = np.random.default_rng(9)
+    logits = _logits(rng, 10, 3000, dt)
+    scores = torch.from_numpy(rng.standard_normal(10).astype(np.float32)).cuda()
+    logits[0] = -inf                                   # a row whose mask leaves nothing
+    logits[1] = float("nan")
+    logits[2, 5:] = -inf                               # five tokens are left
+    logits[3, ::2] = float("nan")
+    logits[4, 7], logits[4, 2000] = inf, inf           # two that share all of it
+    logits[5] = torch.finfo(dt).min                    # the lowest value everywhere: a level row
+    logits[6, 10:] = torch.finfo(dt).min
+    scores[7], scores[8] = -inf, float("nan")
+    for beams, keep in ((1, 64), (2, 64), (5, 16), (10, 40)):
+        got = ck.cocktail_beam_select(logits, scores, beams, keep=keep, eos=3)
+        _check(logits, scores, beams, keep, 3, None, got)
+    got = ck.cocktail_beam_select(logits, scores, 1, keep=8)
+    assert (got[0][[0, 1, 7, 8]] == -1).all() and (got[1][[0, 1, 7, 8]] == -1).all() and (got[2][[0, 1, 7, 8]] == -inf).all()
+    assert got[1][2, 5:].tolist() == [-1] * 3 and got[1][4, :2].tolist() == [7, 2000] and got[1][5].tolist() == list(range(8))
+    # all hypotheses of a request are dead; the first step, where one is alive
+    scores = torch.tensor([0.0, -inf, -inf, -inf] + [-inf] * 4, device="cuda:0")
+    got = ck.cocktail_beam_select(_logits(rng, 8, 500, dt), scores, 4)
+    assert got[0].tolist() == [[0] * 4, [-1] * 4]
+    # all have ended
+    got = ck.cocktail_beam_select(_logits(rng, 4, 500, dt), torch.tensor([-3.0, -1.0, -2.0, -1.0], device="cuda:0"), 4, eos=7,
+                                  finished=torch.ones(4, dtype=torch.uint8, device="cuda:0"))
+    assert got[0].tolist() == [[1, 3, 2, 0]] and got[1].tolist() == [[7] * 4] and got[2].tolist() == [[-1.0, -1.0, -2.0, -3.0]] and got[3].all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_strided_rows_at_any_address(dtype):
+    """Rows that begin at every address that their elements may have, next to values that must not be taken for theirs."""
+    rng = np.random.default_rng(11)
+    for offset in range(9):
+        wide = torch.full((6, 2600), 1e4, dtype=DTYPES[dtype], device="cuda:0")
+        view = wide[:, offset:offset + 2571 - offset]
+        view.copy_(_logits(rng, 6, view.shape[1], DTYPES[dtype]))
+        scores = torch.zeros(6, device="cuda:0")
+        got = ck.cocktail_beam_select(view, scores, 3, keep=7)
+        assert _check(view, scores, 3, 7, -1, None, got)
+        whole = ck.cocktail_beam_select(view.contiguous(), scores, 3, keep=7)
+        assert torch.equal(got[0], whole[0]) and torch.equal(got[1], whole[1])
+
+
+@gpu
+def test_results_in_place_and_given():
+    rng = np.random.default_rng(12)
+    logits, scores = _logits(rng, 8, 4000, torch.float32), torch.from_numpy(rng.standard_normal(8).astype(np.float32)).cuda()
+    finished = torch.tensor([False, True] * 4, device="cuda:0")
+    want = ck.cocktail_beam_select(logits, scores, 4, eos=5, finished=finished)
+    source, token = (torch.zeros(2, 4, dtype=torch.int32, device="cuda:0") for _ in range(2))
+    got = ck.cocktail_beam_select(logits, scores, 4, eos=5, finished=finished, out=(source, token, scores, finished))
+    assert got[0] is source and got[2] is scores
+    for x, y in zip(got, want):
+        assert torch.equal(x.view(2, 4), y)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 2, 12, 64, 300, 4096])
+def test_reordering(rows):
+    rng = np.random.default_rng(rows)
+    make = lambda *shape: torch.from_numpy(rng.integers(0, 256, (rows, *shape), dtype=np.uint8)).to("cuda:0")  # noqa: E731
+    most = 40000 if rows <= 64 else 500
+    states = [make(64), make(7), make(4, 5), make(), make(most // 16 * 16), make(0), make(4100 if rows <= 300 else 36).view(rows, -1, 4), make(most | 1)]
+    states.append(make(260)[:, :256].contiguous().view(torch.float16))
+    base = torch.from_numpy(rng.integers(0, 256, rows * 48 + 4, dtype=np.uint8)).to("cuda:0")
+    states.append(base[4:].view(rows, 48))                                                    # rows of whole pieces from an address of four bytes
+    source = torch.from_numpy(rng.integers(-2, rows + 2, rows).astype(np.int32)).to("cuda:0")
+    want = [O.reorder(t.cpu().numpy(), source.tolist()) for t in states]
+    out = [torch.full_like(t, 77) for t in states]
+    kept = [t.clone() for t in states]
+    assert ck.cocktail_beam_reorder(source, states, out=out) == out
+    moved = ((source >= 0) & (source < rows)).cpu().numpy()
+    for t, o, w, old in zip(states, out, want, kept):
+        assert torch.equal(t.view(torch.uint8) if t.dtype == torch.float16 else t, old.view(torch.uint8) if old.dtype == torch.float16 else old)
+        assert np.array_equal(o.cpu().numpy()[moved].view(np.uint8), w[moved].view(np.uint8)) and (o[torch.from_numpy(~moved)] == 77).all()
+    assert all(a is b for a, b in zip(ck.cocktail_beam_reorder(source, states), states))
+    for t, w in zip(states, want):
+        assert np.array_equal(t.cpu().numpy().view(np.uint8), w.view(np.uint8))
