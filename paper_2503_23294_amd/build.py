@@ -24,7 +24,7 @@ FLAGS = [
 
 # products whose sums need more registers than a wave has of one kind: let them lie in either kind, which saves most of the moves between the two (not
 # all: four operands of 128 channels move some 90 words per 32 keys)
-FILE_FLAGS = {"fp4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FILE_FLAGS = {"fp4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "kv16_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc() -> str:

@@ -4,7 +4,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "kv16_attention.h"
+#include "kv16_decode_impl.h"
 
 namespace cocktail {
 
@@ -20,7 +20,8 @@ __global__ __launch_bounds__(64) void kv16_rows_kernel(Kv16Attention args) {
   // which rows
   int b = -1, tile = 0, run = 0;
   for (int base = 0; base < bt.num_seqs && b < 0; base += 64) {
-    const int n = base + lane < bt.num_seqs ? (paged_span(bt, base + lane).count * a.rep + 15) >> 4 : 0;
+    const int count = base + lane < bt.num_seqs ? paged_span(bt, base + lane).count * a.rep : 0;
+    const int n = count > a.decode_rows ? (count + 15) >> 4 : 0;
     const int upto = wave_prefix(n);
     const uint64_t mask = __ballot(number >= run + upto - n && number < run + upto);
     if (mask) {
@@ -143,15 +144,47 @@ int check_attention(const cocktail_kv16_cache* c, int32_t num_q_heads, int64_t t
   return COCKTAIL_OK;
 }
 
+// What a call launches, from what the host knows: bounds, no lengths.
+struct Split {
+  bool decode, tiles;
+  int rows, row_tiles, workers;
+  int64_t active;   // sequences that have queries at most
+  size_t prefix_bytes, part_rows, bytes;
+};
+
+Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max_new, int64_t max_len, bool uniform) {
+  Split s = {};
+  const int64_t capacity = int64_t(c->pages.table_stride) * c->pages.page_size;
+  if (max_len <= 0 || max_len > capacity) max_len = capacity;
+  const int64_t most_rows = max_new * rep;
+  s.active = c->pages.num_seqs < total ? c->pages.num_seqs : total;
+  // A batch may hold sequences for either kernel, unless all have the same number of queries or the others cannot have so many that one is left with
+  // few: then the tile kernel has them all, whatever their numbers are.
+  s.tiles = most_rows > kDecodeRows;
+  const int64_t least = total - (int64_t(c->pages.num_seqs) - 1) * max_new;
+  s.decode = !s.tiles || (!uniform && rep <= kDecodeRows && least * rep <= kDecodeRows);
+  s.rows = int(most_rows < kDecodeRows ? most_rows : kDecodeRows);
+  s.row_tiles = (s.rows + 15) / 16;
+  if (s.decode) {
+    const int64_t units = s.active * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
+    int64_t workers = (units + 3) / 4;
+    const int64_t fill = s.row_tiles <= 2 ? 2048 : 1024;
+    workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
+    s.workers = int(workers);
+    s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
+    s.part_rows = 2 * size_t(workers) * s.rows;
+  }
+  s.bytes = s.prefix_bytes + s.part_rows * (c->head_dim + 4) * sizeof(float) + 64;
+  return s;
+}
+
 }  // namespace
 
 extern "C" int cocktail_kv16_attention_workspace(const cocktail_kv16_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,
                                                  int32_t max_len, int32_t uniform, size_t* bytes) {
   if (!bytes) return fail(COCKTAIL_EINVAL, "bytes is NULL");
   if (int rc = check_attention(cache, num_q_heads, total, max_new)) return rc;
-  (void)max_len;
-  (void)uniform;
-  *bytes = total ? 64 : 0;
+  *bytes = total ? split_of(cache, num_q_heads / cache->num_kv_heads, total, max_new, max_len, uniform != 0).bytes : 0;
   return COCKTAIL_OK;
 }
 
@@ -171,7 +204,9 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   if (!workspace) return fail(COCKTAIL_EINVAL, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(COCKTAIL_EALIGN, "workspace must be 16-byte aligned");
   const int hd = cache->head_dim;
-  if (workspace_bytes < 64) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %d are needed", workspace_bytes, 64);
+  a.rep = num_q_heads / cache->num_kv_heads;
+  const Split s = split_of(cache, a.rep, total, max_new, max_len, !starts);
+  if (workspace_bytes < s.bytes) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, s.bytes);
   a.batch.max_new = max_new;
   args.v_pool = static_cast<const char*>(cache->v);
   a.q = static_cast<const char*>(q);
@@ -180,13 +215,46 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   a.stride_t = 2 * stride_t;
   a.stride_h = 2 * stride_h;
   a.bf16 = cache->dtype == COCKTAIL_BF16;
-  a.rep = num_q_heads / cache->num_kv_heads;
   a.scale = (sm_scale > 0.f ? sm_scale : 1.f / std::sqrt(float(hd))) * kLog2e;
-  (void)max_len;
-  const int64_t tiles = total * a.rep / 16 + (cache->pages.num_seqs < total ? cache->pages.num_seqs : total);
+  a.rows = s.rows;
+  a.workers = s.workers;
+  a.decode_rows = s.decode ? kDecodeRows : 0;
+  char* w = static_cast<char*>(workspace);
+  a.prefix = reinterpret_cast<int32_t*>(w);
+  w += s.prefix_bytes;
+  a.part_o = reinterpret_cast<float*>(w);
+  w += s.part_rows * hd * sizeof(float);
+  a.part_ml = reinterpret_cast<float*>(w);
+
   typedef void (*Kernel)(Kv16Attention);
-  static const Kernel kernels[2][2] = {{kv16_rows_kernel<64, false>, kv16_rows_kernel<64, true>}, {kv16_rows_kernel<128, false>, kv16_rows_kernel<128, true>}};
-  const hipError_t e = launch(kernels[hd == 128][a.bf16], dim3(uint32_t(tiles * cache->num_kv_heads)), dim3(64), static_cast<hipStream_t>(stream), args);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = hipSuccess;
+  if (s.decode) {
+    static const Kernel kernels[2][2][4] = {
+        {{kv16_decode_kernel<64, false, 1>, kv16_decode_kernel<64, false, 2>, kv16_decode_kernel<64, false, 3>, kv16_decode_kernel<64, false, 4>},
+         {kv16_decode_kernel<64, true, 1>, kv16_decode_kernel<64, true, 2>, kv16_decode_kernel<64, true, 3>, kv16_decode_kernel<64, true, 4>}},
+        {{kv16_decode_kernel<128, false, 1>, kv16_decode_kernel<128, false, 2>, kv16_decode_kernel<128, false, 3>, kv16_decode_kernel<128, false, 4>},
+         {kv16_decode_kernel<128, true, 1>, kv16_decode_kernel<128, true, 2>, kv16_decode_kernel<128, true, 3>, kv16_decode_kernel<128, true, 4>}}};
+    e = launch_lds(kernels[hd == 128][a.bf16][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, args);
+  }
+  if (e == hipSuccess && s.tiles) {
+    static const Kernel kernels[2][2] = {{kv16_rows_kernel<64, false>, kv16_rows_kernel<64, true>}, {kv16_rows_kernel<128, false>, kv16_rows_kernel<128, true>}};
+    const int64_t tiles = total * a.rep / 16 + s.active;
+    e = launch(kernels[hd == 128][a.bf16], dim3(uint32_t(tiles * cache->num_kv_heads)), dim3(64), st, args);
+  }
+  if (e == hipSuccess && s.decode) {
+    int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
+    if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
+    const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;
+    // states that a row has, about: many of them are read by many waves at a time, a few by one
+    const int parts = int(s.workers / (s.active * cache->num_kv_heads));
+    if (parts >= 16 && most <= 512)
+      e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 16> : merge_decode_kernel<Kv16Cost, 64, 16>, dim3(most), dim3(1024), st, a, most_new);
+    else if (parts >= 12 && most <= 2048)
+      e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 4> : merge_decode_kernel<Kv16Cost, 64, 4>, dim3(most), dim3(256), st, a, most_new);
+    else
+      e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 1> : merge_decode_kernel<Kv16Cost, 64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
+  }
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return COCKTAIL_OK;
 }
