@@ -3,16 +3,17 @@
 
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 
 namespace cocktail {
 
-// The selection is two launches.  The first reads the logits once: a workgroup has a piece of a row, keeps its largest value and the sum of exponentials
-// against it, and the `keep` largest logits of the piece; a logit is compared with the smallest of those that are wanted so far, and only what
-// is larger goes into a buffer, which is sorted 64 at a time.  The second has a workgroup per request: it joins the pieces of
-// every row to log sum exp, turns the pieces' candidates into values and selects among them.  All keys differ (a value, then the lower
-// place first), so that the order in which candidates are met does not matter.
+// The selection is two launches.  The first reads the logits once: a workgroup has a piece of a row, sums exponentials against a reference that is
+// only raised when a logit exceeds it by far, and keeps the `keep` largest logits of the piece: a logit is compared with a bound that `keep` of the
+// workgroup's are not below, made of the lanes' maxima, and only what reaches it goes into a buffer, which is sorted 64 at a time.  The second has a workgroup
+// per request: it joins the pieces of every row to log sum exp, turns the pieces' candidates into values and selects among them.  All keys
+// differ (a value, then the lower place first), so that the order in which candidates are met does not matter.
 constexpr int kSelectWaves = 4;
 constexpr int kMostKeep = COCKTAIL_MAX_KEEP;
 constexpr int kPerLane = 8;              // logits that a lane takes at a time
@@ -41,35 +42,74 @@ struct ValueKey {
 __device__ __forceinline__ uint64_t value_place(int j, uint32_t logit, uint32_t token) {
   return uint64_t(63 - j) << 56 | uint64_t(logit) << 24 | (0xffffffu - token);
 }
+__device__ __forceinline__ bool before(uint32_t a, uint32_t b) { return a > b; }
 __device__ __forceinline__ bool before(const LogitKey& a, const LogitKey& b) { return a.x > b.x; }
 __device__ __forceinline__ bool before(const ValueKey& a, const ValueKey& b) { return a.value > b.value || (a.value == b.value && a.place > b.place); }
-__device__ __forceinline__ LogitKey of_lane(const LogitKey& k, int lane) { return {uint64_t(__shfl(static_cast<unsigned long long>(k.x), lane))}; }
-__device__ __forceinline__ ValueKey of_lane(const ValueKey& k, int lane) {
-  return {uint64_t(__shfl(static_cast<unsigned long long>(k.value), lane)), uint64_t(__shfl(static_cast<unsigned long long>(k.place), lane))};
+
+// What lane ^ X has.  Without a trip through shared memory: permutations within quads, mirrors and rotations of sixteen lanes, swaps of rows and of halves.
+template <int X>
+__device__ __forceinline__ uint32_t of_partner(uint32_t v) {
+  auto dpp = [](uint32_t x, auto control) { return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), decltype(control)::value, 0xf, 0xf, true)); };
+  if constexpr (X == 1) return dpp(v, std::integral_constant<int, 0xB1>{});
+  else if constexpr (X == 2) return dpp(v, std::integral_constant<int, 0x4E>{});
+  else if constexpr (X == 4) return dpp(dpp(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{});   // ^ 7, ^ 3
+  else if constexpr (X == 8) return dpp(v, std::integral_constant<int, 0x128>{});
+  else if constexpr (X == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int X>
+__device__ __forceinline__ uint64_t of_partner(uint64_t v) { return uint64_t(of_partner<X>(uint32_t(v >> 32))) << 32 | of_partner<X>(uint32_t(v)); }
+template <int X>
+__device__ __forceinline__ LogitKey of_partner(const LogitKey& k) { return {of_partner<X>(k.x)}; }
+template <int X>
+__device__ __forceinline__ ValueKey of_partner(const ValueKey& k) { return {of_partner<X>(k.value), of_partner<X>(k.place)}; }
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return uint32_t(__builtin_amdgcn_readlane(int(v), lane)); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane) { return uint64_t(of_lane(uint32_t(v >> 32), lane)) << 32 | of_lane(uint32_t(v), lane); }
+__device__ __forceinline__ LogitKey of_lane(const LogitKey& k, int lane) { return {of_lane(k.x, lane)}; }
+__device__ __forceinline__ ValueKey of_lane(const ValueKey& k, int lane) { return {of_lane(k.value, lane), of_lane(k.place, lane)}; }
+
+// The largest of the lanes' values, in all lanes.
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
+  auto step = [&](uint32_t other) { v = other > v ? other : v; };
+  step(of_partner<1>(v));
+  step(of_partner<2>(v));
+  step(of_partner<4>(v));
+  step(of_partner<8>(v));
+  step(of_partner<16>(v));
+  step(of_partner<32>(v));
+  return of_lane(v, 0);
 }
 
-// One step of a bitonic network: the lane keeps the earlier or the later of its key and its partner's.
-template <class Key>
-__device__ __forceinline__ void exchange(Key& k, int partner, bool keep_first) {
-  const Key other = of_lane(k, partner);
+// Steps of a bitonic network: the lane keeps the earlier or the later of its key and its partner's.  Pairs at distance STEP and below it, in
+// blocks of SIZE that are brought into order and, every other one, into the opposite order; FALLING: which of the two the first block's is.
+template <int SIZE, int STEP, bool FALLING, class Key>
+__device__ __forceinline__ void merge_blocks(Key& k, int lane) {
+  const Key other = of_partner<STEP>(k);
+  const bool keep_first = (((lane & STEP) == 0) == (SIZE == 64 || (lane & SIZE) == 0)) == FALLING;
   if (before(other, k) == keep_first) k = other;
+  if constexpr (STEP > 1) merge_blocks<SIZE, STEP / 2, FALLING>(k, lane);
 }
-// The keys of a wave in order, the first one in lane 0.
-template <class Key>
+// The keys of a wave in order: the first one in lane 0 (FALLING), or in lane 63.
+template <bool FALLING, class Key>
 __device__ __forceinline__ Key sorted(Key k, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-    for (int step = size >> 1; step; step >>= 1) exchange(k, lane ^ step, ((lane & step) == 0) == ((lane & size) == 0 || size == 64));
+  merge_blocks<2, 1, true>(k, lane);
+  merge_blocks<4, 2, true>(k, lane);
+  merge_blocks<8, 4, true>(k, lane);
+  merge_blocks<16, 8, true>(k, lane);
+  merge_blocks<32, 16, true>(k, lane);
+  merge_blocks<64, 32, FALLING>(k, lane);
   return k;
 }
-// The first 64 of two sorted lists.
+// The first 64, in order, of a list in order and one in the opposite order.
 template <class Key>
 __device__ __forceinline__ Key merged(Key a, const Key& b, int lane) {
-  const Key other = of_lane(b, 63 - lane);
-  if (before(other, a)) a = other;
-#pragma unroll
-  for (int step = 32; step; step >>= 1) exchange(a, lane ^ step, (lane & step) == 0);
+  if (before(b, a)) a = b;
+  merge_blocks<64, 32, true>(a, lane);
   return a;
 }
 
@@ -96,7 +136,7 @@ struct Best {
     Key k = {};
     if (lane < n) k = buffer[count - n + lane];
     count -= n;
-    list = merged(list, sorted(k, lane), lane);
+    list = merged(list, sorted<false>(k, lane), lane);
     border = of_lane(list, keep - 1);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -129,40 +169,72 @@ struct BeamSelect {
 // Whether a row has candidates that its logits say.
 __device__ __forceinline__ bool reads_logits(const BeamSelect& a, int row) { return a.scores[row] > -__builtin_inff() && !(a.finished && a.finished[row]); }
 
-template <class T>
-__device__ __forceinline__ float as_logit(T x) {
-  const float f = float(x);
-  // no number: none; an infinite one counts as the largest; -0 as 0
-  return f != f ? -__builtin_inff() : fminf(f, FLT_MAX) + 0.f;
+// No number becomes none, an infinite one the largest.  (A maximum is the other operand where one is a quiet no-number, which the sum makes of a
+// signalling one.)
+__device__ __forceinline__ float clean_logit(float x) { return fminf(fmaxf(x + 0.f, -__builtin_inff()), FLT_MAX); }
+
+// The largest of eight; what is no number is passed over, or comes out.  (The instruction itself: a maximum of the language quiets every operand first.)
+__device__ __forceinline__ float most_of(const float* x) {
+  auto max3 = [](float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+  };
+  static_assert(kPerLane == 8, "");
+  const float a = max3(x[0], x[1], x[2]), b = max3(x[3], x[4], x[5]), c = max3(x[6], x[7], a);
+  return max3(b, c, c);
 }
 
-// Eight logits from a multiple of eight (counted from the first aligned address at or before the row), those outside of the row as none.
+// Eight logits as they are in memory.
 template <class T>
-__device__ __forceinline__ void load_logits(const T* row, int skip, int vocab, int64_t piece, float* x) {
-  const int64_t at = piece * kPerLane - skip;
-  if (at >= 0 && at + kPerLane <= vocab) {
-    constexpr int kWords = sizeof(T) * kPerLane / 16;
-    u32x4 w[kWords];
-    const u32x4* src = reinterpret_cast<const u32x4*>(row + at);
+struct Logits {
+  u32x4 w[sizeof(T) * kPerLane / 16];
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t word = w[i >> 2][i & 3];
+      return __builtin_bit_cast(float, word);
+    } else {
+      const uint32_t word = w[0][i >> 1];
+      return float(__builtin_bit_cast(T, uint16_t(i & 1 ? word >> 16 : word)));
+    }
+  }
+};
+
+// A wave's tile: eight logits a lane from a multiple of eight (counted from the first aligned address at or before the row), those outside of the row as
+// none.  (Nothing is made of what a tile within the row brings, so that nobody waits for it here.)
+template <class T>
+__device__ __forceinline__ void load_logits(const T* row, int skip, int vocab, int64_t tile, int lane, Logits<T>& x) {
+  constexpr int kWords = sizeof(T) * kPerLane / 16;
+  const int64_t first = tile * (64 * kPerLane) - skip;
+  const T* src = row + first + lane * kPerLane;
+  if (first >= 0 && first + 64 * kPerLane <= vocab) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = __builtin_nontemporal_load(src + i);
-    T t[kPerLane];
-    __builtin_memcpy(t, w, sizeof t);
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) x[i] = as_logit(t[i]);
+    for (int i = 0; i < kWords; ++i) x.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src) + i);
   } else {
+    const int64_t at = first + lane * kPerLane;
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) x[i] = at + i >= 0 && at + i < vocab ? as_logit(row[at + i]) : -__builtin_inff();
+    for (int i = 0; i < kPerLane; ++i) {
+      const bool there = at + i >= 0 && at + i < vocab;
+      if constexpr (sizeof(T) == 4) {
+        x.w[i >> 2][i & 3] = there ? __builtin_bit_cast(uint32_t, src[i]) : 0xff800000u;
+      } else {
+        const uint32_t v = there ? uint32_t(__builtin_bit_cast(uint16_t, src[i])) : __builtin_bit_cast(uint16_t, T(-__builtin_inff()));
+        x.w[0][i >> 1] = i & 1 ? x.w[0][i >> 1] | v << 16 : v;
+      }
+    }
   }
 }
 
 constexpr float kLog2eBeam = 1.4426950408889634f;
+constexpr float kSlackBeam = 16.f;   // by which a logit may exceed the reference: exponentials up to 2^23
 
 template <class T>
 __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSelect a) {
   __shared__ LogitKey buffers[kSelectWaves][kBuffer];
   __shared__ double lds_sum[kSelectWaves];
   __shared__ float lds_top[kSelectWaves];
+  __shared__ uint32_t lds_border;   // ordered value that `keep` logits of the workgroup's are not below
+  if (threadIdx.x == 0) lds_border = 0;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   if (!reads_logits(a, row)) return;
@@ -175,62 +247,89 @@ __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSele
   const int64_t tile0 = tiles * piece / a.pieces, tile1 = tiles * (piece + 1) / a.pieces;
 
   Best<LogitKey> best(buffers[wave], a.keep, lane);
-  float top = -FLT_MAX;
-  double sum = 0.0;
-  uint32_t border = 0;   // ordered value of the border
-  float next[kPerLane];
+  float ref = -FLT_MAX;          // of the wave's exponentials
+  double sum = 0.0;              // of the lane's
+  float lane_most = -__builtin_inff();
+  float border = -FLT_MAX;       // logits below it are not wanted
+  // two tiles are on their way while one is worked on
+  Logits<T> next[2];
   int64_t tile = tile0 + wave;
-  if (tile < tile1) load_logits(src, skip, a.vocab, tile * 64 + lane, next);
-  for (bool first = true; tile < tile1; tile += kSelectWaves, first = false) {
+  int done = 0;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+    if (tile + d * kSelectWaves < tile1) load_logits(src, skip, a.vocab, tile + d * kSelectWaves, lane, next[d]);
+  __syncthreads();
+  auto step = [&](Logits<T>& own) __attribute__((always_inline)) {
     float x[kPerLane];
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) x[i] = next[i];
-    if (tile + kSelectWaves < tile1) load_logits(src, skip, a.vocab, (tile + kSelectWaves) * 64 + lane, next);
-    float most = x[0];
+    for (int i = 0; i < kPerLane; ++i) x[i] = own.at(i);
+    if (tile + 2 * kSelectWaves < tile1) load_logits(src, skip, a.vocab, tile + 2 * kSelectWaves, lane, own);
+    float most = most_of(x);
+    auto raise = [&]() __attribute__((always_inline)) {
+      const float raised = fmaxf(ref, fminf(from_ordered(wave_most(most == most && most > -__builtin_inff() ? ordered(most) : ordered(-FLT_MAX))), FLT_MAX));
+      sum *= __builtin_amdgcn_exp2f((ref - raised) * kLog2eBeam);
+      ref = raised;
+    };
+    auto exponentials = [&]() __attribute__((always_inline)) {
+      float part = 0.f;
 #pragma unroll
-    for (int i = 1; i < kPerLane; ++i) most = fmaxf(most, x[i]);
-    if (most > top) {
-      sum *= __builtin_amdgcn_exp2f((top - most) * kLog2eBeam);
-      top = most;
+      for (int i = 0; i < kPerLane; ++i) part += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2eBeam);
+      return part;
+    };
+    if (__any(most > ref + kSlackBeam)) raise();
+    float part = exponentials();
+    if (__any(!(part < FLT_MAX))) {
+      // logits that are no numbers or infinite
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) x[i] = clean_logit(x[i]);
+      most = most_of(x);
+      raise();
+      part = exponentials();
     }
-    float part = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) part += __builtin_amdgcn_exp2f((x[i] - top) * kLog2eBeam);
     sum += part;
-    const uint32_t mine = most == -__builtin_inff() ? 0 : ordered(most);
-    if (first) {
-      // as many logits as are wanted are not below the keep-th of the lanes' largest
-      const LogitKey k = sorted(LogitKey{uint64_t(mine)}, lane);
-      border = uint32_t(of_lane(k, a.keep - 1).x);
+    lane_most = fmaxf(lane_most, most);
+    // the bound: the keep-th of the lanes' maxima, after 1, 2, 4, 8 ... tiles, and what other waves found
+    if ((done & (done + 1)) == 0) {
+      const uint32_t mine = lane_most > -__builtin_inff() ? ordered(lane_most + 0.f) : 0;
+      const uint32_t bound = of_lane(sorted<true>(mine, lane), a.keep - 1);
+      if (bound) atomicMax(&lds_border, bound);
     }
-    if (__any(mine && mine >= border)) {
+    ++done;
+    const uint32_t shared = lds_border;
+    if (shared) border = fmaxf(border, from_ordered(shared));
+    if (__any(most >= border)) {
       const int64_t at = (tile * 64 + lane) * kPerLane - skip;
 #pragma unroll
       for (int i = 0; i < kPerLane; ++i) {
-        const LogitKey k = {uint64_t(ordered(x[i])) << 32 | uint32_t(~uint32_t(at + i))};
-        best.offer(k, x[i] > -__builtin_inff() && uint32_t(k.x >> 32) >= border && before(k, best.border));
+        if (!__any(x[i] >= border)) continue;
+        const LogitKey k = {uint64_t(ordered(x[i] + 0.f)) << 32 | uint32_t(~uint32_t(at + i))};   // (-0 as 0)
+        best.offer(k, x[i] >= border && before(k, best.border));
       }
-      best.join_full();
-      const uint32_t now = uint32_t(best.border.x >> 32);
-      border = now > border ? now : border;
+      if (best.count >= 64) {
+        best.join_full();
+        if (best.border.x) atomicMax(&lds_border, uint32_t(best.border.x >> 32));
+      }
     }
+  };
+  while (tile < tile1) {
+    step(next[0]);
+    tile += kSelectWaves;
+    if (tile >= tile1) break;
+    step(next[1]);
+    tile += kSelectWaves;
   }
   best.join_all();
-  // the waves' states together
+  // the lanes' and the waves' states together
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const float other = __shfl_xor(top, d), raised = fmaxf(top, other);
-    const double s = __shfl_xor(sum, d);
-    sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + s * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
-    top = raised;
-  }
-  if (lane == 0) lds_sum[wave] = sum, lds_top[wave] = top;
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) lds_sum[wave] = sum, lds_top[wave] = ref;
   buffers[wave][lane] = best.list;
   __syncthreads();
   if (wave) return;
   LogitKey list = best.list;
+  float top = ref;
   for (int w = 1; w < kSelectWaves; ++w) {
-    list = merged(list, buffers[w][lane], lane);
+    list = merged(list, buffers[w][63 - lane], lane);
     const float other = lds_top[w], raised = fmaxf(top, other);
     sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + lds_sum[w] * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
     top = raised;
@@ -240,68 +339,85 @@ __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSele
   if (lane == 0) a.sums[slot] = sum, a.tops[slot] = top;
 }
 
-__global__ __launch_bounds__(64 * kSelectWaves) void beam_join_kernel(BeamSelect a) {
-  __shared__ ValueKey buffers[kSelectWaves][kBuffer];
-  __shared__ double log_sum[64];
+// Sixteen waves: a row each (or several) for log sum exp, then 64 candidates each at a time, the best of all pieces first; the first wave joins what they kept.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamSelect a) {
+  __shared__ ValueKey kept[kJoinWaves * 64];
+  __shared__ double log_sum[64], score_of[64];
   __shared__ float row_top[64];
   __shared__ uint8_t over[64];
+  __shared__ unsigned long long lds_border;   // ordered value that `keep` candidates are not below
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x, row0 = group * a.beams;
-  // a wave takes every fourth row: its pieces together
-  for (int j = wave; j < a.beams; j += kSelectWaves) {
+  const int lists = a.beams * a.pieces, all = lists * a.keep;
+  if (threadIdx.x == 0) lds_border = 0;
+  // the first candidates are on their way meanwhile
+  LogitKey first_key = {};
+  {
+    const int i = int(threadIdx.x), rank = i / lists, at = i - rank * lists, j = at / a.pieces;
+    if (i < all && reads_logits(a, row0 + j)) first_key = a.keys[(int64_t(row0) * a.pieces + at) * a.keep + rank];
+  }
+  for (int j = wave; j < a.beams; j += kJoinWaves) {
     const int row = row0 + j;
     float top = -FLT_MAX;
     double sum = 0.0;
-    if (reads_logits(a, row)) {
+    const bool live = reads_logits(a, row);
+    if (live) {
       for (int p = lane; p < a.pieces; p += 64) {
         const int64_t slot = int64_t(row) * a.pieces + p;
         const float other = a.tops[slot], raised = fmaxf(top, other);
         sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + a.sums[slot] * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
         top = raised;
       }
+      const float raised = from_ordered(wave_most(ordered(top)));
+      sum *= __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam);
+      top = raised;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const float other = __shfl_xor(top, d), raised = fmaxf(top, other);
-        const double s = __shfl_xor(sum, d);
-        sum = sum * __builtin_amdgcn_exp2f((top - raised) * kLog2eBeam) + s * __builtin_amdgcn_exp2f((other - raised) * kLog2eBeam);
-        top = raised;
-      }
+      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
     }
     if (lane == 0) {
-      log_sum[j] = log(sum);
+      const bool ended = a.finished && a.finished[row];
+      log_sum[j] = live ? log(sum) : 0.0;
       row_top[j] = top;
-      over[j] = a.finished && a.finished[row] ? 1 : 0;
+      score_of[j] = a.scores[row];
+      over[j] = ended;
     }
   }
   __syncthreads();
-  Best<ValueKey> best(buffers[wave], a.keep, lane);
-  const int per_row = a.pieces * a.keep, all = a.beams * per_row;
-  for (int base = wave * 64; base < all; base += 64 * kSelectWaves) {
-    const int i = base + lane, j = i < all ? i / per_row : 0, row = row0 + j;
-    const double score = a.scores[row];
+  ValueKey list = {};
+  for (int base = wave * 64; base < all; base += 64 * kJoinWaves) {
+    // the best of every piece, then the second ones ...
+    const int i = base + lane, rank = i / lists, at = i - rank * lists, j = i < all ? at / a.pieces : 0;
+    const double score = score_of[j];
     ValueKey k = {};
-    bool there = false;
     if (i < all && score > -__builtin_inf()) {
       if (over[j]) {
-        // one candidate
-        there = i == j * per_row;
-        k = {ordered(score), value_place(j, 0, uint32_t(a.eos))};
+        if (rank == 0 && at == j * a.pieces) k = {ordered(score), value_place(j, 0, uint32_t(a.eos))};   // one candidate
       } else {
-        const LogitKey x = a.keys[int64_t(row) * per_row + (i - j * per_row)];
-        there = x.x != 0;
+        const LogitKey x = base == wave * 64 ? first_key : a.keys[(int64_t(row0) * a.pieces + at) * a.keep + rank];
         const uint32_t logit = uint32_t(x.x >> 32);
-        if (there) k = {ordered(score + ((double(from_ordered(logit)) - row_top[j]) - log_sum[j])), value_place(j, logit, ~uint32_t(x.x))};
+        if (x.x) k = {ordered(score + ((double(from_ordered(logit)) - row_top[j]) - log_sum[j])), value_place(j, logit, ~uint32_t(x.x))};
       }
     }
-    best.offer(k, there && before(k, best.border));
-    best.join_full();
+    if (k.value < lds_border) k = {};
+    if (!__any(k.value != 0)) continue;
+    list = base == wave * 64 ? sorted<true>(k, lane) : merged(list, sorted<false>(k, lane), lane);
+    const uint64_t bound = of_lane(list, a.keep - 1).value;
+    if (bound && lane == 0) atomicMax(&lds_border, static_cast<unsigned long long>(bound));
   }
-  best.join_all();
-  buffers[wave][lane] = best.list;
+  // `keep` of every wave's
+  if (lane < a.keep) kept[wave * a.keep + lane] = list;
   __syncthreads();
   if (wave) return;
-  ValueKey list = best.list;
-  for (int w = 1; w < kSelectWaves; ++w) list = merged(list, buffers[w][lane], lane);
+  const int rest = a.keep * kJoinWaves;
+  const uint64_t border = lds_border;
+  list = lane < rest ? kept[lane] : ValueKey{};
+  list = sorted<true>(list, lane);
+  for (int base = 64; base < rest; base += 64) {
+    ValueKey k = base + lane < rest ? kept[base + lane] : ValueKey{};
+    if (k.value < border) k = {};
+    if (__any(k.value != 0)) list = merged(list, sorted<false>(k, lane), lane);
+  }
   if (lane >= a.keep) return;
   const bool there = list.value != 0;
   const int j = there ? 63 - int(list.place >> 56) : 0;
@@ -482,7 +598,7 @@ extern "C" int cocktail_beam_select(const void* logits, int32_t dtype, int64_t s
   const uint32_t blocks = uint32_t(groups) * uint32_t(beams) * uint32_t(s.pieces);
   hipError_t e = launch(dtype == COCKTAIL_FP32 ? beam_pieces_kernel<float> : dtype == COCKTAIL_BF16 ? beam_pieces_kernel<__bf16> : beam_pieces_kernel<_Float16>,
                         dim3(blocks), dim3(64 * kSelectWaves), st, a);
-  if (e == hipSuccess) e = launch(beam_join_kernel, dim3(uint32_t(groups)), dim3(64 * kSelectWaves), st, a);
+  if (e == hipSuccess) e = launch(beam_join_kernel, dim3(uint32_t(groups)), dim3(64 * kJoinWaves), st, a);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "beam selection launch failed: %s", hipGetErrorString(e));
   return COCKTAIL_OK;
 }

@@ -159,6 +159,9 @@ def test_what_has_no_probability_is_no_candidate(dtype):
     logits[1] = float("nan")
     logits[2, 5:] = -inf                               # five tokens are left
     logits[3, ::2] = float("nan")
+    bits = torch.int32 if dtype == "fp32" else torch.int16
+    logits[3].view(bits)[1::6] = {"fp16": 0x7c01, "bf16": 0x7f81, "fp32": 0x7f800001}[dtype]      # signalling ones
+    logits[3].view(bits)[3::6] = {"fp16": -0x3ff, "bf16": -0x7f, "fp32": -0x7fffff}[dtype]        # of the other sign
     logits[4, 7], logits[4, 2000] = inf, inf           # two that share all of it
     logits[5] = torch.finfo(dt).min                    # the lowest value everywhere: a level row
     logits[6, 10:] = torch.finfo(dt).min
