@@ -82,8 +82,21 @@ def cocktail_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int,
     return source, token, score, ended
 
 
-def _span(t: torch.Tensor) -> Tuple[int, int]:
-    return t.data_ptr(), t.data_ptr() + t.nbytes
+_ARRAYS = {}   # ctypes array types by length
+
+
+def _overlap(written, read) -> bool:
+    """Whether one of the spans (first, end) that are written has bytes in common with another one, or with one that is read."""
+    spans = sorted([(a, b, True) for a, b in written if b > a] + [(a, b, False) for a, b in read if b > a])
+    end_written = end_read = 0
+    for first, end, own in spans:
+        if first < end_written or (own and first < end_read):
+            return True
+        if own:
+            end_written = max(end_written, end)
+        else:
+            end_read = max(end_read, end)
+    return False
 
 
 def cocktail_beam_reorder(source: torch.Tensor, states: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None,
@@ -103,25 +116,29 @@ def cocktail_beam_reorder(source: torch.Tensor, states: Sequence[torch.Tensor], 
     _vector("source", source, (torch.int32,), rows, dev)
     states = list(states)
     result = states if out is None else list(out)
-    if len(result) != len(states):
+    n, index = len(states), dev.index
+    if len(result) != n:
         raise ValueError("out must have a tensor for every state")
-    n = len(states)
-    addresses = C.c_void_p * n
+    read, written, sizes = [], [], []
     for t, o in zip(states, result):
-        for x in (t, o):
-            if x.device != dev or not x.is_contiguous() or x.dim() < 1 or x.shape[0] != rows:
-                raise TypeError(f"states must be contiguous tensors [{rows}, ...] on {dev}")
-        if o.dtype != t.dtype or o.shape != t.shape:
-            raise ValueError("out must have the states' types and shapes")
-    # what is written may overlap with nothing else: neighbours in the order of their addresses tell
-    spans = sorted((*_span(t), i, 0) for i, t in enumerate(states)) if out is None else \
-        sorted([(*_span(t), i, 1) for i, t in enumerate(states)] + [(*_span(t), i, 0) for i, t in enumerate(result)])
-    end = [0, 0]   # of what is written, of what is only read
-    for first, stop, i, read in spans:
-        if stop > first:
-            if first < end[0] or (not read and first < end[1]):
-                raise ValueError("states that are written must not overlap with others")
-            end[read] = max(end[read], stop)
-    check(lib().cocktail_beam_reorder(source.data_ptr(), rows, addresses(*[t.data_ptr() for t in states]), addresses(*[t.data_ptr() for t in result]),
-                                      (C.c_int64 * n)(*[t.nbytes // rows for t in states]), n, handle))
+        if t.get_device() != index or not t.is_contiguous() or t.dim() < 1 or t.size(0) != rows:
+            raise TypeError(f"states must be contiguous tensors [{rows}, ...] on {dev}")
+        size, at = t.nbytes, t.data_ptr()
+        sizes.append(size // rows)
+        if o is not t:
+            if o.get_device() != index or not o.is_contiguous():
+                raise TypeError(f"out must have contiguous tensors on {dev}")
+            if o.dtype != t.dtype or o.shape != t.shape:
+                raise ValueError("out must have the states' types and shapes")
+            read.append((at, at + size))
+            at = o.data_ptr()
+        written.append((at, at + size))
+    if n and _overlap(written, read):
+        raise ValueError("states that are written must not overlap with others")
+    arrays = _ARRAYS.get(n)
+    if arrays is None:
+        arrays = _ARRAYS[n] = C.c_void_p * n, C.c_int64 * n
+    to = arrays[0](*[a for a, _ in written])
+    of = to if not read else arrays[0](*[t.data_ptr() for t in states])
+    check(lib().cocktail_beam_reorder(source.data_ptr(), rows, of, to, arrays[1](*sizes), n, handle))
     return result
