@@ -112,42 +112,43 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
   auto place_k = [&](int key) { return (key & 31) * kRowPieces + (piece ^ (HD == 128 ? key & 15 : key >> 1 & 7)); };
   auto place_v = [&](int key) { return key * kRowPieces + (piece ^ 4 * (HD == 128 ? key & 3 : key >> 1 & 1)); };
 
-  // The 16-token tiles of the keys in order: the table is read ahead of the loads, these ahead of their use, without
-  // conditions (behind the last tile it is the last tile again, which is masked by its number).  V of a step is loaded a step after its K.
+  // Where the 16-token tiles of the keys are: a lane knows one of 64, sixteen steps, and a step takes its own from there with a few scalar instructions
+  // (looked up a tile after the other by the scalar unit, they cost a tenth of the kernel's time).  The table is read sixteen steps ahead; behind the
+  // last tile it is the last tile again, which is masked by its number.  V of a step is loaded a step after its K.
   const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
   const int last_tile = len > 0 ? (len - 1) >> 4 : 0;
-  const int tiles_per_page = P / 16;
-  int next16 = 4 * k0, col = next16 / tiles_per_page, in_page = next16 - col * tiles_per_page;
-  int id[4], at[4];
-  auto next_tiles = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      id[x] = table_entry(table + col);
-      at[x] = in_page;
-      const int more = next16 < last_tile ? 1 : 0;
-      next16 += more;
-      in_page += more;
-      const bool turn = in_page == tiles_per_page;
-      col += turn ? 1 : 0;
-      in_page = turn ? 0 : in_page;
-    }
+  const uint32_t tiles_per_page = P / 16;
+  int next16 = 4 * k0 + lane, ahead_id = 0, ahead_at = 0;   // of the next sixteen steps
+  auto look_ahead = [&]() __attribute__((always_inline)) {
+    const uint32_t t = next16 < last_tile ? next16 : last_tile, col = t / tiles_per_page;
+    ahead_id = table[col];
+    ahead_at = int(t - col * tiles_per_page) * (32 * HD);
+    next16 += 64;
   };
+  uint32_t place_lo = 0, place_hi = 0;   // bytes from the head's run of the first page
+  uint64_t bad_tiles = 0;
+  int taken = 64;                        // tiles of these that steps have taken
   u32x4 raw_k[kPieces], raw_v[kPieces];
   int64_t from_v[kPieces];         // of the step whose K was loaded last
   int bad_k;                       // its tiles that lie on no page, a bit each
   auto load_k = [&]() __attribute__((always_inline)) {
-    bad_k = 0;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) bad_k |= uint32_t(id[y]) < uint32_t(bt.num_pages) ? 0 : 1 << y;
+    if (taken == 64) {
+      const bool ok = uint32_t(ahead_id) < uint32_t(bt.num_pages);
+      const int64_t place = (ok ? ahead_id : 0) * page_bytes + ahead_at;
+      place_lo = uint32_t(place);
+      place_hi = uint32_t(place >> 32);
+      bad_tiles = ~__ballot(ok);
+      taken = 0;
+      look_ahead();
+    }
+    bad_k = int(bad_tiles >> taken) & 15;
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) {
-      // the wave's tile among the four
-      const int sub = (x * kKeysAtOnce >> 4) + wave_tile;
-      const int page = sub == 0 ? id[0] : sub == 1 ? id[1] : sub == 2 ? id[2] : id[3];
-      const int tile_at = sub == 0 ? at[0] : sub == 1 ? at[1] : sub == 2 ? at[2] : at[3];
-      from_v[x] = head + (uint32_t(page) < uint32_t(bt.num_pages) ? page : 0) * page_bytes + tile_at * (32 * HD);
+      const int at = taken + (x * kKeysAtOnce >> 4) + wave_tile;
+      from_v[x] = head + int64_t(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(place_hi), at))) << 32 | uint32_t(__builtin_amdgcn_readlane(int(place_lo), at)));
       raw_k[x] = *reinterpret_cast<const u32x4*>(bt.pool + from_v[x] + off);
     }
+    taken += 4;
   };
   auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -278,22 +279,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
 
   if (k0 < k1) {
     // K of the first two steps and V of the first one into LDS, K of the third and V of the second on their way
-    next_tiles();
+    look_ahead();
     load_k();
-    next_tiles();
     load_v();
     int bad0 = bad_k, bad1;         // of this step and of the next
     clean_v(k0, bad0);
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) stage_k(x, 0, 1), stage_v(x, 0);
     load_k();
-    next_tiles();
     load_v();
     bad1 = bad_k;
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) stage_k(x, 2, 3);
     load_k();
-    next_tiles();
     __syncthreads();
     const bool idle = wave_first >= rows;
     f32x16 s0, s1;
@@ -322,7 +320,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       bad1 = bad_k;
       load_v();
       load_k();
-      next_tiles();
       if (!idle && step + 1 < k1) mask(s0, (step + 1) * kTileKeys, bad0 & 3);
       chunk = slot2;
       __syncthreads();
