@@ -224,10 +224,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
     for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] *= alpha;
   };
 
-  // One half of a step: logits of the next 32 keys (`ahead`, from `chunk`), next to the weights of these (`s`); then these' products with V
-  // (32 keys from `rows_v`), next to the putting away of what has been loaded (`put`, kPieces times).  The order is written down
-  // and kept: a product every few other instructions, its operands read four products before.
-  auto half_step = [&](const f32x16& s, f32x16& ahead, const u32x4* chunk, const u32x4* rows_v, auto&& put) __attribute__((always_inline)) {
+  // One half of a step, for 32 keys with logits `s`: the logits of the next 32 (`ahead`, from `chunk`), next to the second half of these' weights; then
+  // these' products with V (from `rows_v`), next to the first half of the next ones' weights and to the putting away of what has been loaded (`put`,
+  // kPieces times).  So both kinds of products have as many exponentials beside them.  The order is written down and kept: a product every few other
+  // instructions, its operands read four products before.
+  uint32_t w[8];                    // weights of the next products with V, those of keys 0 .. 15 from the half step before
+  float first_sum = 0.f;            // of these
+  auto weigh = [&](const f32x16& s, int y, float& sum) __attribute__((always_inline)) {
+    const float a0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -m)), a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y + 1], c, -m));
+    sum += a0 + a1;
+    w[y / 2] = pack_weights<BF16>(a0, a1);
+  };
+  auto half_step = [&](const f32x16& s, f32x16& ahead, const u32x4* chunk, const u32x4* rows_v, int next_tok, int next_bad, auto&& put) __attribute__((always_inline)) {
     constexpr int kLead = 4;
     constexpr int kProductsV = 2 * kChannelTiles;
     constexpr int kOrder = 0x4 | 0x10 | 0x20 | 0x40;   // scalar instructions and loads may move
@@ -235,23 +243,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
     auto fetch_k = [&](int x) { kf[x] = read_k(chunk, x); };
     auto fetch_v = [&](int x) { vf[x] = read_v(rows_v, x % kChannelTiles, x / kChannelTiles); };
     ahead = f32x16{};
-    uint32_t w[8];
-    float sum = 0.f;
+    float sum = first_sum;
 #pragma unroll
     for (int x = 0; x < kLead; ++x) fetch_k(x);
     __builtin_amdgcn_sched_barrier(kOrder);
-    constexpr int kPer = 16 / kSteps;   // weights per product
+    constexpr int kEveryK = kSteps / 4, kEveryV = kProductsV / 4;   // products per pair of weights
 #pragma unroll
     for (int x = 0; x < kSteps; ++x) {
       if (x + kLead < kSteps) fetch_k(x + kLead);
       else if (x + kLead - kSteps < kProductsV) fetch_v(x + kLead - kSteps);
       ahead = product32<BF16>(kf[x], q[x], ahead);
-#pragma unroll
-      for (int y = x * kPer; y < (x + 1) * kPer; y += 2) {
-        const float a0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -m)), a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y + 1], c, -m));
-        sum += a0 + a1;
-        w[y / 2] = pack_weights<BF16>(a0, a1);
-      }
+      if (x % kEveryK == kEveryK - 1) weigh(s, 8 + 2 * (x / kEveryK), sum);
       __builtin_amdgcn_sched_barrier(kOrder);
     }
     // Whether the reference is too small shows in the sum of the weights: then each of them was too large at most by that (the products have not
@@ -260,19 +262,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       raise(s);
       sum = 0.f;
 #pragma unroll
-      for (int y = 0; y < 16; y += 2) {
-        const float a0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -m)), a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y + 1], c, -m));
-        sum += a0 + a1;
-        w[y / 2] = pack_weights<BF16>(a0, a1);
-      }
+      for (int y = 0; y < 16; y += 2) weigh(s, y, sum);
     }
     lsum += sum;
     const u32x4 p[2] = {u32x4{w[0], w[1], w[2], w[3]}, u32x4{w[4], w[5], w[6], w[7]}};
+    mask(ahead, next_tok, next_bad);
+    first_sum = 0.f;
 #pragma unroll
     for (int x = 0; x < kProductsV; ++x) {
       if (x + kLead < kProductsV) fetch_v(x + kLead);
       o[x % kChannelTiles] = product32<BF16>(vf[x], p[x / kChannelTiles], o[x % kChannelTiles]);
       if (x % 2 == 0) put(x / 2);
+      if (x % kEveryV == kEveryV - 1) weigh(ahead, 2 * (x / kEveryV), first_sum);
       __builtin_amdgcn_sched_barrier(kOrder);
     }
   };
@@ -300,6 +301,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
 #pragma unroll
       for (int x = 0; x < kSteps; ++x) s0 = product32<BF16>(read_k(lds.k[0], x), q[x], s0);
       mask(s0, k0 * kTileKeys, bad0 & 3);
+#pragma unroll
+      for (int y = 0; y < 8; y += 2) weigh(s0, y, first_sum);
     }
     __syncthreads();                // the first step writes into the chunk that these products have read
     int chunk = 0;                  // slot of this step's first chunk
@@ -309,9 +312,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       const int slot4 = chunk + 4 < kRing ? chunk + 4 : chunk + 4 - kRing, slot5 = chunk;
       clean_v(step + 1, bad1);
       if (!idle) {
-        half_step(s0, s1, lds.k[slot1], lds.v[buffer], [&](int x) { if (x < kPieces) stage_v(x, buffer ^ 1); });
-        mask(s1, step * kTileKeys + kChunk, bad0 >> 2);
-        half_step(s1, s0, lds.k[slot2], lds.v[buffer] + kChunk * kRowPieces, [&](int x) { if (x < kPieces) stage_k(x, slot4, slot5); });
+        half_step(s0, s1, lds.k[slot1], lds.v[buffer], step * kTileKeys + kChunk, bad0 >> 2, [&](int x) { if (x < kPieces) stage_v(x, buffer ^ 1); });
+        half_step(s1, s0, lds.k[slot2], lds.v[buffer] + kChunk * kRowPieces, (step + 1) * kTileKeys, bad1 & 3,
+                  [&](int x) { if (x < kPieces) stage_k(x, slot4, slot5); });
       } else {
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) stage_v(x, buffer ^ 1), stage_k(x, slot4, slot5);
@@ -320,7 +323,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       bad1 = bad_k;
       load_v();
       load_k();
-      if (!idle && step + 1 < k1) mask(s0, (step + 1) * kTileKeys, bad0 & 3);
       chunk = slot2;
       __syncthreads();
     }
