@@ -59,8 +59,10 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
   if (s.tiles) {
     const int64_t seqs = c->pages.num_seqs;
     // Eight waves share what it takes to bring the keys into LDS where that leaves a workgroup for every compute unit and the rows see about as
-    // many keys each; else four, whose smaller pieces leave less to wait for at the end.
-    s.tile_waves = total * rep * c->num_kv_heads >= 256 * 256 && most_rows > 128 && max_len >= 2 * max_new ? 8 : 4;
+    // many keys each, or else two of them (head_dim 128, us with four and eight: 2048 new of 8192, 8 x 4 heads 253, 245; prompts of 2048, 3000, 4096, 8192
+    // tokens with 32, 40, 32, 32 heads 63, 68; 115, 125; 160, 158; 573, 550; head_dim 64 the same within 5 %); else four, whose smaller pieces leave less
+    // to wait for at the end.
+    s.tile_waves = total * rep * c->num_kv_heads >= 256 * 256 * (max_len >= 2 * max_new ? 1 : 2) && most_rows > 128 ? 8 : 4;
     const int64_t tile_rows = 32 * s.tile_waves;
     s.tile_blocks = int(uniform ? seqs * ((most_rows + tile_rows - 1) / tile_rows) : total * rep / tile_rows + (seqs < total ? seqs : total));
     const int64_t have = int64_t(s.tile_blocks) * c->num_kv_heads;

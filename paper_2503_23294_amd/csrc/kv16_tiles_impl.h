@@ -2,8 +2,9 @@
 //
 // Bound by the matrix cores and, close behind, by the exponentials of the softmax.  A workgroup takes 128 or 256 rows of one (sequence, kv head), 32
 // per wave, and walks over the keys 64 at a time; K and V are loaded a step or two ahead of their use and go to LDS as they are, rows of channels in
-// pieces of sixteen bytes, and serve all waves.  The pieces of a row lie in an order of the row's own, so that what a load of the products' operands
-// touches is in different banks: of K, the same piece of sixteen rows; of V, which the transposing load reads, 32 bytes of four rows twice.
+// pieces of sixteen bytes, and serve all waves.  What a load of the products' operands touches is in different banks: of K, the same piece of
+// sixteen rows, which are a piece longer than their channels; of V, which the transposing load reads, 32 bytes of four rows twice, whose pieces lie
+// in an order of the row's own.
 // S^T = K Q^T leaves a lane with one query row and half the keys of a step, in the order in which O^T = V^T P^T takes them (the transposing load
 // picks the tokens in that order), so weights stay in their lanes.
 #pragma once
@@ -17,7 +18,7 @@ constexpr int kChunk = 32, kRing = 5;
 constexpr float kSumLimit = 61440.f;   // of the weights of 16 keys that a lane has: their largest is a finite fp16 then (behind a new reference it is 16 * 2^7 at most)
 template <int HD>
 struct Kv16TileLds {
-  u32x4 k[kRing][kChunk * HD / 8];
+  u32x4 k[kRing][kChunk * (HD / 8 + 1)];   // rows shift by four banks
   u32x4 v[2][kTileKeys * HD / 8];
 };
 
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
   const uint32_t off = (own_key & 15) * (2 * HD) + piece * 16;       // inside sixteen tokens (kKeysAtOnce is a multiple of those)
   const int wave_tile = wave * kWaveKeys >> 4;
   // where the piece of key `own_key` goes: K of a key within a chunk, V of a key within a step
-  auto place_k = [&](int key) { return (key & 31) * kRowPieces + (piece ^ (HD == 128 ? key & 15 : key >> 1 & 7)); };
+  auto place_k = [&](int key) { return (key & 31) * (kRowPieces + 1) + piece; };
   auto place_v = [&](int key) { return key * kRowPieces + (piece ^ 4 * (HD == 128 ? key & 3 : key >> 1 & 1)); };
 
   // Where the 16-token tiles of the keys are: a lane knows one of 64, sixteen steps, and a step takes its own from there with a few scalar instructions
@@ -187,10 +188,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
   for (int ct = 0; ct < kChannelTiles; ++ct) o[ct] = f32x16{};
 
   // Operands: of K, lane (row, half) has piece 2 x + half of its row; of V, 32 channels of the four tokens 4 half + .. and of those eight behind them.
-  const uint32_t swizzle_k = HD == 128 ? row_lane & 15 : row_lane >> 1 & 7;
-  const uint32_t base_k = row_lane * (2 * HD) + (half ^ swizzle_k) * 16;
+  const uint32_t base_k = row_lane * (2 * HD + 16) + half * 16;
   auto read_k = [&](const u32x4* chunk, int x) __attribute__((always_inline)) {
-    return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(chunk) + (base_k ^ x * 32));
+    return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(chunk) + base_k + x * 32);
   };
   const int token = lane >> 2 & 3, swizzle_v = HD == 128 ? token : token >> 1;
   const uint32_t base_v = (4 * half + token) * (2 * HD) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
@@ -265,6 +265,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       for (int y = 0; y < 16; y += 2) weigh(s, y, sum);
     }
     lsum += sum;
+    __builtin_amdgcn_s_setprio(1);   // the other wave of the SIMD is to be found beside its exponentials (1 %)
     const u32x4 p[2] = {u32x4{w[0], w[1], w[2], w[3]}, u32x4{w[4], w[5], w[6], w[7]}};
     mask(ahead, next_tok, next_bad);
     first_sum = 0.f;
@@ -276,6 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
       if (x % kEveryV == kEveryV - 1) weigh(ahead, 2 * (x / kEveryV), first_sum);
       __builtin_amdgcn_sched_barrier(kOrder);
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (k0 < k1) {
