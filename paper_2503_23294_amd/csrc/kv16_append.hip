@@ -44,6 +44,8 @@ struct Kv16Token {
   int32_t valid;   // the row belongs to a sequence
 };
 
+// Bound by memory: 4 D bytes a head in and out; 32K tokens of 32 + 8 + 8 heads of 128 (805 MB) 154 us, 5.2 TB/s, where a copy of as much reaches 5.0 .. 5.4;
+// a step of 8 tokens is a launch and a chain of four loads, 4.2 us.
 // A workgroup takes TOKENS rows (blockIdx.x) and a part of their heads (blockIdx.y), a thread sixteen channels of a head at a time: two pieces of
 // sixteen bytes that are the two halves of eight pairs (or eight neighbouring pairs), or are only moved.  What a token needs is found out
 // once, and the sines and cosines are one per (token, pair) in LDS for all heads.
@@ -108,20 +110,20 @@ __global__ __launch_bounds__(256) void kv16_append_kernel(PagedBatch a, Kv16Rows
     turn_sin[t][pair] = s * r.factor;
   }
   __syncthreads();
-  const int heads = r.q_heads + 2 * a.num_kv_heads;
-  const int units = heads * kParts, per_block = (units + int(gridDim.y) - 1) / int(gridDim.y);
-  const int first = int(blockIdx.y) * per_block, last = first + per_block < units ? first + per_block : units;
-  for (int i = tid; i < TOKENS * (last - first); i += 256) {
-    const int t = i / (last - first), unit = first + i - t * (last - first);
+  const int units = (r.q_heads + 2 * a.num_kv_heads) * kParts, per_block = (units + int(gridDim.y) - 1) / int(gridDim.y);
+  const int first = int(blockIdx.y) * per_block, mine = first + per_block < units ? per_block : units - first;
+  // items: the units of the first token, of the second ...; a thread has every 256th of them
+  for (int t = 0, unit = tid;; unit += 256) {
+    while (unit >= mine && t < TOKENS) unit -= mine, ++t;   // (mine > 0)
+    if (t >= TOKENS) break;
     const Kv16Token x = tokens[t];
-    int head = unit / kParts;
-    const int part = unit % kParts;
+    const int at = first + unit, part = at % kParts, row = t0 + t;
+    int head = at / kParts;
     const bool is_q = head < r.q_heads;
     if (!x.valid || (!is_q && x.place < 0)) continue;
     const char* src;
     char* dst;
     bool turned = part * 16 < r.rotary;
-    const int row = t0 + t;
     if (is_q) {
       src = r.q + row * r.q_stride_t + head * r.q_stride_h;
       dst = r.q_out + (int64_t(row) * r.q_heads + head) * (2 * HD);
@@ -249,14 +251,18 @@ extern "C" int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void
     r.factor = rotation->factor;
   }
   r.q_heads = num_q_heads;
-  constexpr int kTokens = 4;
-  const int64_t blocks = (total + kTokens - 1) / kTokens;
-  if (blocks >= (int64_t(1) << 24)) return fail(COCKTAIL_EINVAL, "append of %lld rows is more than one launch takes", (long long)total);
+  // Four tokens share what is to be found out for them where that leaves workgroups enough, else workgroups share a token.  (32K tokens of 48 heads: 2, 4, 8,
+  // 16 tokens 161, 154, 165, 180 us, and with two or four items of a thread on their way instead of one 164 and 173: it is the order in which the memory is
+  // touched; without the caches 157 .. 170, and neighbouring pairs, which write half lines, 287 instead of 184.)
+  const int tokens = total >= 2048 ? 4 : 1;
+  const int parts = tokens == 1 ? ((num_q_heads + 2 * cache->num_kv_heads) * (hd / 16) + 255) / 256 : 1;
+  const int64_t blocks = (total + tokens - 1) / tokens;
+  if (blocks * parts >= (int64_t(1) << 24)) return fail(COCKTAIL_EINVAL, "append of %lld rows is more than one launch takes", (long long)total);
   typedef void (*Kernel)(PagedBatch, Kv16Rows);
-  static const Kernel kernels[2][2] = {{kv16_append_kernel<64, false, kTokens>, kv16_append_kernel<64, true, kTokens>},
-                                       {kv16_append_kernel<128, false, kTokens>, kv16_append_kernel<128, true, kTokens>}};
+  static const Kernel kernels[2][2][2] = {{{kv16_append_kernel<64, false, 1>, kv16_append_kernel<64, false, 4>}, {kv16_append_kernel<64, true, 1>, kv16_append_kernel<64, true, 4>}},
+                                          {{kv16_append_kernel<128, false, 1>, kv16_append_kernel<128, false, 4>}, {kv16_append_kernel<128, true, 1>, kv16_append_kernel<128, true, 4>}}};
   const size_t lds = starts ? (a.num_seqs + 1) * sizeof(int32_t) : 0;
-  const hipError_t e = launch_lds(kernels[hd == 128][cache->dtype == COCKTAIL_BF16], dim3(uint32_t(blocks)), dim3(256), lds, static_cast<hipStream_t>(stream), a, r);
+  const hipError_t e = launch_lds(kernels[hd == 128][cache->dtype == COCKTAIL_BF16][tokens > 1], dim3(uint32_t(blocks), uint32_t(parts)), dim3(256), lds, static_cast<hipStream_t>(stream), a, r);
   if (e != hipSuccess) return fail(COCKTAIL_EHIP, "append launch failed: %s", hipGetErrorString(e));
   return COCKTAIL_OK;
 }

@@ -48,8 +48,11 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
   s.row_tiles = (s.rows + 15) / 16;
   if (s.decode) {
     const int64_t units = s.active * ((max_len + kUnit - 1) / kUnit) * c->num_kv_heads;
-    int64_t workers = (units + 3) / 4;
-    const int64_t fill = s.row_tiles <= 2 ? 2048 : 1024;
+    // A wave per SIMD of 256 compute units: one has 16 KB on their way at any time, which is enough (128K, 40 heads: 390 us; 64 of up to 4K, 8 kv heads:
+    // 512, 768, 1024, 1280, 2048 waves 152, 113, 102, 137, 111).  Of short contexts a wave has one unit, or two where there are more than 512 (2K,
+    // 8 heads: 1, 2, 4 units a wave 11.5, 12.5, 14.6; 8K: 18.8, 14.8, 15.7).
+    int64_t workers = units <= 512 ? units : units <= 1024 ? 512 : units / 2;
+    const int64_t fill = 1024;
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;

@@ -25,7 +25,7 @@ struct Kv16Cost {
 };
 
 template <int HD, bool BF16, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, RT <= 2 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
+__global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
   constexpr int kSteps = HD / 32;           // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
