@@ -27,7 +27,7 @@ int check_attention(const cocktail_kv16_cache* c, int32_t num_q_heads, int64_t t
 
 // What a call launches, from what the host knows: bounds, no lengths.
 struct Split {
-  bool decode, tiles;
+  bool decode, whole, tiles;
   int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
   int64_t active;   // sequences that have queries at most
   size_t prefix_bytes, part_rows, tile_rows, bytes;
@@ -55,6 +55,11 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
     const int64_t fill = 1024;
     workers = workers > fill ? fill : workers < 4 ? 4 : (workers + 3) / 4 * 4;
     s.workers = int(workers);
+    // A workgroup per segment and no merge where contexts are short, of 128 KB of K at most: a compute unit reads no faster (8 heads of 128, 200
+    // tokens: two launches 10.0 us, one 7.7; 1000: 11.5, 14.3; 32 sequences of 512: 19.7, 15.2, of 2048: 48.8, 46.5; 24 x 32 heads, 1024: 68.9, 77.8, of 64
+    // channels 37.2, 33.0).
+    s.whole = s.row_tiles == 1 && max_len * c->head_dim <= 65536;
+    if (s.whole) workers = 0;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
   }
@@ -142,18 +147,21 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   hipError_t e = hipSuccess;
   if (s.decode) {
     static const Kernel kernels[2][2][4] = {
-        {{kv16_decode_kernel<64, false, 1>, kv16_decode_kernel<64, false, 2>, kv16_decode_kernel<64, false, 3>, kv16_decode_kernel<64, false, 4>},
-         {kv16_decode_kernel<64, true, 1>, kv16_decode_kernel<64, true, 2>, kv16_decode_kernel<64, true, 3>, kv16_decode_kernel<64, true, 4>}},
-        {{kv16_decode_kernel<128, false, 1>, kv16_decode_kernel<128, false, 2>, kv16_decode_kernel<128, false, 3>, kv16_decode_kernel<128, false, 4>},
-         {kv16_decode_kernel<128, true, 1>, kv16_decode_kernel<128, true, 2>, kv16_decode_kernel<128, true, 3>, kv16_decode_kernel<128, true, 4>}}};
-    e = launch_lds(kernels[hd == 128][a.bf16][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, args);
+        {{kv16_decode_kernel<64, false, 1, false>, kv16_decode_kernel<64, false, 2, false>, kv16_decode_kernel<64, false, 3, false>, kv16_decode_kernel<64, false, 4, false>},
+         {kv16_decode_kernel<64, true, 1, false>, kv16_decode_kernel<64, true, 2, false>, kv16_decode_kernel<64, true, 3, false>, kv16_decode_kernel<64, true, 4, false>}},
+        {{kv16_decode_kernel<128, false, 1, false>, kv16_decode_kernel<128, false, 2, false>, kv16_decode_kernel<128, false, 3, false>, kv16_decode_kernel<128, false, 4, false>},
+         {kv16_decode_kernel<128, true, 1, false>, kv16_decode_kernel<128, true, 2, false>, kv16_decode_kernel<128, true, 3, false>, kv16_decode_kernel<128, true, 4, false>}}};
+    static const Kernel whole[2][2] = {{kv16_decode_kernel<64, false, 1, true>, kv16_decode_kernel<64, true, 1, true>},
+                                       {kv16_decode_kernel<128, false, 1, true>, kv16_decode_kernel<128, true, 1, true>}};
+    if (s.whole) e = launch(whole[hd == 128][a.bf16], dim3(uint32_t(s.active * cache->num_kv_heads)), dim3(64 * kWholeWaves), st, args);
+    else e = launch_lds(kernels[hd == 128][a.bf16][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, args);
   }
   if (e == hipSuccess && s.tiles) {
     static const Kernel kernels[2][2][2] = {{{kv16_tile_kernel<64, false, 4>, kv16_tile_kernel<64, false, 8>}, {kv16_tile_kernel<64, true, 4>, kv16_tile_kernel<64, true, 8>}},
                                             {{kv16_tile_kernel<128, false, 4>, kv16_tile_kernel<128, false, 8>}, {kv16_tile_kernel<128, true, 4>, kv16_tile_kernel<128, true, 8>}}};
     e = launch(kernels[hd == 128][a.bf16][s.tile_waves == 8], dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * s.tile_waves), st, args);
   }
-  if (e == hipSuccess && s.decode) {
+  if (e == hipSuccess && s.decode && !s.whole) {
     int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
     const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;

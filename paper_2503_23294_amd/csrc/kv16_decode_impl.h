@@ -24,25 +24,32 @@ struct Kv16Cost {
   __device__ static int unit(const PagedAttention&, const PagedSeq&) { return 1; }
 };
 
-template <int HD, bool BF16, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
+// WHOLE: a workgroup of kWholeWaves waves has one segment and shares it out among them, their states are joined in LDS: one launch, for short contexts.
+template <int HD, bool BF16, int RT, bool WHOLE>
+__global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
   constexpr int kSteps = HD / 32;           // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
-  __shared__ int32_t lds_words[kDecodeWaves];
-  __shared__ float lds_state[kDecodeWaves][16][HD + 4];
+  __shared__ int32_t lds_words[kWholeWaves + 1];
+  __shared__ float lds_state[WHOLE ? kWholeWaves : kDecodeWaves][16][HD + 4];   // sums, then (m, l, l unrounded) of WHOLE
   const PagedAttention& a = args.p;
   const PagedBatch& bt = a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j = lane >> 4;
-  const CostLine line = make_line<Kv16Cost>(a, pre, lds_words);
-  const uint32_t share = cost_share<Kv16Cost>(line.total, a.workers);
-  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
-  uint32_t u = w * share;
-  const uint32_t end = u + share < line.total ? u + share : line.total;
-  if (u >= end) return;
-  // read once and not again before hundreds of MB have passed: past the caches
-  const bool stream = uint64_t(line.total) * (kUnit * 4 * HD) > kCachedBytes;
+  CostLine line = {};
+  int w = 0;
+  uint32_t u = 0, end = 1;
+  bool stream = false;
+  if constexpr (!WHOLE) {
+    line = make_line<Kv16Cost>(a, pre, lds_words);
+    const uint32_t share = cost_share<Kv16Cost>(line.total, a.workers);
+    w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+    u = w * share;
+    end = u + share < line.total ? u + share : line.total;
+    if (u >= end) return;
+    // read once and not again before hundreds of MB have passed: past the caches
+    stream = uint64_t(line.total) * (kUnit * 4 * HD) > kCachedBytes;
+  }
   const int P = bt.page_size;
   const uint32_t run = uint32_t(P) * (2 * HD);
   const int64_t page_bytes = int64_t(run) * bt.num_kv_heads;
@@ -50,12 +57,30 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? 2 : 1) void kv16_decod
 
   bool first_segment = true;
   while (u < end) {
-    const CostPlace place = find_place(a, line, pre, u);
+    CostPlace place;
+    int h, u0, u1;
+    if constexpr (WHOLE) {
+      const int number = blockIdx.x / bt.num_kv_heads;
+      h = blockIdx.x - number * bt.num_kv_heads;
+      // more sequences than rows: the workgroups are for those that have any
+      place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
+      if (place.b < 0) return;
+      place.seq = of_lane(decode_seq(a, place.b), 0);
+      if (place.seq.n == 0) return;
+      const uint32_t units = decode_units(place.seq);
+      place.cost = units;
+      u0 = units * wave / kWholeWaves;
+      u1 = units * (wave + 1) / kWholeWaves;
+      u = end;
+    } else {
+      place = find_place(a, line, pre, u);
+      const uint32_t units = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
+      h = local / units;
+      u0 = local - uint32_t(h) * units, u1 = end - u < units - u0 ? u0 + (end - u) : units;
+      u += u1 - u0;
+    }
     const int b = place.b, len = place.seq.len, rows = place.seq.n * a.rep;
-    const uint32_t units = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
-    const int h = local / units;
-    const int u0 = local - uint32_t(h) * units, u1 = end - u < units - u0 ? u0 + (end - u) : units;
-    u += u1 - u0;
+    const uint32_t units = place.cost;
 
     // the queries: lane (row c16, quarter j) has the channels that its K pieces have
     u32x4 q[RT][kSteps] = {};
@@ -74,9 +99,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? 2 : 1) void kv16_decod
     // and every wait becomes one for all of them.
     const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
     const int tiles = (len + 15) / 16;
-    const int last_tile = 2 * u1 < tiles ? 2 * u1 - 1 : tiles - 1;
+    const int last_tile = u0 == u1 ? 0 : 2 * u1 < tiles ? 2 * u1 - 1 : tiles - 1;   // (a wave of WHOLE may have no keys: it reads the first)
     const int tiles_per_page = P / 16;
-    int tile = 2 * u0, col = tile / tiles_per_page, in_page = tile - col * tiles_per_page;   // of the table read
+    int tile = u0 == u1 ? 0 : 2 * u0, col = tile / tiles_per_page, in_page = tile - col * tiles_per_page;   // of the table read
     auto next_tile = [&](int& id, int& at) {
       id = table_entry(table + col);
       at = in_page;
@@ -236,6 +261,41 @@ __global__ __launch_bounds__(64 * kDecodeWaves, RT == 1 ? 2 : 1) void kv16_decod
       for (int k = u0; k < u1; ++k) step(std::integral_constant<bool, false>{}, k * kUnit);
     }
 
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float sum = lsum[rt];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        float* dst = lds_state[wave][c16];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < kChannelTiles / 4; ++y)
+            *reinterpret_cast<f32x4*>(dst + j * (HD / 4) + x * kChannelTiles + 4 * y) = f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
+        if (j == 0) dst[HD] = m[rt], dst[HD + 1] = l[rt][0], dst[HD + 2] = sum;
+      }
+      __syncthreads();
+      // a wave joins every eighth row, a lane its channels of it
+      for (int r = wave; r < rows; r += kWholeWaves) {
+        Merged<HD> all = {};
+        all.top = kNoMax;
+#pragma unroll
+        for (int v = 0; v < kWholeWaves; ++v) all.top = fmaxf(all.top, lds_state[v][r][HD]);
+#pragma unroll
+        for (int v = 0; v < kWholeWaves; ++v) {
+          const float* src = lds_state[v][r];
+          const float weight = __builtin_amdgcn_exp2f(src[HD] - all.top);
+          all.l += weight * src[HD + 1];
+          all.lsum += weight * src[HD + 2];
+#pragma unroll
+          for (int y = 0; y < HD / 64; ++y) all.o[y] += weight * src[lane * (HD / 64) + y];
+        }
+        const int i = r / a.rep;
+        write_merged<HD>(a, all, int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep, lane);
+      }
+      return;
+    }
     // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
     // each end, so two places per wave are enough
     const bool whole = u0 == 0 && u1 == int(units);
