@@ -55,35 +55,50 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_tile_kernel(Kv16Attention 
   const uint32_t heads = bt.num_kv_heads, splits = a.splits;
   const int h = blockIdx.x % heads;
   const int number = blockIdx.x / heads / splits, split = blockIdx.x / heads % splits;   // tile of the batch, part of its keys
-  int run_tiles = 0;
-  if (tid == 0) found[0] = -1;
-  for (int base = 0; base < bt.num_seqs; base += kThreads) {
-    const int b = base + tid;
-    const PagedSpan s = b < bt.num_seqs ? paged_span(bt, b) : PagedSpan{0, 0};
-    const int v = tile_count<WAVES>(a, s);
-    const int x = wave_prefix(v);
-    __syncthreads();
-    if (lane == 63) scratch[wave] = x;
-    __syncthreads();
-    int before = run_tiles;
-    for (int w = 0; w < WAVES; ++w) {
-      if (w < wave) before += scratch[w];
-      run_tiles += scratch[w];
+  int b, tile, first, n, all;
+  if (bt.num_seqs <= 64) {
+    // every wave has all sequences in its lanes: one read of them, and nobody waits for anybody
+    const PagedSpan s = lane < bt.num_seqs ? paged_span(bt, lane) : PagedSpan{0, 0};
+    const int tokens = lane < bt.num_seqs ? paged_len(bt, lane) : 0;
+    const int v = tile_count<WAVES>(a, s), upto = wave_prefix(v);
+    const uint64_t mask = __ballot(number >= upto - v && number < upto);
+    if (!mask) return;
+    b = __builtin_ctzll(mask);
+    tile = __builtin_amdgcn_readlane(upto, b) - 1 - number;   // the last rows of a sequence see most keys: first
+    first = __builtin_amdgcn_readlane(s.first, b);
+    n = __builtin_amdgcn_readlane(s.count, b);
+    all = __builtin_amdgcn_readlane(tokens, b);
+  } else {
+    int run_tiles = 0;
+    if (tid == 0) found[0] = -1;
+    for (int base = 0; base < bt.num_seqs; base += kThreads) {
+      const int mine = base + tid;
+      const int v = mine < bt.num_seqs ? tile_count<WAVES>(a, paged_span(bt, mine)) : 0;
+      const int x = wave_prefix(v);
+      __syncthreads();
+      if (lane == 63) scratch[wave] = x;
+      __syncthreads();
+      int upto = run_tiles + x;
+      for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) upto += scratch[w];
+        run_tiles += scratch[w];
+      }
+      if (number >= upto - v && number < upto) {
+        found[0] = mine;
+        found[1] = upto - 1 - number;
+      }
+      if (run_tiles > number) break;
     }
-    const int mine = before + x - v;
-    if (number >= mine && number < mine + v) {
-      found[0] = b;
-      found[1] = v - 1 - (number - mine);   // the last rows of a sequence see most keys: first
-    }
-    if (run_tiles > number) break;
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(found[0]);
+    if (b < 0) return;
+    tile = __builtin_amdgcn_readfirstlane(found[1]);
+    const PagedSpan span = paged_span(bt, b);
+    first = __builtin_amdgcn_readfirstlane(span.first);
+    n = __builtin_amdgcn_readfirstlane(span.count);
+    all = __builtin_amdgcn_readfirstlane(paged_len(bt, b));
   }
-  __syncthreads();
-  const int b = __builtin_amdgcn_readfirstlane(found[0]);
-  if (b < 0) return;
-  const int tile = __builtin_amdgcn_readfirstlane(found[1]);
-  const PagedSpan span = paged_span(bt, b);
-  const int first = __builtin_amdgcn_readfirstlane(span.first), n = __builtin_amdgcn_readfirstlane(span.count);
-  const int rows = n * a.rep, all = __builtin_amdgcn_readfirstlane(paged_len(bt, b)), len = paged_held(bt, all);
+  const int rows = n * a.rep, len = paged_held(bt, all);
   const PagedSeq seq = {first, n, len, all - n};
   const int r0 = tile * kTileRows;
   const int last_row = (r0 + kTileRows < rows ? r0 + kTileRows : rows) - 1;
