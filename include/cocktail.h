@@ -678,7 +678,7 @@ typedef struct cocktail_rotation {
  *   positions  DEVICE int32 [total]: positions of the rows for the rotation, or NULL: the tokens' numbers in their sequences
  *   q          DEVICE, 16-byte aligned, strides as k's, or NULL
  *   q_out      DEVICE [total][num_q_heads][D], 16-byte aligned; may be q itself where that is laid out the same; otherwise they must
- *              not overlap.  Rows of a sequence with a bad range are not written.
+ *              not overlap, nor q_out and k or v.  Rows of a sequence with a bad range are not written.
  *   num_q_heads  1 .. 65536 with q, else 0
  *
  * One launch.  Errors: EINVAL, EUNSUPPORTED (head_dim, rotary_dim), EALIGN, EHIP.
@@ -689,9 +689,10 @@ int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void* k, const 
 
 /*
  * Attention of the newest tokens of every sequence over its cached keys, themselves included (causal): rows, arguments, workspace and
- * what is left out as cocktail_fp4_attention; q and out are of the cache's dtype.
- * Products and sums in binary32; softmax weights rounded to the cache's dtype (fp16: as there; bf16: by 2^-8 of themselves), and
- * divided by the sum of the rounded ones.  A value of V that is not finite spoils its channel for all queries of its sequence and kv head in the
+ * what is left out as cocktail_fp4_attention; q and out are of the cache's dtype.  out may be q where that is laid out the same; otherwise
+ * they must not overlap.
+ * Products and sums in binary32; softmax weights rounded to the cache's dtype (fp16: as there; bf16: by 2^-8 of themselves), and divided by the
+ * sum of the rounded ones (calls with max_new * num_q_heads / num_kv_heads > 64: or of the others).  A value of V that is not finite spoils its channel for all queries of its sequence and kv head in the
  * call, also for those that do not see its token.  Calls on the same inputs agree bit for bit.  Up to four launches.
  * Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
  */

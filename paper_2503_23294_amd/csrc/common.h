@@ -10,6 +10,12 @@ namespace cocktail {
 // Records a message for cocktail_last_error() and returns `code`.
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
+// Whether two ranges of memory have bytes in common.
+inline bool overlap(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return bytes_a && bytes_b && x < y + uint64_t(bytes_b) && y < x + uint64_t(bytes_a);
+}
+
 // Validates the geometry common to all entry points.
 int check_shape(const cocktail_shape* s);
 

@@ -231,6 +231,12 @@ extern "C" int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void
     return fail(COCKTAIL_EINVAL, "without q there are no query heads and no q_out");
   }
   if (!total) return COCKTAIL_OK;
+  if (q) {
+    const int64_t written = 2 * total * num_q_heads * hd, rows = kv16_extent(cache, stride_t, stride_h, total, cache->num_kv_heads);
+    if ((q != q_out && overlap(q_out, written, q, kv16_extent(cache, q_stride_t, q_stride_h, total, num_q_heads))) || overlap(q_out, written, k, rows) ||
+        overlap(q_out, written, v, rows))
+      return fail(COCKTAIL_EINVAL, "q_out overlaps with the rows");
+  }
   Kv16Rows r = {};
   r.k = static_cast<const char*>(k);
   r.v = static_cast<const char*>(v);

@@ -7,6 +7,10 @@ namespace cocktail {
 int check_kv16_cache(const cocktail_kv16_cache* c);
 // Rows [total][heads] of the cache's dtype.
 int check_kv16_rows(const cocktail_kv16_cache* c, const void* x, const void* y, int64_t stride_t, int64_t stride_h, int64_t total, int heads);
+// Bytes from the first of such rows to the end of the last (total > 0).
+inline int64_t kv16_extent(const cocktail_kv16_cache* c, int64_t stride_t, int64_t stride_h, int64_t total, int heads) {
+  return 2 * ((total - 1) * stride_t + (heads - 1) * stride_h + c->head_dim);
+}
 // The batch of a call, with K's pool; checks `total` against `starts`.
 int check_kv16_batch(const cocktail_kv16_cache* c, int64_t total, const int32_t* starts, PagedBatch* a);
 

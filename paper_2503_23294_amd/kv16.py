@@ -93,7 +93,10 @@ def cocktail_kv16_append(cache: Kv16Cache, k: torch.Tensor, v: torch.Tensor, sta
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif q_out.dtype != q.dtype or q_out.shape != q.shape or q_out.device != dev or not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous tensor of q's type, shape and device")
-        src, dst = q.data_ptr(), q_out.data_ptr()
+        if total == 0:
+            heads = 0   # (no rows have no address)
+        else:
+            src, dst = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out is for q")
     check(lib().cocktail_kv16_append(cache.desc_ref, k.data_ptr(), v.data_ptr(), rows[1], rows[2], rows[0], _starts(cache, starts),

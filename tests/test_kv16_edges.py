@@ -1,6 +1,7 @@
 """The paged 16-bit cache and beam search where they can go wrong besides what test_kv16.py and test_beam.py look at: lengths and ranges, large pools,
 streams, threads, graphs, far tails of a softmax; and runs of the operators together, as they are used."""
 import contextlib
+import ctypes as C
 import math
 import threading
 
@@ -712,3 +713,83 @@ def test_the_bindings_refusals():
     out, lse = ck.cocktail_kv16_attention(B.cache, empty, starts)
     assert out.shape == (0, 2, 128) and lse.shape == (0, 2)
     assert ck.cocktail_beam_reorder(starts, []) == []
+
+
+# ---- memory that results share with arguments ----------------------------------------------------------------------------------------
+
+
+def test_results_that_overlap_with_arguments_are_refused():
+    L = _lib.lib()
+    pages = _lib.PageTableDesc(4096, 4096, 4096, 4096, 4, 8, 16, 32)
+    cache = C.byref(_lib.Kv16CacheDesc(pages, 1 << 30, 1 << 31, 2, 128, _lib.FP16, 0))
+    turn = C.byref(_lib.RotationDesc(4096, 128, 0, 1.0, 0))
+    k, v, q = 1 << 20, 2 << 20, 3 << 20                       # eight rows of two heads, and of four that lie a row of eight apart
+
+    def append(q_out, **more):
+        a = dict(q=q, st=1024, sh=128)
+        a.update(more)
+        return L.cocktail_kv16_append(cache, k, v, 256, 128, 8, 4096, turn, None, a["q"], 4, a["st"], a["sh"], q_out, None)
+
+    def attention(out, st=1024):
+        return L.cocktail_kv16_attention(cache, 4, q, st, 128, 8, 4096, 8, 0, 0.0, out, None, 4096, 1 << 40, None)
+    last = q + 2 * (7 * 1024 + 4 * 128) - 16                  # the last sixteen bytes of the queries
+    for call, where in [(append, x) for x in (q, q + 16, last, q - 2 * 8 * 512 + 16, k, k + 2 * 8 * 256 - 16, v, v - 2 * 8 * 512 + 16)] + \
+            [(attention, x) for x in (q, q + 16, last, q - 2 * 8 * 512 + 16)]:
+        assert call(where) == _lib.EINVAL, (call, where - q)
+        assert b"over" in L.cocktail_last_error() or b"in place" in L.cocktail_last_error()
+    assert append(k, q=k, st=512) == _lib.EINVAL and b"over" in L.cocktail_last_error()
+    assert attention(q + 512 * 2, st=512) == _lib.EINVAL and b"over" in L.cocktail_last_error()
+
+    def select(keep=4, **more):
+        a = dict(logits=1 << 20, scores=1 << 16, finished=1 << 17, source=1 << 12, token=2 << 12, score=3 << 12, out=4 << 12)
+        a.update(more)
+        return L.cocktail_beam_select(a["logits"], _lib.FP32, 128, 2, 4, 100, keep, a["scores"], a["finished"], 7, a["source"], a["token"], a["score"], a["out"],
+                                      1 << 28, 1 << 40, None)
+    logits_end = (1 << 20) + 4 * (7 * 128 + 100)
+    for more in (dict(source=2 << 12), dict(source=(2 << 12) + 28), dict(token=3 << 12), dict(score=(4 << 12) - 28), dict(out=(1 << 12) + 31),
+                 dict(source=1 << 20), dict(token=logits_end - 4), dict(score=(1 << 20) - 28), dict(out=logits_end - 1), dict(source=1 << 16),
+                 dict(score=(1 << 16) + 4), dict(score=1 << 17), dict(out=1 << 16), dict(out=(1 << 17) + 1), dict(token=(1 << 17) + 4),
+                 dict(score=1 << 16, finished=(1 << 16) + 4)):
+        assert select(**more) == _lib.EINVAL, more
+        assert b"overlap" in L.cocktail_last_error(), more
+
+
+def test_more_rows_than_a_launch_takes_are_refused():
+    L = _lib.lib()
+    pages = _lib.PageTableDesc(4096, 4096, 4096, 4096, 4096, 1, 16, 4096)
+    cache = C.byref(_lib.Kv16CacheDesc(pages, 1 << 40, 1 << 41, 1024, 128, _lib.FP16, 0))
+    assert L.cocktail_kv16_attention(cache, 1024, 1 << 42, 1024 * 128, 128, 1 << 18, 4096, 64, 0, 0.0, 1 << 43, None, 1 << 44, 1 << 44, None) == _lib.EINVAL
+    assert b"too many" in L.cocktail_last_error()
+
+
+@gpu
+def test_queries_of_no_tokens():
+    B = Batch([40, 20], 2, 128, 16, torch.float16)
+    empty = torch.zeros(0, 2, 128, device=B.dev, dtype=torch.float16)
+    starts = torch.zeros(3, dtype=torch.int32, device=B.dev)
+    before = [t.clone() for t in B.cache.pools]
+    for given in (None, empty.clone()):
+        got = ck.cocktail_kv16_append(B.cache, empty, empty, starts, _rotation(128), empty, q_out=given)
+        assert got.shape == (0, 2, 128) and (given is None or got is given)
+    assert all(torch.equal(t.view(torch.int16), u.view(torch.int16)) for t, u in zip(B.cache.pools, before))
+
+
+@gpu
+@pytest.mark.parametrize("lens, new, rep, max_len", [
+    ([300, 40, 7], [1, 1, 1], 4, 300),             # a workgroup per segment
+    ([9000, 40, 2500], [1, 1, 1], 4, 0),           # cut by tokens, states joined
+    ([700, 3000], [6, 9], 4, 0),
+    ([900, 300, 130], [900, 1, 130], 4, 0),        # both kernels
+    ([5000], [200], 2, 0),                         # many rows, their keys in parts
+    ([700, 700], [700, 700], 1, 700),
+])
+def test_attention_in_place(lens, new, rep, max_len):
+    B = Batch(lens, 2, 128, 16, torch.float16, seed=5)
+    for t in B.cache.pools:
+        t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(3)).to(t.dtype))
+    q = torch.randn(sum(new), 2 * rep, 128, generator=torch.Generator().manual_seed(4)).to(B.dev, torch.float16)
+    starts = torch.tensor([0, *np.cumsum(new)], dtype=torch.int32, device=B.dev)
+    want, lse = ck.cocktail_kv16_attention(B.cache, q, starts, max(new), max_len)
+    own = q.clone()
+    got, again = ck.cocktail_kv16_attention(B.cache, own, starts, max(new), max_len, out=own)
+    assert got is own and torch.equal(got, want) and torch.equal(again, lse)
