@@ -67,15 +67,17 @@ def cocktail_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int,
             _NEEDS.clear()
         need = _NEEDS[key] = int(size.value)
     if out is None:
-        source, token = (torch.empty((groups, keep), dtype=torch.int32, device=dev) for _ in range(2))
-        score, ended = torch.empty((groups, keep), dtype=torch.float32, device=dev), torch.empty((groups, keep), dtype=torch.bool, device=dev)
+        # (empty_strided: the call costs less on the host than the others that make a tensor, 1.3 of 1.7 us, and small steps are as long as the host takes)
+        size, strides, make = (groups, keep), (keep, 1), torch.empty_strided
+        source, token = make(size, strides, dtype=torch.int32, device=dev), make(size, strides, dtype=torch.int32, device=dev)
+        score, ended = make(size, strides, dtype=torch.float32, device=dev), make(size, strides, dtype=torch.bool, device=dev)
     else:
         source, token, score, ended = out
         _vector("source", source, (torch.int32,), groups * keep, dev)
         _vector("token", token, (torch.int32,), groups * keep, dev)
         _vector("score", score, (torch.float32,), groups * keep, dev)
         _vector("finished", ended, (torch.bool, torch.uint8), groups * keep, dev)
-    workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=dev)
     check(lib().cocktail_beam_select(logits.data_ptr(), _LOGITS[logits.dtype], logits.stride(0) if rows > 1 else vocab, groups, beams, vocab, keep,
                                      scores.data_ptr(), finished.data_ptr() if finished is not None else None, int(eos), source.data_ptr(),
                                      token.data_ptr(), score.data_ptr(), ended.data_ptr(), workspace.data_ptr(), need, handle))

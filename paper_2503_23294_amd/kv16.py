@@ -128,7 +128,7 @@ def cocktail_kv16_attention(cache: Kv16Cache, q: torch.Tensor, starts: Optional[
     elif out.dtype != q.dtype or out.shape != q.shape or out.device != dev or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's type, shape and device")
     if lse is None:
-        lse = q.new_empty((total, heads), dtype=torch.float32)
+        lse = torch.empty_strided((total, heads), (heads, 1), dtype=torch.float32, device=dev)
     elif lse.dtype != torch.float32 or tuple(lse.shape) != (total, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor [tokens, Hq]")
     first = _starts(cache, starts)
