@@ -24,6 +24,7 @@ namespace cocktail {
 // 55.6 us by operands alone, 47.4 by operands + 1, 49.4 by operands + 2).
 struct Fp4Cost {
   static constexpr uint32_t kMost = 5;
+  static constexpr bool kJoins = false;
   __device__ static int unit(const PagedAttention& a, const PagedSeq& s) { return decode_operands(a, s) + 1; }
 };
 

@@ -27,7 +27,7 @@ int check_attention(const cocktail_kv16_cache* c, int32_t num_q_heads, int64_t t
 
 // What a call launches, from what the host knows: bounds, no lengths.
 struct Split {
-  bool decode, whole, tiles;
+  bool decode, whole, tiles, joins;
   int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
   int64_t active;   // sequences that have queries at most
   size_t prefix_bytes, part_rows, tile_rows, bytes;
@@ -60,6 +60,10 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
     // channels 37.2, 33.0).
     s.whole = s.row_tiles == 1 && max_len * c->head_dim <= 65536;
     if (s.whole) workers = 0;
+    // Whether a workgroup's waves leave one state where all have parts of one segment: less to write and to read for the merge, which else takes (2 heads
+    // of one kv head, 84K tokens, 880 states) 20.7 us, joined 9.8; 7 of one, 4.7K 7.5, 5.8; 32 of 8, 20K 6.2, 5.1; but 8 of 8, 2K, 64 states 5.4, 5.7.  Of
+    // many rows states are large (verification behind 16K, 16 states of 48 rows: both kernels 74.8, 73.5).
+    s.joins = workers > (s.row_tiles > 1 ? 8 : 64) * s.active * c->num_kv_heads;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
   }
@@ -137,6 +141,7 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   a.rows = s.rows;
   a.workers = s.workers;
   a.splits = s.splits;
+  a.joins = s.joins;
   a.decode_rows = s.decode ? kDecodeRows : 0;
   char* w = static_cast<char*>(workspace);
   a.prefix = reinterpret_cast<int32_t*>(w);

@@ -5,7 +5,8 @@
 // (380 MB) 66 .. 68, 5.6 TB/s.
 //  * Work is cut by tokens, not by sequences: the units of 32 tokens of all (sequence, kv head) segments lie one behind the other, and every wave
 //    takes its share of that line, whatever the lengths are.  The numbering is made on the device from seq_lens, so that lengths can change
-//    under a captured graph.  A segment inside one share is finished by its wave, the others leave a partial state per wave.
+//    under a captured graph.  A segment inside one share is finished by its wave, the others leave a partial state per wave, or, where that would
+//    make many of them, per workgroup whose waves all have parts of it.
 //  * A lane's operands are whole pieces of memory.  Of K, lane (token c, quarter j) of sixteen tokens has channels 32 s + 8 j .. of its token, an operand of
 //    S^T = K Q^T per s.  Of V, lane (c, j) has channels [8 c, 8 c + 8) of tokens 4 j .. 4 j + 3 (64 channels: [4 c, 4 c + 4)), whole rows per
 //    load; pairs of tokens are put together by one byte permutation each, and are the operands of O^T = V^T P^T with the channels 8 c + t of product t.
@@ -23,6 +24,7 @@ namespace cocktail {
 // A unit's keys are read by one wave whatever its rows are, and the memory is what is waited for.
 struct Kv16Cost {
   static constexpr uint32_t kMost = 1;
+  static constexpr bool kJoins = true;
   __device__ static int unit(const PagedAttention&, const PagedSeq&) { return 1; }
 };
 
@@ -33,18 +35,18 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
   constexpr int kChannelTiles = HD / 16;
   extern __shared__ int32_t pre[];
   __shared__ int32_t lds_words[kWholeWaves + 1];
-  __shared__ float lds_state[WHOLE ? kWholeWaves : kDecodeWaves][16][HD + 4];   // sums, then (m, l, l unrounded) of WHOLE
+  __shared__ float lds_state[WHOLE ? kWholeWaves : kDecodeWaves][WHOLE ? 16 : 16 * RT][HD + 4];   // sums, then (m, l, l unrounded) of those that are joined here
   const PagedAttention& a = args.p;
   const PagedBatch& bt = a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j = lane >> 4;
   CostLine line = {};
   int w = 0;
-  uint32_t u = 0, end = 1;
-  bool stream = false;
+  uint32_t u = 0, end = 1, share = 0;
+  bool stream = false, joined = false;   // joined: the workgroup's waves have parts of one segment and leave one state
   if constexpr (!WHOLE) {
     line = make_line<Kv16Cost>(a, pre, lds_words);
-    const uint32_t share = cost_share<Kv16Cost>(line.total, a.workers);
+    share = cost_share<Kv16Cost>(line.total, a.workers);
     w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
     u = w * share;
     end = u + share < line.total ? u + share : line.total;
@@ -78,6 +80,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
       place = find_place(a, line, pre, u);
       const uint32_t units = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
       h = local / units;
+      if (a.joins) {
+        const uint32_t begin = u - (local - uint32_t(h) * units);
+        joined = workgroup_joins(begin, begin + units, blockIdx.x, share);
+      }
       u0 = local - uint32_t(h) * units, u1 = end - u < units - u0 ? u0 + (end - u) : units;
       u += u1 - u0;
     }
@@ -295,6 +301,45 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
         }
         const int i = r / a.rep;
         write_merged<HD>(a, all, int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep, lane);
+      }
+      return;
+    }
+    if (joined) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float sum = lsum[rt];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        float* dst = lds_state[wave][rt * 16 + c16];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < kChannelTiles / 4; ++y)
+            *reinterpret_cast<f32x4*>(dst + j * (HD / 4) + x * kChannelTiles + 4 * y) = f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
+        if (j == 0) *reinterpret_cast<f32x4*>(dst + HD) = f32x4{m[rt], l[rt][0], sum, 0.f};
+      }
+      __syncthreads();
+      constexpr int kLanes = HD / 4, kAtOnce = 64 / kLanes;   // lanes of a row, rows of a wave
+      const int at = lane % kLanes * 4;
+      const int64_t first_row = 2 * int64_t(w - wave) * a.rows;
+      for (int r = wave * kAtOnce + lane / kLanes; r < rows; r += kDecodeWaves * kAtOnce) {
+        f32x4 ml[kDecodeWaves], all = {}, sums = {};
+        float top = kNoMax;
+#pragma unroll
+        for (int v = 0; v < kDecodeWaves; ++v) ml[v] = *reinterpret_cast<const f32x4*>(lds_state[v][r] + HD), top = fmaxf(top, ml[v][0]);
+#pragma unroll
+        for (int v = 0; v < kDecodeWaves; ++v) {
+          const float weight = __builtin_amdgcn_exp2f(ml[v][0] - top);
+          all += weight * *reinterpret_cast<const f32x4*>(lds_state[v][r] + at);
+          sums += weight * ml[v];
+        }
+        *reinterpret_cast<f32x4*>(a.part_o + (first_row + r) * HD + at) = all;
+        if (at == 0) {
+          float* dst = a.part_ml + (first_row + r) * 3;
+          dst[0] = top;
+          dst[1] = sums[1];
+          dst[2] = sums[2];
+        }
       }
       return;
     }

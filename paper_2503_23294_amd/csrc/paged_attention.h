@@ -43,6 +43,7 @@ struct PagedAttention {
   float* part_o;                // their weighted sums
   float* tile_ml;
   float* tile_o;
+  int32_t joins;                // where COST::kJoins: workgroups of the decode kernel whose waves all have parts of one segment leave one state
 };
 
 // A sequence as one kernel sees it: its rows (none if they are the other kernel's), tokens that the table holds, tokens before the new ones.  Query i
@@ -70,6 +71,12 @@ template <class COST>
 __device__ __forceinline__ uint32_t cost_share(uint32_t cost, int workers) {
   const uint32_t n = (cost + uint32_t(workers) - 1) / uint32_t(workers);
   return n < COST::kMost ? COST::kMost : n;
+}
+
+// Whether all waves of a workgroup of the decode kernel have parts of the segment [begin, end) of the line and nothing else.
+__device__ __forceinline__ bool workgroup_joins(uint32_t begin, uint32_t end, uint32_t group, uint32_t share) {
+  const uint32_t all = kDecodeWaves * share;
+  return group * all >= begin && (group + 1) * all <= end;
 }
 
 __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
@@ -264,13 +271,11 @@ __device__ __forceinline__ int seq_of_row(const PagedBatch& bt, int t) {
   return b;
 }
 
-// Sum of a row's partial states: `parts` of them, the first at row `first_slot` of the arrays and the others at second_slot, second_slot + step ...
+// Sum of a row's partial states: `parts` of them, the k-th at row slot(k) of the arrays.
 // Wave `wave` of `waves` takes every waves-th; o: the lane's channels, l and lsum: whole sums (in every wave).
-template <int HD>
-__device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* po, int64_t first_slot, int64_t second_slot, int64_t step, int parts,
-                                                  int wave, int waves, int lane) {
+template <int HD, class Slot>
+__device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* po, Slot&& slot, int parts, int wave, int waves, int lane) {
   constexpr int kPer = HD / 64;
-  auto slot = [&](int k) -> int64_t { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
   Merged<HD> r = {};
   r.top = kNoMax;
   for (int k = lane; k < parts; k += 64) r.top = fmaxf(r.top, ml[slot(k) * 3]);
@@ -311,7 +316,7 @@ __device__ __forceinline__ Merged<HD> merge_parts(const float* ml, const float* 
   return r;
 }
 
-// Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves of its segment left, if there were several, and
+// Rows of the decode kernel, one per (sequence, new token, query head): joins what the waves (or workgroups) of its segment left, if there were several, and
 // writes rows without keys.  WAVES waves for a row, at least four to a workgroup.  Numbered by sequence, most_new tokens each, or, where most of those
 // would have no token, by new token (most_new 0), which is looked for among the sequences.
 template <class COST, int HD, int WAVES>
@@ -340,8 +345,22 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void merge_decode_ker
     const uint32_t w0 = u0 / share, w1 = u1 / share;
     if (w0 == w1) return;   // its wave has finished it
     const int in_state = i * a.rep + int(hq - h * a.rep);
-    r = merge_parts<HD>(a.part_ml, a.part_o, (2 * int64_t(w0) + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state, 2 * (int64_t(w0) + 1) * a.rows + in_state,
-                        2 * int64_t(a.rows), int(w1 - w0) + 1, wave, WAVES, lane);
+    const int64_t first = (2 * int64_t(w0) + (u0 == w0 * share ? 0 : 1)) * a.rows + in_state;
+    if (COST::kJoins && a.joins) {
+      // waves, then workgroups (workgroup_joins), then waves
+      const uint32_t all = kDecodeWaves * share, from = w0 / kDecodeWaves, to = w1 / kDecodeWaves + 1;
+      const uint32_t g0 = u0 == from * all ? from : from + 1, g1 = u0 + units * per_unit == to * all ? to : to - 1;
+      const int groups = g0 < g1 ? int(g1 - g0) : 0;
+      const int head = groups ? int(kDecodeWaves * g0 - w0) : int(w1 - w0) + 1, tail = groups ? int(w1 + 1 - kDecodeWaves * g1) : 0;
+      auto slot = [&](int k) -> int64_t {
+        const int of = k < head ? int(w0) + k : k < head + groups ? kDecodeWaves * (int(g0) + k - head) : kDecodeWaves * int(g1) + (k - head - groups);
+        return k == 0 ? first : 2 * int64_t(of) * a.rows + in_state;
+      };
+      r = merge_parts<HD>(a.part_ml, a.part_o, slot, head + groups + tail, wave, WAVES, lane);
+    } else {
+      const int64_t second = 2 * (int64_t(w0) + 1) * a.rows + in_state, step = 2 * int64_t(a.rows);
+      r = merge_parts<HD>(a.part_ml, a.part_o, [&](int k) -> int64_t { return k == 0 ? first : second + (k - 1) * step; }, int(w1 - w0) + 1, wave, WAVES, lane);
+    }
   }
   if constexpr (WAVES > 1) {
     if (wave) {
@@ -371,7 +390,7 @@ __global__ __launch_bounds__(256) void merge_tiles_kernel(PagedAttention a) {
   // not the rows of a sequence with a bad range, or of the decode kernel
   if (t < s.first || t >= s.first + s.count || s.count * a.rep <= a.decode_rows) return;
   const int64_t step = int64_t(bt.total) * heads;
-  write_merged<HD>(a, merge_parts<HD>(a.tile_ml, a.tile_o, row, row + step, step, a.splits, 0, 1, lane), row, lane);
+  write_merged<HD>(a, merge_parts<HD>(a.tile_ml, a.tile_o, [&](int k) -> int64_t { return row + k * step; }, a.splits, 0, 1, lane), row, lane);
 }
 
 }  // namespace cocktail

@@ -793,3 +793,27 @@ def test_attention_in_place(lens, new, rep, max_len):
     own = q.clone()
     got, again = ck.cocktail_kv16_attention(B.cache, own, starts, max(new), max_len, out=own)
     assert got is own and torch.equal(got, want) and torch.equal(again, lse)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("lens, new, kv_heads, rep, d, page", [
+    ([9001], [1], 1, 2, 128, 16),
+    ([33, 20011, 700], [1, 1, 1], 1, 3, 64, 16),
+    ([12345, 9000], [1, 1], 1, 8, 128, 48),
+    ([4096, 4192, 4096], [1, 1, 1], 1, 1, 128, 64),                # segments that end where workgroups do, and a wave before
+    ([5000, 0, 4097], [9, 3, 7], 2, 4, 128, 16),                   # states of 48 rows
+    ([2048], [16], 1, 4, 64, 16),                                  # of 64
+    ([3000, 777], [5, 6], 1, 5, 128, 32),                          # of 32
+    ([6000 if b in (3, 40, 99) else 10 for b in range(100)], [1 if b in (3, 40, 99) else 0 for b in range(100)], 1, 4, 128, 16),
+    ([30000, 40, 30016], [1, 1, 1], 4, 4, 64, 16),
+])
+def test_workgroups_that_leave_one_state(lens, new, kv_heads, rep, d, page, dtype):
+    B = Batch(lens, kv_heads, d, page, DTYPES[dtype], seed=len(lens), spread=4.0)
+    B.store_all()
+    q = B.query(new, rep)
+    for max_len in (max(lens), 0, max(lens) // 3):                 # (other numbers of workers)
+        out, lse = ck.cocktail_kv16_attention(B.cache, q, B.starts(new), max(new), max_len)
+        B.check(q, new, out, lse)
+        again, lse2 = ck.cocktail_kv16_attention(B.cache, q, B.starts(new), max(new), max_len)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
