@@ -27,7 +27,8 @@ int check_attention(const cocktail_kv16_cache* c, int32_t num_q_heads, int64_t t
 
 // What a call launches, from what the host knows: bounds, no lengths.
 struct Split {
-  bool decode, whole, tiles, joins;
+  bool decode, tiles, joins;
+  DecodeWork work;
   int rows, row_tiles, workers, tile_waves, tile_blocks, splits;
   int64_t active;   // sequences that have queries at most
   size_t prefix_bytes, part_rows, tile_rows, bytes;
@@ -57,13 +58,20 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
     s.workers = int(workers);
     // A workgroup per segment and no merge where contexts are short, of 128 KB of K at most: a compute unit reads no faster (8 heads of 128, 200
     // tokens: two launches 10.0 us, one 7.7; 1000: 11.5, 14.3; 32 sequences of 512: 19.7, 15.2, of 2048: 48.8, 46.5; 24 x 32 heads, 1024: 68.9, 77.8, of 64
-    // channels 37.2, 33.0).
-    s.whole = s.row_tiles == 1 && max_len * c->head_dim <= 65536;
-    if (s.whole) workers = 0;
+    // channels 37.2, 33.0).  Of more rows two launches cost more: 32 rows of 8 heads of 128, 200 and 512 tokens 12.2, 10.1 and 12.7, 12.6, 64 rows of 256 (32
+    // sequences, 8 heads) 36.3, 13 and 35, 17; where there are segments for half the compute units, also of longer contexts: 32 rows of 160, 1000 tokens 28.3,
+    // 20.1; 64 of 160, 1000, 2000 38, 23; 51, 34.
+    const int64_t segments = s.active * c->num_kv_heads;
+    const bool whole = max_len * c->head_dim <= 65536 * (segments < 128 || s.row_tiles == 1 ? 1 : s.row_tiles == 2 ? 2 : 3);
+    // Shares of workgroups from some 32 units of a workgroup on (64 rows, 512 segments of 2000, 4000 tokens 145, 109; 236, 185; 256 of 1000 44, 36; 8 of 20K: 30,
+    // 36; 40 rows, 64 of 300 .. 4000: 27.6, 32).
+    s.work = whole ? kWholeSegments : s.row_tiles > 1 && units >= 32 * kComputeUnits ? kGroupShares : kWaveShares;
+    if (s.work == kGroupShares) s.workers = int(workers /= kDecodeWaves);
+    if (whole) workers = 0;
     // Whether a workgroup's waves leave one state where all have parts of one segment: less to write and to read for the merge, which else takes (2 heads
     // of one kv head, 84K tokens, 880 states) 20.7 us, joined 9.8; 7 of one, 4.7K 7.5, 5.8; 32 of 8, 20K 6.2, 5.1; but 8 of 8, 2K, 64 states 5.4, 5.7.  Of
     // many rows states are large (verification behind 16K, 16 states of 48 rows: both kernels 74.8, 73.5).
-    s.joins = workers > (s.row_tiles > 1 ? 8 : 64) * s.active * c->num_kv_heads;
+    s.joins = s.work == kWaveShares && workers > (s.row_tiles > 1 ? 8 : 64) * segments;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;
     s.part_rows = 2 * size_t(workers) * s.rows;
   }
@@ -127,7 +135,7 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   if (!in_place && overlap(out, 2 * rows * hd, q, kv16_extent(cache, stride_t, stride_h, total, num_q_heads)))
     return fail(COCKTAIL_EINVAL, "out overlaps with q");
   // a wave of the merge per row, fewer than 2^32 threads (what check_attention and the numbers of sequences and heads leave keeps the other launches below that)
-  if (s.decode && !s.whole && int64_t(cache->pages.num_seqs) * s.rows * cache->num_kv_heads >= int64_t(1) << 26)
+  if (s.decode && s.work != kWholeSegments && int64_t(cache->pages.num_seqs) * s.rows * cache->num_kv_heads >= int64_t(1) << 26)
     return fail(COCKTAIL_EINVAL, "%d sequences of %d heads with up to %d rows each are too many for one call", cache->pages.num_seqs, cache->num_kv_heads, s.rows);
   a.batch.max_new = max_new;
   args.v_pool = static_cast<const char*>(cache->v);
@@ -158,22 +166,28 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (s.decode) {
-    static const Kernel kernels[2][2][4] = {
-        {{kv16_decode_kernel<64, false, 1, false>, kv16_decode_kernel<64, false, 2, false>, kv16_decode_kernel<64, false, 3, false>, kv16_decode_kernel<64, false, 4, false>},
-         {kv16_decode_kernel<64, true, 1, false>, kv16_decode_kernel<64, true, 2, false>, kv16_decode_kernel<64, true, 3, false>, kv16_decode_kernel<64, true, 4, false>}},
-        {{kv16_decode_kernel<128, false, 1, false>, kv16_decode_kernel<128, false, 2, false>, kv16_decode_kernel<128, false, 3, false>, kv16_decode_kernel<128, false, 4, false>},
-         {kv16_decode_kernel<128, true, 1, false>, kv16_decode_kernel<128, true, 2, false>, kv16_decode_kernel<128, true, 3, false>, kv16_decode_kernel<128, true, 4, false>}}};
-    static const Kernel whole[2][2] = {{kv16_decode_kernel<64, false, 1, true>, kv16_decode_kernel<64, true, 1, true>},
-                                       {kv16_decode_kernel<128, false, 1, true>, kv16_decode_kernel<128, true, 1, true>}};
-    if (s.whole) e = launch(whole[hd == 128][a.bf16], dim3(uint32_t(s.active * cache->num_kv_heads)), dim3(64 * kWholeWaves), st, args);
-    else e = launch_lds(kernels[hd == 128][a.bf16][s.row_tiles - 1], dim3(s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st, args);
+    // by head_dim, type and operands of rows
+#define COCKTAIL_ROWS(hd, bf16, work, one) {one, kv16_decode_kernel<hd, bf16, 2, work>, kv16_decode_kernel<hd, bf16, 3, work>, kv16_decode_kernel<hd, bf16, 4, work>}
+#define COCKTAIL_ONE(hd, bf16, work) COCKTAIL_ROWS(hd, bf16, work, (kv16_decode_kernel<hd, bf16, 1, work>))
+    static const Kernel kernels[3][2][2][4] = {
+        {{COCKTAIL_ONE(64, false, kWaveShares), COCKTAIL_ONE(64, true, kWaveShares)}, {COCKTAIL_ONE(128, false, kWaveShares), COCKTAIL_ONE(128, true, kWaveShares)}},
+        {{COCKTAIL_ROWS(64, false, kGroupShares, nullptr), COCKTAIL_ROWS(64, true, kGroupShares, nullptr)},
+         {COCKTAIL_ROWS(128, false, kGroupShares, nullptr), COCKTAIL_ROWS(128, true, kGroupShares, nullptr)}},
+        {{COCKTAIL_ONE(64, false, kWholeSegments), COCKTAIL_ONE(64, true, kWholeSegments)}, {COCKTAIL_ONE(128, false, kWholeSegments), COCKTAIL_ONE(128, true, kWholeSegments)}}};
+#undef COCKTAIL_ONE
+#undef COCKTAIL_ROWS
+    const Kernel kernel = kernels[s.work][hd == 128][a.bf16][s.row_tiles - 1];
+    if (s.work == kWholeSegments) e = launch(kernel, dim3(uint32_t(s.active * cache->num_kv_heads)), dim3(64 * whole_waves(s.row_tiles)), st, args);
+    else
+      e = launch_lds(kernel, dim3(s.work == kGroupShares ? s.workers : s.workers / kDecodeWaves), dim3(64 * kDecodeWaves), (a.batch.num_seqs + 1) * sizeof(int32_t), st,
+                     args);
   }
   if (e == hipSuccess && s.tiles) {
     static const Kernel kernels[2][2][2] = {{{kv16_tile_kernel<64, false, 4>, kv16_tile_kernel<64, false, 8>}, {kv16_tile_kernel<64, true, 4>, kv16_tile_kernel<64, true, 8>}},
                                             {{kv16_tile_kernel<128, false, 4>, kv16_tile_kernel<128, false, 8>}, {kv16_tile_kernel<128, true, 4>, kv16_tile_kernel<128, true, 8>}}};
     e = launch(kernels[hd == 128][a.bf16][s.tile_waves == 8], dim3(uint32_t(s.tile_blocks) * s.splits * cache->num_kv_heads), dim3(64 * s.tile_waves), st, args);
   }
-  if (e == hipSuccess && s.decode && !s.whole) {
+  if (e == hipSuccess && s.decode && s.work != kWholeSegments) {
     int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
     const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;

@@ -28,14 +28,23 @@ struct Kv16Cost {
   __device__ static int unit(const PagedAttention&, const PagedSeq&) { return 1; }
 };
 
-// WHOLE: a workgroup of kWholeWaves waves has one segment and shares it out among them, their states are joined in LDS: one launch, for short contexts.
-template <int HD, bool BF16, int RT, bool WHOLE>
-__global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
+// Who takes what of the line:
+//  kWaveShares: every wave a share of its own.
+//  kGroupShares: every workgroup, whose waves share each part of a segment in it and join their states in LDS.  Where there are many rows and many keys: a
+//    state of 64 rows is as large as 128 keys, and this way there are a quarter as many; but a second part in a share costs 6 us.
+//  kWholeSegments: a workgroup has one segment, shared out in the same way: one launch, for short contexts.  (The states have to fit into LDS: eight waves
+//    for up to 32 rows, else four.)
+enum DecodeWork { kWaveShares, kGroupShares, kWholeSegments };
+constexpr int whole_waves(int row_tiles) { return row_tiles <= 2 ? kWholeWaves : kDecodeWaves; }
+template <int HD, bool BF16, int RT, DecodeWork WORK>
+__global__ __launch_bounds__(64 * (WORK == kWholeSegments ? whole_waves(RT) : kDecodeWaves), RT == 1 ? 2 : 1) void kv16_decode_kernel(Kv16Attention args) {
+  constexpr bool kWhole = WORK == kWholeSegments, kShared = WORK != kWaveShares;
   constexpr int kSteps = HD / 32;           // products per 16 tokens of S
   constexpr int kChannelTiles = HD / 16;
+  constexpr int kWaves = kWhole ? whole_waves(RT) : kDecodeWaves;
   extern __shared__ int32_t pre[];
   __shared__ int32_t lds_words[kWholeWaves + 1];
-  __shared__ float lds_state[WHOLE ? kWholeWaves : kDecodeWaves][WHOLE ? 16 : 16 * RT][HD + 4];   // sums, then (m, l, l unrounded) of those that are joined here
+  __shared__ float lds_state[kWaves][16 * RT][HD + 4];   // sums, then (m, l, l unrounded) of those that are joined here
   const PagedAttention& a = args.p;
   const PagedBatch& bt = a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -44,10 +53,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
   int w = 0;
   uint32_t u = 0, end = 1, share = 0;
   bool stream = false, joined = false;   // joined: the workgroup's waves have parts of one segment and leave one state
-  if constexpr (!WHOLE) {
+  if constexpr (!kWhole) {
     line = make_line<Kv16Cost>(a, pre, lds_words);
     share = cost_share<Kv16Cost>(line.total, a.workers);
-    w = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+    w = kShared ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
     u = w * share;
     end = u + share < line.total ? u + share : line.total;
     if (u >= end) return;
@@ -62,33 +71,33 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
   bool first_segment = true;
   while (u < end) {
     CostPlace place;
-    int h, u0, u1;
-    if constexpr (WHOLE) {
+    int h, p0, p1;   // the part of the segment
+    if constexpr (kWhole) {
       const int number = blockIdx.x / bt.num_kv_heads;
       h = blockIdx.x - number * bt.num_kv_heads;
       // more sequences than rows: the workgroups are for those that have any
-      place.b = bt.num_seqs > bt.total ? nth_active(a, number, lds_words) : number;
+      place.b = bt.num_seqs > bt.total ? nth_active<kWaves>(a, number, lds_words) : number;
       if (place.b < 0) return;
       place.seq = of_lane(decode_seq(a, place.b), 0);
       if (place.seq.n == 0) return;
       const uint32_t units = decode_units(place.seq);
       place.cost = units;
-      u0 = units * wave / kWholeWaves;
-      u1 = units * (wave + 1) / kWholeWaves;
+      p0 = 0, p1 = units;
       u = end;
     } else {
       place = find_place(a, line, pre, u);
       const uint32_t units = place.cost, local = u - uint32_t(place.before) * uint32_t(bt.num_kv_heads);
       h = local / units;
-      if (a.joins) {
+      if (!kShared && a.joins) {
         const uint32_t begin = u - (local - uint32_t(h) * units);
         joined = workgroup_joins(begin, begin + units, blockIdx.x, share);
       }
-      u0 = local - uint32_t(h) * units, u1 = end - u < units - u0 ? u0 + (end - u) : units;
-      u += u1 - u0;
+      p0 = local - uint32_t(h) * units, p1 = end - u < units - p0 ? p0 + (end - u) : units;
+      u += p1 - p0;
     }
     const int b = place.b, len = place.seq.len, rows = place.seq.n * a.rep;
     const uint32_t units = place.cost;
+    const int u0 = kShared ? p0 + (p1 - p0) * wave / kWaves : p0, u1 = kShared ? p0 + (p1 - p0) * (wave + 1) / kWaves : p1;   // (what is a product fits: 2^26 units, 8 waves)
 
     // the queries: lane (row c16, quarter j) has the channels that its K pieces have
     u32x4 q[RT][kSteps] = {};
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
     // and every wait becomes one for all of them.
     const int32_t* table = bt.table + int64_t(b) * bt.table_stride;
     const int tiles = (len + 15) / 16;
-    const int last_tile = u0 == u1 ? 0 : 2 * u1 < tiles ? 2 * u1 - 1 : tiles - 1;   // (a wave of WHOLE may have no keys: it reads the first)
+    const int last_tile = u0 == u1 ? 0 : 2 * u1 < tiles ? 2 * u1 - 1 : tiles - 1;   // (a wave of those that share may have no keys: it reads the first)
     const int tiles_per_page = P / 16;
     int tile = u0 == u1 ? 0 : 2 * u0, col = tile / tiles_per_page, in_page = tile - col * tiles_per_page;   // of the table read
     auto next_tile = [&](int& id, int& at) {
@@ -269,42 +278,11 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
       for (int k = u0; k < u1; ++k) step(std::integral_constant<bool, false>{}, k * kUnit);
     }
 
-    if constexpr (WHOLE) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float sum = lsum[rt];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        float* dst = lds_state[wave][c16];
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int y = 0; y < kChannelTiles / 4; ++y)
-            *reinterpret_cast<f32x4*>(dst + j * (HD / 4) + x * kChannelTiles + 4 * y) = f32x4{o[rt][4 * y][x], o[rt][4 * y + 1][x], o[rt][4 * y + 2][x], o[rt][4 * y + 3][x]};
-        if (j == 0) dst[HD] = m[rt], dst[HD + 1] = l[rt][0], dst[HD + 2] = sum;
-      }
-      __syncthreads();
-      // a wave joins every eighth row, a lane its channels of it
-      for (int r = wave; r < rows; r += kWholeWaves) {
-        Merged<HD> all = {};
-        all.top = kNoMax;
-#pragma unroll
-        for (int v = 0; v < kWholeWaves; ++v) all.top = fmaxf(all.top, lds_state[v][r][HD]);
-#pragma unroll
-        for (int v = 0; v < kWholeWaves; ++v) {
-          const float* src = lds_state[v][r];
-          const float weight = __builtin_amdgcn_exp2f(src[HD] - all.top);
-          all.l += weight * src[HD + 1];
-          all.lsum += weight * src[HD + 2];
-#pragma unroll
-          for (int y = 0; y < HD / 64; ++y) all.o[y] += weight * src[lane * (HD / 64) + y];
-        }
-        const int i = r / a.rep;
-        write_merged<HD>(a, all, int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep, lane);
-      }
-      return;
-    }
-    if (joined) {
+    // whole segments are finished here, others leave their state: a wave (or workgroup) has at most one that ends behind its share (or begins before
+    // it) at each end, so two places are enough
+    const bool whole = p0 == 0 && p1 == int(units);
+    const int64_t slot = 2 * int64_t(w) + (first_segment ? 0 : 1);
+    if (kShared || joined) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float sum = lsum[rt];
@@ -319,34 +297,44 @@ __global__ __launch_bounds__(64 * (WHOLE ? kWholeWaves : kDecodeWaves), RT == 1 
         if (j == 0) *reinterpret_cast<f32x4*>(dst + HD) = f32x4{m[rt], l[rt][0], sum, 0.f};
       }
       __syncthreads();
-      constexpr int kLanes = HD / 4, kAtOnce = 64 / kLanes;   // lanes of a row, rows of a wave
+      // a wave joins a row or more at a time, a lane four channels
+      constexpr int kLanes = HD / 4, kAtOnce = 64 / kLanes;
       const int at = lane % kLanes * 4;
-      const int64_t first_row = 2 * int64_t(w - wave) * a.rows;
-      for (int r = wave * kAtOnce + lane / kLanes; r < rows; r += kDecodeWaves * kAtOnce) {
-        f32x4 ml[kDecodeWaves], all = {}, sums = {};
+      const int64_t first_state = (kShared ? slot : 2 * int64_t(w - wave)) * a.rows;
+#pragma unroll(kShared ? 2 : 1)
+      for (int r = wave * kAtOnce + lane / kLanes; r < rows; r += kWaves * kAtOnce) {
+        f32x4 ml[kWaves], all = {}, sums = {};
         float top = kNoMax;
 #pragma unroll
-        for (int v = 0; v < kDecodeWaves; ++v) ml[v] = *reinterpret_cast<const f32x4*>(lds_state[v][r] + HD), top = fmaxf(top, ml[v][0]);
+        for (int v = 0; v < kWaves; ++v) ml[v] = *reinterpret_cast<const f32x4*>(lds_state[v][r] + HD), top = fmaxf(top, ml[v][0]);
 #pragma unroll
-        for (int v = 0; v < kDecodeWaves; ++v) {
+        for (int v = 0; v < kWaves; ++v) {
           const float weight = __builtin_amdgcn_exp2f(ml[v][0] - top);
           all += weight * *reinterpret_cast<const f32x4*>(lds_state[v][r] + at);
           sums += weight * ml[v];
         }
-        *reinterpret_cast<f32x4*>(a.part_o + (first_row + r) * HD + at) = all;
-        if (at == 0) {
-          float* dst = a.part_ml + (first_row + r) * 3;
-          dst[0] = top;
-          dst[1] = sums[1];
-          dst[2] = sums[2];
+        if (kWhole || (kShared && whole)) {
+          const int i = r / a.rep;
+          const int64_t row = int64_t(place.seq.first + i) * bt.num_kv_heads * a.rep + h * a.rep + r - i * a.rep;
+          const float inv = sums[1] == 0.f ? 0.f : 1.f / sums[1];
+          *reinterpret_cast<u32x2*>(a.out + row * (2 * HD) + at * 2) = u32x2{pack_out(all[0] * inv, all[1] * inv, BF16), pack_out(all[2] * inv, all[3] * inv, BF16)};
+          if (a.lse && at == 0) a.lse[row] = sums[1] == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sums[2])) * kLn2;
+        } else {
+          const int64_t state = first_state + r;
+          *reinterpret_cast<f32x4*>(a.part_o + state * HD + at) = all;
+          if (at == 0) {
+            float* dst = a.part_ml + state * 3;
+            dst[0] = top;
+            dst[1] = sums[1];
+            dst[2] = sums[2];
+          }
         }
       }
-      return;
+      if constexpr (WORK != kGroupShares) return;
+      __syncthreads();   // the next part's states take the place of these
+      first_segment = false;
+      continue;
     }
-    // whole segments are finished here, others leave their state: a wave has at most one that ends behind its share (or begins before it) at
-    // each end, so two places per wave are enough
-    const bool whole = u0 == 0 && u1 == int(units);
-    const int64_t slot = 2 * int64_t(w) + (first_segment ? 0 : 1);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float sum = lsum[rt];

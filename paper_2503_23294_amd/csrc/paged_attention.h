@@ -211,12 +211,13 @@ __device__ __forceinline__ CostPlace find_place(const PagedAttention& a, const C
 
 constexpr int kWholeWaves = 8;          // waves that share a segment where contexts are short
 
-// The number-th sequence that has queries for this kernel, or -1; for a workgroup of kWholeWaves waves, `lds`: kWholeWaves + 1 words.
+// The number-th sequence that has queries for this kernel, or -1; for a workgroup of WAVES waves, `lds`: WAVES + 1 words.
+template <int WAVES = kWholeWaves>
 __device__ __forceinline__ int nth_active(const PagedAttention& a, int number, int32_t* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int run = 0;
-  if (threadIdx.x == 0) lds[kWholeWaves] = -1;
-  for (int base = 0; base < a.batch.num_seqs && run <= number; base += 64 * kWholeWaves) {
+  if (threadIdx.x == 0) lds[WAVES] = -1;
+  for (int base = 0; base < a.batch.num_seqs && run <= number; base += 64 * WAVES) {
     const int b = base + int(threadIdx.x);
     const bool active = b < a.batch.num_seqs && decode_seq(a, b).n > 0;
     const uint64_t mask = __ballot(active);
@@ -224,14 +225,14 @@ __device__ __forceinline__ int nth_active(const PagedAttention& a, int number, i
     if (lane == 0) lds[wave] = __builtin_popcountll(mask);
     __syncthreads();
     int before = run;
-    for (int w = 0; w < kWholeWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w < wave) before += lds[w];
       run += lds[w];
     }
-    if (active && before + __builtin_popcountll(mask & ((uint64_t(1) << lane) - 1)) == number) lds[kWholeWaves] = b;
+    if (active && before + __builtin_popcountll(mask & ((uint64_t(1) << lane) - 1)) == number) lds[WAVES] = b;
   }
   __syncthreads();
-  return __builtin_amdgcn_readfirstlane(lds[kWholeWaves]);
+  return __builtin_amdgcn_readfirstlane(lds[WAVES]);
 }
 
 // The number-th longest of up to 64 sequences, for a workgroup of kWholeWaves waves: a lane has a sequence, a wave counts which of its share of them are

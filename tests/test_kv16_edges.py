@@ -817,3 +817,30 @@ def test_workgroups_that_leave_one_state(lens, new, kv_heads, rep, d, page, dtyp
         B.check(q, new, out, lse)
         again, lse2 = ck.cocktail_kv16_attention(B.cache, q, B.starts(new), max(new), max_len)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("num_seqs, kv_heads, rep, new, longest, d, page", [
+    (40, 2, 8, 8, 900, 128, 16),         # 64 rows
+    (40, 1, 8, 6, 1300, 128, 48),        # 48
+    (33, 4, 5, 6, 500, 64, 16),          # 30
+    (130, 1, 16, 4, 300, 64, 32),        # more sequences than lanes
+    (70, 2, 12, 2, 700, 128, 16),        # 24
+    (3, 8, 16, 3, 4000, 128, 16),
+    (600, 1, 3, 7, 60, 64, 16),
+])
+def test_several_queries_of_many_sequences(num_seqs, kv_heads, rep, new, longest, d, page, dtype):
+    rng = np.random.default_rng(num_seqs)
+    lens = [int(t) for t in rng.integers(0, longest + 1, num_seqs)]
+    lens[0], lens[-1] = longest, 0
+    count = [int(n) for n in rng.integers(0, new + 1, num_seqs)]
+    count[0] = count[-1] = new
+    B = Batch(lens, kv_heads, d, page, DTYPES[dtype], seed=num_seqs, spread=4.0)
+    B.store_all()
+    q = B.query(count, rep)
+    for max_len in (longest, 0, 1, 20000):                         # a workgroup per segment, shares of waves or of workgroups
+        out, lse = ck.cocktail_kv16_attention(B.cache, q, B.starts(count), new, max_len)
+        B.check(q, count, out, lse)
+        again, lse2 = ck.cocktail_kv16_attention(B.cache, q, B.starts(count), new, max_len)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
