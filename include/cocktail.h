@@ -694,6 +694,7 @@ int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void* k, const 
  * Products and sums in binary32; softmax weights rounded to the cache's dtype (fp16: as there; bf16: by 2^-8 of themselves), and divided by the
  * sum of the rounded ones (calls with max_new * num_q_heads / num_kv_heads > 64: or of the others).  A value of V that is not finite spoils its channel for all queries of its sequence and kv head in the
  * call, also for those that do not see its token.  Calls on the same inputs agree bit for bit.  Up to four launches.
+ * Batches with sequences of up to 64 rows (queries times num_q_heads / num_kv_heads): num_seqs * num_kv_heads * min(64, most rows) below 2^26.
  * Errors: EINVAL, EUNSUPPORTED, EALIGN, ENOSPACE, EHIP.
  */
 int cocktail_kv16_attention_workspace(const cocktail_kv16_cache* cache, int32_t num_q_heads, int64_t total, int32_t max_new,

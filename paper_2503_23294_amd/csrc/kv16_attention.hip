@@ -134,8 +134,9 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   const bool in_place = q == out && (num_q_heads == 1 || stride_h == hd) && (total == 1 || stride_t == int64_t(num_q_heads) * hd);
   if (!in_place && overlap(out, 2 * rows * hd, q, kv16_extent(cache, stride_t, stride_h, total, num_q_heads)))
     return fail(COCKTAIL_EINVAL, "out overlaps with q");
-  // a wave of the merge per row, fewer than 2^32 threads (what check_attention and the numbers of sequences and heads leave keeps the other launches below that)
-  if (s.decode && s.work != kWholeSegments && int64_t(cache->pages.num_seqs) * s.rows * cache->num_kv_heads >= int64_t(1) << 26)
+  // A wave of the merge per row, fewer than 2^32 threads; refused also where the call needs no merge, so that the limit does not hang on max_len.  (What
+  // check_attention and the numbers of sequences and heads leave keeps the other launches below that.)
+  if (s.decode && int64_t(cache->pages.num_seqs) * s.rows * cache->num_kv_heads >= int64_t(1) << 26)
     return fail(COCKTAIL_EINVAL, "%d sequences of %d heads with up to %d rows each are too many for one call", cache->pages.num_seqs, cache->num_kv_heads, s.rows);
   a.batch.max_new = max_new;
   args.v_pool = static_cast<const char*>(cache->v);

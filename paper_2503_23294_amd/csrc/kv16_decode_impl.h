@@ -301,7 +301,7 @@ __global__ __launch_bounds__(64 * (WORK == kWholeSegments ? whole_waves(RT) : kD
       constexpr int kLanes = HD / 4, kAtOnce = 64 / kLanes;
       const int at = lane % kLanes * 4;
       const int64_t first_state = (kShared ? slot : 2 * int64_t(w - wave)) * a.rows;
-#pragma unroll(kShared ? 2 : 1)
+#pragma unroll kShared ? 2 : 1
       for (int r = wave * kAtOnce + lane / kLanes; r < rows; r += kWaves * kAtOnce) {
         f32x4 ml[kWaves], all = {}, sums = {};
         float top = kNoMax;
