@@ -782,6 +782,8 @@ def test_queries_of_no_tokens():
     ([900, 300, 130], [900, 1, 130], 4, 0),        # both kernels
     ([5000], [200], 2, 0),                         # many rows, their keys in parts
     ([700, 700], [700, 700], 1, 700),
+    ([900, 31, 2000, 64, 500, 1, 333, 1200], [9] * 8, 4, 0),     # shares of workgroups
+    ([100, 31, 200, 64], [9] * 4, 4, 200),         # a workgroup per segment, 36 rows
 ])
 def test_attention_in_place(lens, new, rep, max_len):
     B = Batch(lens, 2, 128, 16, torch.float16, seed=5)
