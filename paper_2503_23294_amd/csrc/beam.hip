@@ -202,21 +202,23 @@ struct Logits {
   }
 };
 
-// A wave's tile: eight logits a lane from a multiple of eight (counted from the first aligned address at or before the row), those outside of the row as
-// none.  (Nothing is made of what a tile within the row brings, so that nobody waits for it here.)
+// A wave's tile: eight logits a lane from a multiple of eight, counted from the row's first, those behind its end as none.  (Nothing is made of what a tile
+// within the row brings, so that nobody waits for it here.)  Rows begin at any address of their elements, and the words of sixteen bytes with them: which
+// logits are summed together must not depend on where a row lies, or equal rows would have different sums.  It costs nothing: both launches for 64 rows
+// of 65001 in bf16 18.1 us, 17.6 with rows that begin at whole words, 17.8 either way with words counted from aligned addresses.
 template <class T>
-__device__ __forceinline__ void load_logits(const T* row, int skip, int vocab, int64_t tile, int lane, Logits<T>& x) {
+__device__ __forceinline__ void load_logits(const T* row, int vocab, int64_t tile, int lane, Logits<T>& x) {
   constexpr int kWords = sizeof(T) * kPerLane / 16;
-  const int64_t first = tile * (64 * kPerLane) - skip;
-  const T* src = row + first + lane * kPerLane;
-  if (first >= 0 && first + 64 * kPerLane <= vocab) {
+  typedef u32x4 Words __attribute__((aligned(2)));   // (the hardware takes them from any address)
+  const int64_t first = tile * (64 * kPerLane), at = first + lane * kPerLane;
+  const T* src = row + at;
+  if (first + 64 * kPerLane <= vocab) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) x.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src) + i);
+    for (int i = 0; i < kWords; ++i) x.w[i] = __builtin_nontemporal_load(reinterpret_cast<const Words*>(src) + i);
   } else {
-    const int64_t at = first + lane * kPerLane;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-      const bool there = at + i >= 0 && at + i < vocab;
+      const bool there = at + i < vocab;
       if constexpr (sizeof(T) == 4) {
         x.w[i >> 2][i & 3] = there ? __builtin_bit_cast(uint32_t, src[i]) : 0xff800000u;
       } else {
@@ -240,11 +242,8 @@ __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSele
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   const T* src = static_cast<const T*>(a.logits) + int64_t(row) * a.stride_row;
-  // sixteen-byte words lie at aligned addresses
-  const int skip = int(reinterpret_cast<uintptr_t>(src) % (sizeof(T) * kPerLane) / sizeof(T));
-  const int64_t words = (int64_t(skip) + a.vocab + kPerLane - 1) / kPerLane;
-  // of 64 words each; the piece's, then the wave's
-  const int64_t tiles = (words + 63) / 64;
+  // the piece's, then the wave's
+  const int64_t tiles = (int64_t(a.vocab) + 64 * kPerLane - 1) / (64 * kPerLane);
   const int64_t tile0 = tiles * piece / a.pieces, tile1 = tiles * (piece + 1) / a.pieces;
 
   Best<LogitKey> best(buffers[wave], a.keep, lane);
@@ -258,14 +257,14 @@ __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSele
   int done = 0;
 #pragma unroll
   for (int d = 0; d < 2; ++d)
-    if (tile + d * kSelectWaves < tile1) load_logits(src, skip, a.vocab, tile + d * kSelectWaves, lane, next[d]);
+    if (tile + d * kSelectWaves < tile1) load_logits(src, a.vocab, tile + d * kSelectWaves, lane, next[d]);
   if (!reads_logits(a, row)) return;   // (behind the first loads, which it need not wait for)
   __syncthreads();
   auto step = [&](Logits<T>& own) __attribute__((always_inline)) {
     float x[kPerLane];
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) x[i] = own.at(i);
-    if (tile + 2 * kSelectWaves < tile1) load_logits(src, skip, a.vocab, tile + 2 * kSelectWaves, lane, own);
+    if (tile + 2 * kSelectWaves < tile1) load_logits(src, a.vocab, tile + 2 * kSelectWaves, lane, own);
     float most = most_of(x);
     auto raise = [&]() __attribute__((always_inline)) {
       const float raised = fmaxf(ref, fminf(from_ordered(wave_most(most == most && most > -__builtin_inff() ? ordered(most) : ordered(-FLT_MAX))), FLT_MAX));
@@ -300,7 +299,7 @@ __global__ __launch_bounds__(64 * kSelectWaves) void beam_pieces_kernel(BeamSele
     const uint32_t shared = lds_border;
     if (shared) border = fmaxf(border, from_ordered(shared));
     if (__any(most >= border)) {
-      const int64_t at = (tile * 64 + lane) * kPerLane - skip;
+      const int64_t at = (tile * 64 + lane) * kPerLane;
 #pragma unroll
       for (int i = 0; i < kPerLane; ++i) {
         if (!__any(x[i] >= border)) continue;
