@@ -690,7 +690,7 @@ int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void* k, const 
 /*
  * Attention of the newest tokens of every sequence over its cached keys, themselves included (causal): rows, arguments, workspace and
  * what is left out as cocktail_fp4_attention; q and out are of the cache's dtype.  out may be q where that is laid out the same; otherwise
- * they must not overlap.
+ * out, lse and workspace must not overlap with each other or with anything that the call reads.
  * Products and sums in binary32; softmax weights rounded to the cache's dtype (fp16: as there; bf16: by 2^-8 of themselves), and divided by the
  * sum of the rounded ones (calls with max_new * num_q_heads / num_kv_heads > 64: or of the others).  A value of V that is not finite spoils its channel for all queries of its sequence and kv head in the
  * call, also for those that do not see its token.  Calls on the same inputs agree bit for bit.  Up to four launches.

@@ -16,6 +16,22 @@ inline bool overlap(const void* a, int64_t bytes_a, const void* b, int64_t bytes
   return bytes_a && bytes_b && x < y + uint64_t(bytes_b) && y < x + uint64_t(bytes_a);
 }
 
+// Memory that a call reads or writes; whether a range that is written shares bytes with another one of those, or with one that is read.
+struct MemoryRange {
+  const void* at;
+  int64_t bytes;
+};
+template <int W, int R>
+inline bool overlap(const MemoryRange (&written)[W], const MemoryRange (&read)[R]) {
+  for (int i = 0; i < W; ++i) {
+    for (int k = i + 1; k < W; ++k)
+      if (overlap(written[i].at, written[i].bytes, written[k].at, written[k].bytes)) return true;
+    for (const MemoryRange& r : read)
+      if (overlap(written[i].at, written[i].bytes, r.at, r.bytes)) return true;
+  }
+  return false;
+}
+
 // Validates the geometry common to all entry points.
 int check_shape(const cocktail_shape* s);
 

@@ -132,8 +132,12 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
   if (workspace_bytes < s.bytes) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, s.bytes);
   const int64_t rows = total * num_q_heads;
   const bool in_place = q == out && (num_q_heads == 1 || stride_h == hd) && (total == 1 || stride_t == int64_t(num_q_heads) * hd);
-  if (!in_place && overlap(out, 2 * rows * hd, q, kv16_extent(cache, stride_t, stride_h, total, num_q_heads)))
-    return fail(COCKTAIL_EINVAL, "out overlaps with q");
+  const cocktail_page_table& pt = cache->pages;
+  const int64_t q_bytes = kv16_extent(cache, stride_t, stride_h, total, num_q_heads), pool_bytes = kv16_pool_bytes(cache);
+  const MemoryRange written[] = {{out, 2 * rows * hd}, {lse, lse ? 4 * rows : 0}, {workspace, int64_t(s.bytes)}};
+  const MemoryRange read[] = {{q, in_place ? 0 : q_bytes}, {cache->k, pool_bytes}, {cache->v, pool_bytes}, {pt.table, 4 * int64_t(pt.num_seqs) * pt.table_stride},
+                              {pt.seq_lens, 4 * int64_t(pt.num_seqs)}, {starts, starts ? 4 * (int64_t(pt.num_seqs) + 1) : 0}};
+  if (overlap(written, read)) return fail(COCKTAIL_EINVAL, "out, lse and workspace overlap with each other or with what the call reads");
   // A wave of the merge per row, fewer than 2^32 threads; refused also where the call needs no merge, so that the limit does not hang on max_len.  (What
   // check_attention and the numbers of sequences and heads leave keeps the other launches below that.)
   if (s.decode && int64_t(cache->pages.num_seqs) * s.rows * cache->num_kv_heads >= int64_t(1) << 26)

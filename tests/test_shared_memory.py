@@ -1,0 +1,98 @@
+"""Memory that results of the paged 16-bit cache and of beam search share with each other or with what a call reads: refused before anything is launched,
+also where only a few bytes are shared; what lies side by side is not."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_23294_amd as ck
+from paper_2503_23294_amd import _lib
+from test_kv16 import Batch
+
+gpu = pytest.mark.gpu
+MB = 1 << 20
+
+
+def _overlap_refused(rc, what):
+    assert rc == _lib.EINVAL, what
+    assert b"overlap" in _lib.lib().cocktail_last_error(), what
+
+
+# where things are, and their bytes: four sequences of up to eight pages of sixteen tokens, 32 pages of 2 heads of 128 channels, eight rows of four heads
+PLACES = dict(table=(MB, 4 * 4 * 8), seq_lens=(2 * MB, 4 * 4), status=(3 * MB, 16), k=(4 * MB, 32 * 2 * 16 * 256), v=(6 * MB, 32 * 2 * 16 * 256), starts=(8 * MB, 4 * 5),
+              q=(9 * MB, 2 * (7 * 1024 + 4 * 128)))
+
+
+def _cache(**more):
+    at = {n: p[0] for n, p in PLACES.items()}
+    at.update(more)
+    pages = _lib.PageTableDesc(at["table"], at["seq_lens"], 20 * MB, at["status"], 4, 8, 16, 32)
+    return C.byref(_lib.Kv16CacheDesc(pages, at["k"], at["v"], 2, 128, _lib.FP16, 0))
+
+
+def _ends(place, size, align):
+    """Addresses of `size` bytes that share a few with a place: its beginning, and its end."""
+    at, n = place
+    return [at - size + align, at, at + (n - 1) // align * align]
+
+
+def test_results_of_attention_over_what_the_call_reads():
+    L = _lib.lib()
+    need = C.c_size_t(0)
+    assert L.cocktail_kv16_attention_workspace(_cache(), 4, 8, 8, 0, 0, C.byref(need)) == 0
+
+    def call(out=10 * MB, lse=11 * MB, ws=12 * MB, st=1024):
+        return L.cocktail_kv16_attention(_cache(), 4, PLACES["q"][0], st, 128, 8, PLACES["starts"][0], 8, 0, 0.0, out, lse, ws, need.value, None)
+    out_bytes, lse_bytes = 8 * 512 * 2, 8 * 4 * 4
+    for name in ("q", "k", "v", "table", "seq_lens", "starts"):
+        for at in _ends(PLACES[name], lse_bytes, 4):
+            _overlap_refused(call(lse=at), ("lse", name, at))
+        for at in _ends(PLACES[name], out_bytes, 16):
+            _overlap_refused(call(out=at), ("out", name, at))
+        for at in _ends(PLACES[name], need.value // 16 * 16, 16):
+            _overlap_refused(call(ws=at), ("workspace", name, at))
+    for at in _ends((10 * MB, out_bytes), lse_bytes, 4):
+        _overlap_refused(call(lse=at), ("lse", "out", at))
+    for at in _ends((12 * MB, need.value), lse_bytes, 4):
+        _overlap_refused(call(lse=at), ("lse", "workspace", at))
+    for at in _ends((12 * MB, need.value), out_bytes, 16):
+        _overlap_refused(call(out=at), ("out", "workspace", at))
+    # in place: the log-sum-exp is elsewhere all the same
+    _overlap_refused(call(out=PLACES["q"][0], lse=PLACES["q"][0] + 512, st=512), "in place")
+
+
+def _carved(dev, *specs):
+    """Tensors side by side in one allocation, sixteen bytes aligned each where their sizes are."""
+    sizes = [int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size() for shape, dtype in specs]
+    flat = torch.zeros(sum(sizes), dtype=torch.uint8, device=dev)
+    out, at = [], 0
+    for (shape, dtype), n in zip(specs, sizes):
+        out.append(flat[at:at + n].view(dtype).view(shape))
+        at += n
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_between_its_neighbours(new):
+    """q, out, lse and both pools without a byte between them; and the calls that are refused leave everything as it is."""
+    B = Batch([300, 77], 2, 128, 16, torch.float16, seed=new)
+    B.store_all()
+    q = B.query([new, new], 4)
+    want, wlse = ck.cocktail_kv16_attention(B.cache, q)
+    f16 = torch.float16
+    k, own, out, lse, v = _carved(B.dev, (B.cache.k.shape, f16), (q.shape, f16), (q.shape, f16), (wlse.shape, torch.float32), (B.cache.v.shape, f16))
+    for to, of in ((k, B.cache.k), (own, q), (v, B.cache.v)):
+        to.view(torch.int16).copy_(of.view(torch.int16))
+    cache = ck.Kv16Cache(B.pages, 2, 128, pools=(k, v))
+    ck.cocktail_kv16_attention(cache, own, out=out, lse=lse)
+    assert torch.equal(out, want) and torch.equal(lse, wlse)
+    kept = [t.view(torch.int16).clone() for t in (k, own, v)]
+    over = lambda t: t.view(-1)[:q.numel()].view(q.shape)  # noqa: E731
+    floats = lambda t: t.view(-1)[:2 * wlse.numel()].view(torch.float32).view(wlse.shape)  # noqa: E731
+    for more in (dict(lse=floats(own)), dict(lse=floats(out), out=out), dict(lse=floats(k)), dict(lse=floats(v)), dict(out=over(k)), dict(out=over(v)),
+                 dict(out=own, lse=floats(own))):
+        with pytest.raises(ck.CocktailError, match="overlap"):
+            ck.cocktail_kv16_attention(cache, own, **more)
+    assert torch.equal(out, want) and all(torch.equal(t.view(torch.int16), old) for t, old in zip((k, own, v), kept))
