@@ -677,8 +677,8 @@ typedef struct cocktail_rotation {
  *   rotation   HOST, or NULL: K is stored as it is, q must be NULL
  *   positions  DEVICE int32 [total]: positions of the rows for the rotation, or NULL: the tokens' numbers in their sequences
  *   q          DEVICE, 16-byte aligned, strides as k's, or NULL
- *   q_out      DEVICE [total][num_q_heads][D], 16-byte aligned; may be q itself where that is laid out the same; otherwise they must
- *              not overlap, nor q_out and k or v.  Rows of a sequence with a bad range are not written.
+ *   q_out      DEVICE [total][num_q_heads][D], 16-byte aligned; may be q itself where that is laid out the same; must not overlap with
+ *              anything else that the call reads or stores to.  Rows of a sequence with a bad range are not written.
  *   num_q_heads  1 .. 65536 with q, else 0
  *
  * One launch.  Errors: EINVAL, EUNSUPPORTED (head_dim, rotary_dim), EALIGN, EHIP.

@@ -232,10 +232,14 @@ extern "C" int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void
   }
   if (!total) return COCKTAIL_OK;
   if (q) {
-    const int64_t written = 2 * total * num_q_heads * hd, rows = kv16_extent(cache, stride_t, stride_h, total, cache->num_kv_heads);
-    if ((q != q_out && overlap(q_out, written, q, kv16_extent(cache, q_stride_t, q_stride_h, total, num_q_heads))) || overlap(q_out, written, k, rows) ||
-        overlap(q_out, written, v, rows))
-      return fail(COCKTAIL_EINVAL, "q_out overlaps with the rows");
+    const cocktail_page_table& pt = cache->pages;
+    const int64_t rows = kv16_extent(cache, stride_t, stride_h, total, cache->num_kv_heads), pool_bytes = kv16_pool_bytes(cache);
+    const MemoryRange written[] = {{q_out, 2 * total * num_q_heads * hd}};
+    const MemoryRange others[] = {{q, q == q_out ? 0 : kv16_extent(cache, q_stride_t, q_stride_h, total, num_q_heads)}, {k, rows}, {v, rows}, {cache->k, pool_bytes}, {cache->v, pool_bytes},
+                                  {pt.table, 4 * int64_t(pt.num_seqs) * pt.table_stride}, {pt.seq_lens, 4 * int64_t(pt.num_seqs)}, {pt.status, 16},
+                                  {starts, starts ? 4 * (int64_t(pt.num_seqs) + 1) : 0}, {positions, positions ? 4 * total : 0},
+                                  {rotation->inv_freq, 4 * int64_t(rotation->rotary_dim)}};
+    if (overlap(written, others)) return fail(COCKTAIL_EINVAL, "q_out overlaps with what the call reads or stores to");
   }
   Kv16Rows r = {};
   r.k = static_cast<const char*>(k);

@@ -16,7 +16,8 @@ MB = 1 << 20
 
 def _overlap_refused(rc, what):
     assert rc == _lib.EINVAL, what
-    assert b"overlap" in _lib.lib().cocktail_last_error(), what
+    message = _lib.lib().cocktail_last_error()
+    assert b"overlap" in message or b"in place only" in message, (what, message)      # (exactly over rows that lie apart)
 
 
 # where things are, and their bytes: four sequences of up to eight pages of sixteen tokens, 32 pages of 2 heads of 128 channels, eight rows of four heads
@@ -62,6 +63,19 @@ def test_results_of_attention_over_what_the_call_reads():
     _overlap_refused(call(out=PLACES["q"][0], lse=PLACES["q"][0] + 512, st=512), "in place")
 
 
+def test_queries_of_append_over_what_the_call_reads_or_stores_to():
+    L = _lib.lib()
+    rows = dict(PLACES, k_rows=(13 * MB, 8 * 256 * 2), v_rows=(14 * MB, 8 * 256 * 2), positions=(15 * MB, 4 * 8), inv_freq=(16 * MB, 8 * 64))
+    turn = C.byref(_lib.RotationDesc(rows["inv_freq"][0], 128, 0, 1.0, 0))
+
+    def call(q_out=10 * MB, st=1024, cache=None):
+        return L.cocktail_kv16_append(cache or _cache(), rows["k_rows"][0], rows["v_rows"][0], 256, 128, 8, rows["starts"][0], turn, rows["positions"][0],
+                                      rows["q"][0], 4, st, 128, q_out, None)
+    for name in rows:
+        for at in _ends(rows[name], 8 * 512 * 2, 16):
+            _overlap_refused(call(at), (name, at))
+
+
 def _carved(dev, *specs):
     """Tensors side by side in one allocation, sixteen bytes aligned each where their sizes are."""
     sizes = [int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size() for shape, dtype in specs]
@@ -96,3 +110,28 @@ def test_attention_between_its_neighbours(new):
         with pytest.raises(ck.CocktailError, match="overlap"):
             ck.cocktail_kv16_attention(cache, own, **more)
     assert torch.equal(out, want) and all(torch.equal(t.view(torch.int16), old) for t, old in zip((k, own, v), kept))
+
+
+@gpu
+def test_append_between_its_neighbours():
+    B = Batch([40, 9], 2, 64, 16, torch.float16, seed=3)
+    q = B.query([40, 9], 3)
+    rot = ck.Rotation(torch.full((32,), 0.1, dtype=torch.float64, device=B.dev))
+    want = ck.cocktail_kv16_append(B.cache, B.k, B.v, B.starts([40, 9]), rotation=rot, q=q)
+    f16 = torch.float16
+    k, q_out, v, rows_k, own, rows_v, _ = _carved(B.dev, *((t.shape, f16) for t in (B.cache.k, q, B.cache.v, B.k, q, B.v, q)))
+    rows_k.copy_(B.k), own.copy_(q), rows_v.copy_(B.v)
+    for to, of in ((k, B.cache.k), (v, B.cache.v)):
+        to.view(torch.int16).copy_(of.view(torch.int16))
+    cache = ck.Kv16Cache(B.pages, 2, 64, pools=(k, v))
+    ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=q_out)
+    same = lambda a, b: torch.equal(a.view(torch.int16), b.view(torch.int16))  # noqa: E731
+    assert same(q_out, want) and same(k, B.cache.k) and same(v, B.cache.v) and same(rows_k, B.k) and same(rows_v, B.v) and same(own, q)
+    kept = [t.clone() for t in (k, v, rows_k, own, rows_v)]
+    for place in (k, v, rows_k, rows_v, own):
+        start = place.storage_offset()
+        room = k.as_strided(q.shape, q.stride(), max(0, start - 8))
+        with pytest.raises(ck.CocktailError, match="overlap"):
+            ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=room)
+    assert all(same(t, old) for t, old in zip((k, v, rows_k, own, rows_v), kept))
+    assert ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=own) is own and same(own, want)
