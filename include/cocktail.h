@@ -669,7 +669,7 @@ typedef struct cocktail_rotation {
  * sequence b (token seq_lens[b] - n + t - starts[b]), k rotated on the way; the queries of the same tokens are rotated into q_out.
  * Call cocktail_pages_resize first, as for cocktail_fp4_store: where it found no room nothing is stored (the queries are rotated all
  * the same), and rows for tokens before the first, or behind what the table row can hold, or on a page that is no page of the
- * pool, are left out.  Nothing else in the pools is written.
+ * pool, are left out.  Nothing else in the pools is written.  The pools must not overlap; k, v and q may lie in them in places that the call does not store to.
  *
  *   k, v       DEVICE, 16-byte aligned; element (t, h, d) at t * stride_t + h * stride_h + d; strides in elements, multiples of 8; of the
  *              cache's dtype, as q and q_out are

@@ -231,9 +231,11 @@ extern "C" int cocktail_kv16_append(const cocktail_kv16_cache* cache, const void
     return fail(COCKTAIL_EINVAL, "without q there are no query heads and no q_out");
   }
   if (!total) return COCKTAIL_OK;
+  const int64_t pool_bytes = kv16_pool_bytes(cache);
+  if (overlap(cache->k, pool_bytes, cache->v, pool_bytes)) return fail(COCKTAIL_EINVAL, "the pools overlap");
   if (q) {
     const cocktail_page_table& pt = cache->pages;
-    const int64_t rows = kv16_extent(cache, stride_t, stride_h, total, cache->num_kv_heads), pool_bytes = kv16_pool_bytes(cache);
+    const int64_t rows = kv16_extent(cache, stride_t, stride_h, total, cache->num_kv_heads);
     const MemoryRange written[] = {{q_out, 2 * total * num_q_heads * hd}};
     const MemoryRange others[] = {{q, q == q_out ? 0 : kv16_extent(cache, q_stride_t, q_stride_h, total, num_q_heads)}, {k, rows}, {v, rows}, {cache->k, pool_bytes}, {cache->v, pool_bytes},
                                   {pt.table, 4 * int64_t(pt.num_seqs) * pt.table_stride}, {pt.seq_lens, 4 * int64_t(pt.num_seqs)}, {pt.status, 16},

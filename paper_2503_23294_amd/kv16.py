@@ -28,7 +28,7 @@ class Kv16Cache:
             if t.dtype != dtype or t.device != pages.device or not t.is_contiguous() or tuple(t.shape) != shape:
                 raise TypeError(f"the pools must be contiguous {dtype} tensors {list(shape)} on {pages.device}")
         self.k, self.v = pools
-        if self.k.data_ptr() == self.v.data_ptr():
+        if abs(self.k.data_ptr() - self.v.data_ptr()) < self.k.nbytes:
             raise ValueError("K and V must have pools of their own")
         self.pages, self.pools, self.dtype = pages, (self.k, self.v), dtype
         self.num_kv_heads, self.head_dim = int(num_kv_heads), int(head_dim)

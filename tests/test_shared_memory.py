@@ -76,6 +76,27 @@ def test_queries_of_append_over_what_the_call_reads_or_stores_to():
             _overlap_refused(call(at), (name, at))
 
 
+def test_pools_that_share_memory():
+    """K and V of a token would be stored over each other."""
+    L = _lib.lib()
+    k, n = PLACES["k"]
+    for v in _ends((k, n), n, 16):
+        _overlap_refused(L.cocktail_kv16_append(_cache(v=v), 13 * MB, 14 * MB, 256, 128, 8, PLACES["starts"][0], None, None, None, 0, 0, 0, None, None), v)
+
+
+@gpu
+def test_a_cache_of_pools_that_share_memory():
+    B = Batch([40, 9], 2, 64, 16, torch.float16)
+    flat = torch.zeros(2 * B.cache.k.numel(), dtype=torch.float16, device=B.dev)
+    n = B.cache.k.numel()
+    at = lambda first: flat[first:first + n].view(B.cache.k.shape)  # noqa: E731
+    for k, v in ((0, 0), (0, n - 8), (n - 8, 0), (8, 0)):
+        with pytest.raises(ValueError):
+            ck.Kv16Cache(B.pages, 2, 64, pools=(at(k), at(v)))
+    for k, v in ((0, n), (n, 0)):
+        ck.Kv16Cache(B.pages, 2, 64, pools=(at(k), at(v)))
+
+
 def _carved(dev, *specs):
     """Tensors side by side in one allocation, sixteen bytes aligned each where their sizes are."""
     sizes = [int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size() for shape, dtype in specs]
