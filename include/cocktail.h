@@ -743,7 +743,7 @@ int cocktail_beam_select(const void* logits, int32_t dtype, int64_t stride_row, 
  * Reorders what hypotheses carry: row r of every state becomes what row source[r] was before the call; rows whose source is negative,
  * or no row, stay as they are.  The counterpart of cocktail_pages_fork for tensors (token histories, recurrent states).
  *
- *   source     DEVICE int32 [rows]
+ *   source     DEVICE int32 [rows]; no state may be written over it
  *   rows       1 .. COCKTAIL_MAX_SEQS
  *   from, to   HOST arrays of num_states DEVICE pointers to contiguous rows; to[i] == from[i] reorders in place, otherwise they must not
  *              overlap; no memory may be written twice in a call

@@ -121,7 +121,8 @@ def cocktail_beam_reorder(source: torch.Tensor, states: Sequence[torch.Tensor], 
     n, index = len(states), dev.index
     if len(result) != n:
         raise ValueError("out must have a tensor for every state")
-    read, written, sizes = [], [], []
+    first = source.data_ptr()
+    read, written, sizes = [(first, first + 4 * rows)], [], []
     for t, o in zip(states, result):
         if t.get_device() != index or not t.is_contiguous() or t.dim() < 1 or t.size(0) != rows:
             raise TypeError(f"states must be contiguous tensors [{rows}, ...] on {dev}")
@@ -136,11 +137,11 @@ def cocktail_beam_reorder(source: torch.Tensor, states: Sequence[torch.Tensor], 
             at = o.data_ptr()
         written.append((at, at + size))
     if n and _overlap(written, read):
-        raise ValueError("states that are written must not overlap with others")
+        raise ValueError("states that are written must not overlap with others or with the sources")
     arrays = _ARRAYS.get(n)
     if arrays is None:
         arrays = _ARRAYS[n] = C.c_void_p * n, C.c_int64 * n
     to = arrays[0](*[a for a, _ in written])
-    of = to if not read else arrays[0](*[t.data_ptr() for t in states])
-    check(lib().cocktail_beam_reorder(source.data_ptr(), rows, of, to, arrays[1](*sizes), n, handle))
+    of = to if len(read) == 1 else arrays[0](*[t.data_ptr() for t in states])   # (all of them in place)
+    check(lib().cocktail_beam_reorder(first, rows, of, to, arrays[1](*sizes), n, handle))
     return result

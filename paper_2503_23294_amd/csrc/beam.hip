@@ -641,6 +641,7 @@ extern "C" int cocktail_beam_reorder(const int32_t* source, int32_t rows, const 
   for (int i = 0; i < num_states; ++i) {
     if (row_bytes[i] < 0 || row_bytes[i] > (int64_t(1) << 40)) return fail(COCKTAIL_EINVAL, "row_bytes of state %d is not in 0 .. 2^40", i);
     if (row_bytes[i] && (!from[i] || !to[i])) return fail(COCKTAIL_EINVAL, "state %d is NULL", i);
+    if (overlap(to[i], row_bytes[i] * rows, source, 4 * int64_t(rows))) return fail(COCKTAIL_EINVAL, "state %d overlaps with the sources", i);
     s.from[i] = static_cast<const char*>(from[i]);
     s.to[i] = static_cast<char*>(to[i]);
     s.row_bytes[i] = row_bytes[i];

@@ -9,6 +9,7 @@ import torch
 import paper_2503_23294_amd as ck
 from paper_2503_23294_amd import _lib
 from test_kv16 import Batch
+from test_kv16_edges import quiet  # noqa: F401 (a fixture)
 
 gpu = pytest.mark.gpu
 MB = 1 << 20
@@ -156,3 +157,55 @@ def test_append_between_its_neighbours():
             ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=room)
     assert all(same(t, old) for t, old in zip((k, v, rows_k, own, rows_v), kept))
     assert ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=own) is own and same(own, want)
+
+
+# ---- reordering --------------------------------------------------------------------------------------------------------------------
+
+
+def _reorder(states, source=MB, rows=4):
+    """states: (from, to, bytes of a row)"""
+    n = len(states)
+    of, to, size = zip(*states)
+    return _lib.lib().cocktail_beam_reorder(source, rows, (C.c_void_p * n)(*of), (C.c_void_p * n)(*to), (C.c_int64 * n)(*size), n, None)
+
+
+@pytest.mark.parametrize("states", [
+    [(MB, MB, 4)],                                          # in place, the sources themselves
+    [(MB - 60, MB - 60, 16)], [(MB + 12, MB + 12, 16)],     # or the last or first word of them
+    [(2 * MB, MB, 4)], [(2 * MB, MB + 15, 1)], [(2 * MB, MB - 3, 1)],
+    [(3 * MB, 3 * MB, 8), (2 * MB, MB + 8, 64)],
+])
+def test_states_that_are_written_over_the_sources(states):
+    _overlap_refused(_reorder(states), states)
+
+
+def test_states_that_are_views_of_the_sources(quiet):
+    source = torch.zeros(12, dtype=torch.int32)
+    state = torch.zeros(4, 6)
+    for states, out in (([source[:4]], None), ([state, source[:8].view(4, 2)], None), ([torch.zeros(4, 1)], [source[:4].view(torch.float32).view(4, 1)]),
+                        ([torch.zeros(4, 2, dtype=torch.int32)], [source[3:11].view(4, 2)])):
+        with pytest.raises(ValueError):
+            ck.cocktail_beam_reorder(source[:4], states, out=out)
+    ck.cocktail_beam_reorder(source[:4], [source[4:8]])                                    # next to them
+    ck.cocktail_beam_reorder(source[:4], [source[:4]], out=[source[4:8]])                  # read twice
+
+
+@gpu
+def test_states_next_to_the_sources():
+    """A state that ends where the sources begin, and one that begins where they end; a history to which the sources themselves are copied."""
+    rows = 300
+    flat = torch.arange(6 * rows, dtype=torch.int32, device="cuda:0")
+    source = flat[2 * rows:3 * rows]
+    source.copy_(torch.arange(rows, device="cuda:0").flip(0))
+    want = flat.clone()
+    a, b, copy = flat[:2 * rows].view(rows, 2), flat[3 * rows:4 * rows], flat[4 * rows:5 * rows]
+    ck.cocktail_beam_reorder(source, [a, b])
+    ck.cocktail_beam_reorder(source, [source], out=[copy])
+    order = source.long()
+    want[:2 * rows] = want[:2 * rows].view(rows, 2)[order].view(-1)
+    want[3 * rows:4 * rows] = want[3 * rows:4 * rows][order]
+    want[4 * rows:5 * rows] = source[order]
+    assert torch.equal(flat, want)
+    with pytest.raises(ValueError):
+        ck.cocktail_beam_reorder(source, [flat[rows:2 * rows + 1][1:], flat[2 * rows + 1:3 * rows + 1]])
+    assert torch.equal(flat, want)
