@@ -745,8 +745,8 @@ int cocktail_beam_select(const void* logits, int32_t dtype, int64_t stride_row, 
  *
  *   source     DEVICE int32 [rows]; no state may be written over it
  *   rows       1 .. COCKTAIL_MAX_SEQS
- *   from, to   HOST arrays of num_states DEVICE pointers to contiguous rows; to[i] == from[i] reorders in place, otherwise they must not
- *              overlap; no memory may be written twice in a call
+ *   from, to   HOST arrays of num_states DEVICE pointers to contiguous rows; to[i] == from[i] reorders in place.  No memory may be written
+ *              twice in a call, and none that is copied to may be copied from (what is reordered in place may: the copies are made first)
  *   row_bytes  HOST int64 [num_states], bytes of a row of each state; any number up to 2^40 (whole pieces of 16 bytes are fastest, then of 4)
  *   num_states 0 .. COCKTAIL_MAX_STATES
  *

@@ -1,6 +1,7 @@
 // cocktail_beam_select / cocktail_beam_reorder: a step of beam search over the logits, and the reordering of what its hypotheses carry.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
@@ -552,6 +553,31 @@ int plan_select(int32_t groups, int32_t beams, int32_t vocab, int32_t keep, Sele
   return COCKTAIL_OK;
 }
 
+// Whether states are written over each other, or over what others are copied from while they are.  (What is in place may be copied from too: the
+// copies are made first.)
+bool states_overlap(const BeamStates& s) {
+  enum { kRead, kWritten, kInPlace };
+  struct Span {
+    uint64_t first, end;
+    int kind;
+  } spans[2 * COCKTAIL_MAX_STATES];
+  int n = 0;
+  for (int i = 0; i < s.num_states; ++i) {
+    const uint64_t from = reinterpret_cast<uintptr_t>(s.from[i]), to = reinterpret_cast<uintptr_t>(s.to[i]), bytes = uint64_t(s.row_bytes[i]) * s.rows;
+    if (!bytes) continue;
+    spans[n++] = {to, to + bytes, from == to ? kInPlace : kWritten};
+    if (from != to) spans[n++] = {from, from + bytes, kRead};
+  }
+  std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.first < b.first; });
+  uint64_t end[3] = {};   // of the spans of each kind so far
+  for (int i = 0; i < n; ++i) {
+    const Span& x = spans[i];
+    if (x.first < end[kWritten] || (x.kind != kRead && x.first < end[kInPlace]) || (x.kind == kWritten && x.first < end[kRead])) return true;
+    end[x.kind] = std::max(end[x.kind], x.end);
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" int cocktail_beam_select_workspace(int32_t groups, int32_t beams, int32_t vocab, int32_t keep, size_t* bytes) {
@@ -648,6 +674,7 @@ extern "C" int cocktail_beam_reorder(const int32_t* source, int32_t rows, const 
     if (from[i] == to[i]) columns += (row_bytes[i] + width - 1) / width;
     else copies += (row_bytes[i] + kCopyBytes - 1) / kCopyBytes;
   }
+  if (states_overlap(s)) return fail(COCKTAIL_EINVAL, "states are written over each other, or overlap with what they are copied from");
   if (copies * rows >= (int64_t(1) << 24) || copies >= (int64_t(1) << 24) || columns >= (int64_t(1) << 24))
     return fail(COCKTAIL_EINVAL, "the states are more than one launch takes");
   hipError_t e = hipSuccess;

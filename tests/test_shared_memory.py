@@ -179,6 +179,22 @@ def test_states_that_are_written_over_the_sources(states):
     _overlap_refused(_reorder(states), states)
 
 
+@pytest.mark.parametrize("states", [
+    [(2 * MB, 2 * MB, 16), (2 * MB, 2 * MB, 16)],           # written twice, in place and not
+    [(2 * MB, 2 * MB, 16), (2 * MB + 63, 2 * MB + 63, 1)],
+    [(2 * MB, 3 * MB, 16), (4 * MB, 3 * MB + 60, 32)],
+    [(2 * MB, 3 * MB, 16), (3 * MB - 4, 3 * MB - 4, 2)],
+    [(2 * MB, 2 * MB + 16, 16)],                            # read and written
+    [(2 * MB, 2 * MB - 63, 16)],
+    [(2 * MB, 3 * MB, 16), (3 * MB, 4 * MB, 16)],
+    [(2 * MB, 3 * MB, 16), (3 * MB - 124, 4 * MB, 32)],
+    [(5 * MB, 6 * MB, 1), (2 * MB, 3 * MB, 16), (7 * MB, 8 * MB, 4), (9 * MB, 9 * MB, 64), (9 * MB, 2 * MB + 32, 4)],
+])
+def test_states_that_are_written_over_each_other(states):
+    for order in (states, states[::-1]):
+        _overlap_refused(_reorder(order), order)
+
+
 def test_states_that_are_views_of_the_sources(quiet):
     source = torch.zeros(12, dtype=torch.int32)
     state = torch.zeros(4, 6)
@@ -208,4 +224,19 @@ def test_states_next_to_the_sources():
     assert torch.equal(flat, want)
     with pytest.raises(ValueError):
         ck.cocktail_beam_reorder(source, [flat[rows:2 * rows + 1][1:], flat[2 * rows + 1:3 * rows + 1]])
+    assert torch.equal(flat, want)
+
+
+@gpu
+def test_a_state_that_is_copied_and_then_reordered_in_place():
+    """By the C entry: the copy has what the state was before the call."""
+    rows, dev = 50, "cuda:0"
+    rng = np.random.default_rng(1)
+    flat = torch.from_numpy(rng.integers(0, 1 << 30, 3 * rows * 700)).to(dev, torch.int32).view(3, rows, 700)
+    source = torch.from_numpy(rng.integers(0, rows, rows)).to(dev, torch.int32)
+    want = flat.clone()
+    want[0] = want[1] = flat[1][source.long()]
+    a, b = flat[0].data_ptr(), flat[1].data_ptr()
+    assert _lib.lib().cocktail_beam_reorder(source.data_ptr(), rows, (C.c_void_p * 2)(b, b), (C.c_void_p * 2)(a, b), (C.c_int64 * 2)(2800, 2800), 2,
+                                            torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(flat, want)
