@@ -728,7 +728,7 @@ int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t num_q_head
  *   workspace DEVICE, cocktail_beam_select_workspace bytes, 16-byte aligned, not initialised; shared between calls as that of
  *             cocktail_fp4_attention
  *
- * Exponentials and sums of up to eight of them in binary32, longer sums and the candidates' values in binary64.  The results may not overlap
+ * Exponentials and sums of up to eight of them in binary32, longer sums and the candidates' values in binary64.  Results and workspace may not overlap
  * with each other or the inputs, but for score over scores and finished_out over finished where keep == beams.
  * Calls on the same inputs agree bit for bit.  Two launches.  Errors: EINVAL, EALIGN, ENOSPACE, EHIP.
  */

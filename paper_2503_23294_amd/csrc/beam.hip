@@ -609,21 +609,10 @@ extern "C" int cocktail_beam_select(const void* logits, int32_t dtype, int64_t s
   if (workspace_bytes < s.bytes) return fail(COCKTAIL_ENOSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, s.bytes);
   const int64_t rows = int64_t(groups) * beams, places = int64_t(groups) * keep;
   const int64_t all_logits = ((rows - 1) * stride_row + vocab) * (dtype == COCKTAIL_FP32 ? 4 : 2);
-  struct Range {
-    const void* at;
-    int64_t bytes;
-  };
-  const Range results[] = {{source, 4 * places}, {token, 4 * places}, {score, 4 * places}, {finished_out, finished_out ? places : 0}};
-  const Range inputs[] = {{logits, all_logits}, {scores, 4 * rows}, {finished, finished ? rows : 0}};
-  for (const Range& x : results) {
-    bool bad = false;
-    for (const Range* y = &x + 1; y < results + 4; ++y) bad = bad || overlap(x.at, x.bytes, y->at, y->bytes);
-    for (const Range& y : inputs) {
-      const bool in_place = x.at == y.at && ((x.at == score && y.at == scores) || (x.at == finished_out && y.at == finished));
-      bad = bad || (!in_place && overlap(x.at, x.bytes, y.at, y.bytes));
-    }
-    if (bad) return fail(COCKTAIL_EINVAL, "results overlap with each other or with the inputs");
-  }
+  // (a result in the place of its own input is none that overlaps with it)
+  const MemoryRange written[] = {{source, 4 * places}, {token, 4 * places}, {score, 4 * places}, {finished_out, finished_out ? places : 0}, {workspace, int64_t(s.bytes)}};
+  const MemoryRange read[] = {{logits, all_logits}, {scores, score == scores ? 0 : 4 * rows}, {finished, finished && finished_out != finished ? rows : 0}};
+  if (overlap(written, read)) return fail(COCKTAIL_EINVAL, "results or workspace overlap with each other or with the inputs");
   BeamSelect a = {};
   a.logits = logits;
   a.stride_row = stride_row;

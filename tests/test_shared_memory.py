@@ -159,6 +159,19 @@ def test_append_between_its_neighbours():
     assert ck.cocktail_kv16_append(cache, rows_k, rows_v, B.starts([40, 9]), rotation=rot, q=own, q_out=own) is own and same(own, want)
 
 
+def test_the_workspace_of_a_selection():
+    L = _lib.lib()
+    need = C.c_size_t(0)
+    assert L.cocktail_beam_select_workspace(2, 4, 100, 4, C.byref(need)) == 0
+    places = dict(logits=(MB, 4 * (7 * 128 + 100)), scores=(2 * MB, 32), finished=(3 * MB, 8), source=(4 * MB, 32), token=(5 * MB, 32), score=(6 * MB, 32),
+                  out=(7 * MB, 8))
+    p = {n: at for n, (at, _) in places.items()}
+    for name in places:
+        for ws in _ends(places[name], need.value // 16 * 16, 16):
+            _overlap_refused(L.cocktail_beam_select(p["logits"], _lib.FP32, 128, 2, 4, 100, 4, p["scores"], p["finished"], 7, p["source"], p["token"], p["score"],
+                                                    p["out"], ws, need.value, None), (name, ws))
+
+
 # ---- reordering --------------------------------------------------------------------------------------------------------------------
 
 
