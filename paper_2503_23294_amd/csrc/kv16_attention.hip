@@ -196,11 +196,14 @@ extern "C" int cocktail_kv16_attention(const cocktail_kv16_cache* cache, int32_t
     int most_new = kDecodeRows / a.rep < max_new ? kDecodeRows / a.rep : max_new;
     if (int64_t(cache->pages.num_seqs) * most_new > 4 * total) most_new = 0;
     const uint32_t most = uint32_t(most_new ? int64_t(cache->pages.num_seqs) * most_new : total) * num_q_heads;
-    // states that a row has, about: many of them are read by many waves at a time, a few by one
-    const int parts = int(s.workers / (s.active * cache->num_kv_heads));
-    if (parts >= 16 && most <= 512)
+    // States that a row has, about: one for a share, or, where workgroups leave one, for their waves' shares together.  Many of them are read by many waves at a
+    // time, a few by one (calls on contexts of 16384 tokens, heads of 128, us with 1, 4, 16 waves: 128 states of 1, 16, 64 rows 24.5, 13.2, 12.5; 26.4, 15.0, 13.9;
+    // 32.7, 21.1, 20.5; 64 of 4, 64, 256 rows 18.5, 13.2, 13.2; 19.9, 14.2, 14.4; 33.4, 29.9, 29.9; 32 of 8, 512 rows 21.8, 18.9, 19.8; 50.4, 49.3, 51.5; 16 of 256, 1024
+    // rows 86.2, 85.5, 86.4; 90.8, 91.1, 97.4; 12 of 340, 1360 rows 112.5, 112.1, 114.5; 118.4, 119.9, 128.1; 8 of 1024 rows 49.5, 50.3, 55.1).
+    const int states = int(s.workers / (s.active * cache->num_kv_heads) / (a.joins ? kDecodeWaves : 1));
+    if (states >= 96 && most <= 512)
       e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 16> : merge_decode_kernel<Kv16Cost, 64, 16>, dim3(most), dim3(1024), st, a, most_new);
-    else if (parts >= 12 && most <= 2048)
+    else if (states >= 10 && most <= 1024)
       e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 4> : merge_decode_kernel<Kv16Cost, 64, 4>, dim3(most), dim3(256), st, a, most_new);
     else
       e = launch(hd == 128 ? merge_decode_kernel<Kv16Cost, 128, 1> : merge_decode_kernel<Kv16Cost, 64, 1>, dim3((most + 3) / 4), dim3(256), st, a, most_new);
