@@ -12,8 +12,9 @@
 //    The result layout of S^T (lane: a query row, tokens 4 j + x) is the operand layout of P^T with tokens numbered accordingly: weights
 //    never leave their lane.
 //  * Codes become fp16 with one instruction per pair that applies the scale as well.
-//  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4 (exact, the result does not depend on it), so that the
-//    common step has no exchange between lanes at all.
+//  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4, so that the common step has no exchange
+//    between lanes at all.  (What is there is multiplied by a power of two with a real exponent then, and weights are rounded against another reference: when
+//    that takes place shows in the last bits, and is the same for the same inputs.)
 #pragma once
 #include "fp4_common.h"
 #include "paged_attention.h"

@@ -12,8 +12,9 @@
 //    load; pairs of tokens are put together by one byte permutation each, and are the operands of O^T = V^T P^T with the channels 8 c + t of product t.
 //    The result layout of S^T (lane: a query row, tokens 4 j + x) is the operand layout of P^T with tokens numbered accordingly: weights
 //    never leave their lane.
-//  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4 (exact, the result does not depend on it), so that the
-//    common step has no exchange between lanes at all.
+//  * The reference of the weights is only raised when a logit exceeds what it was made for by 2^4, so that the common step has no exchange
+//    between lanes at all.  (What is there is multiplied by a power of two with a real exponent then, and weights are rounded against another reference: when
+//    that takes place shows in the last bits, and is the same for the same inputs.)
 #pragma once
 #include <type_traits>
 
