@@ -116,6 +116,8 @@ def cocktail_beam_reorder(source: torch.Tensor, states: Sequence[torch.Tensor], 
         return result
     rows = source.numel()
     _vector("source", source, (torch.int32,), rows, dev)
+    if rows < 1:
+        raise ValueError("source must have a row at least")
     states = list(states)
     result = states if out is None else list(out)
     n, index = len(states), dev.index

@@ -253,3 +253,10 @@ def test_a_state_that_is_copied_and_then_reordered_in_place():
     assert _lib.lib().cocktail_beam_reorder(source.data_ptr(), rows, (C.c_void_p * 2)(b, b), (C.c_void_p * 2)(a, b), (C.c_int64 * 2)(2800, 2800), 2,
                                             torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(flat, want)
+
+
+def test_reordering_of_no_rows_is_refused(quiet):
+    none = torch.zeros(0, dtype=torch.int32)
+    for states, out in (([torch.zeros(0, 3)], None), ([torch.zeros(0, 3)], [torch.zeros(0, 3)]), ([], None)):
+        with pytest.raises(ValueError):
+            ck.cocktail_beam_reorder(none, states, out=out)
