@@ -69,7 +69,7 @@ Split split_of(const cocktail_kv16_cache* c, int rep, int64_t total, int64_t max
     if (s.work == kGroupShares) s.workers = int(workers /= kDecodeWaves);
     if (whole) workers = 0;
     // Whether a workgroup's waves leave one state where all have parts of one segment: less to write and to read for the merge, which else takes (2 heads
-    // of one kv head, 84K tokens, 880 states) 20.7 us, joined 9.8; 7 of one, 4.7K 7.5, 5.8; 32 of 8, 20K 6.2, 5.1; but 8 of 8, 2K, 64 states 5.4, 5.7.  Of
+    // of one kv head, 84K tokens, 880 states) 20.3 us, joined 9.8; 7 of one, 4.7K 7.4, 5.9; 32 of 8, 20K 6.2, 5.2; but 8 of 8, 2K, 64 states 4.8, 4.8.  Of
     // many rows states are large (verification behind 16K, 16 states of 48 rows: both kernels 74.8, 73.5).
     s.joins = s.work == kWaveShares && workers > (s.row_tiles > 1 ? 8 : 64) * segments;
     s.prefix_bytes = (size_t(c->pages.num_seqs) + 1 + 63) / 64 * 256;

@@ -5,8 +5,8 @@
 // pieces of sixteen bytes, and serve all waves.  What a load of the products' operands touches is in different banks: of K, the same piece of
 // sixteen rows, which are a piece longer than their channels; of V, which the transposing load reads, 32 bytes of four rows twice, whose pieces lie
 // in an order of the row's own.
-// Measured (averages): 2048 tokens of 4 x 8 heads of 128 behind 30K 0.99 .. 1.02 ms (1.05 .. 1.08 PFLOP/s; a large library product of fp16 matrices reaches 1.30, at a
-// lower clock: power is a limit of both), a prompt of 16384 tokens, 32 heads 1.97 ms (1.11, of the products that are not masked), two of 8190 and 4095 0.70 (0.99).
+// Measured (averages): 2048 tokens of 4 x 8 heads of 128 behind 30K 0.99 .. 1.03 ms by card (1.04 .. 1.08 PFLOP/s; a large library product of fp16 matrices reaches 1.30, at a
+// lower clock: power is a limit of both), a prompt of 16384 tokens, 32 heads 1.97 ms (1.11, of the products that are not masked), two of 8190 and 4095 0.70 .. 0.74 (0.93 .. 0.99).
 // S^T = K Q^T leaves a lane with one query row and half the keys of a step, in the order in which O^T = V^T P^T takes them (the transposing load
 // picks the tokens in that order), so weights stay in their lanes.
 #pragma once
